@@ -711,6 +711,166 @@ rmm_status_t rmm_decode_products_shared(const rmm_decode_group_t *groups, int ng
 rmm_status_t rmm_decode_step_shared(const rmm_decode_group_t *groups, int ngroups, int64_t B,
                                     void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Position rotation, a paged key/value cache and attention over it   (Sec. 3.3
+ * and App. A: what stands between a layer's reduced projections and its
+ * reduced attention when a model is served; not part of RMM itself).
+ *
+ * rmm_heads_t: n heads of D contiguous elements per token; batch entry b, token
+ * t, head h begins at data + b*batch_stride + t*token_stride + h*head_stride
+ * (in elements, >= 0).  data is 16-byte aligned and the strides are multiples
+ * of 16 bytes, so a slice of a projection's output rows can be passed.
+ * rmm_rope_t : float32 tables cos and sin [n_pos][rot/2] (16-byte aligned); the
+ * first rot dims of a head (a multiple of 16, at most D) are rotated in pairs
+ * (i, i + rot/2), or (2i, 2i+1) when interleaved != 0.
+ */
+typedef struct rmm_heads {
+    void *data;
+    int64_t n, batch_stride, token_stride, head_stride;
+} rmm_heads_t;
+typedef struct rmm_rope {
+    const float *cos, *sin;
+    int64_t n_pos, rot;
+    int interleaved;
+} rmm_rope_t;
+
+/*
+ * Per-head RMSNorm and position rotation of queries and keys in one pass.
+ *
+ *   y   = x * r * gamma, r = 1/sqrt(mean over D of x^2 + eps)   (gamma given)
+ *   out = y with each pair (u, w) of dims replaced by (u c - w s, w c + u s),
+ *         c, s = cos, sin[positions[b*L + t]][pair]             (rope given)
+ *   energy[(b*H + h)*D + j] = sum over t of q_out[b][t][h][j]^2 (energy given):
+ *         what rmm_score gives for q_out laid out [batch*H][L][D], for rmm_select
+ *
+ * The mean square is formed in float64 and r rounded to fp32; norm and
+ * rotation are evaluated in fp32, each product and sum rounded by itself, and
+ * rounded once to the output type.  Energies are float64 sums of the stored
+ * values' squares in a fixed order.  A position outside [0, n_pos) gives NaN.
+ * q_out may be q itself (same strides), k_out k.
+ *
+ * dtype     : RMM_BF16 or RMM_F32, of q, k, outputs and gammas.
+ * q, k      : [batch][L] heads, either may be NULL with its output (energy needs
+ *             q); gamma_q, gamma_k: [D], 16-byte aligned, or NULL (no norm).
+ * rope      : or NULL (no rotation; positions is then not read).
+ * positions : int32 [batch*L].     energy: float64 [batch*H*D] or NULL.
+ * workspace : rmm_qk_norm_rope_workspace_size(batch, H, L, D) bytes with energy,
+ *             8-byte aligned (may be NULL when that size is 0 or energy is NULL).
+ * Errors    : INVALID_ARGUMENT for null pointers, sizes < 1, output head counts
+ *             that differ, negative strides, eps negative, infinite or NaN, rot
+ *             outside [0, D] or n_pos < 1 with rot > 0; UNSUPPORTED unless D is 64 or 128, rot % 16 == 0, the
+ *             alignments above hold, batch*L < 2^31 and there are fewer than
+ *             2^16 heads; WORKSPACE_TOO_SMALL.
+ */
+size_t rmm_qk_norm_rope_workspace_size(int64_t batch, int64_t H, int64_t L, int64_t D);
+rmm_status_t rmm_qk_norm_rope(rmm_dtype_t dtype, int64_t batch, int64_t L, int64_t D, const rmm_heads_t *q,
+                              const rmm_heads_t *q_out, const rmm_heads_t *k, const rmm_heads_t *k_out,
+                              const void *gamma_q, const void *gamma_k, float eps, const rmm_rope_t *rope,
+                              const int32_t *positions, double *energy, void *workspace,
+                              size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A paged key/value cache: n_pages pages of page_size tokens.  Page p of each
+ * array begins p * its stride BYTES after its pointer and holds
+ * [Hkv][page_size] rows.
+ *   RMM_CACHE_BF : k, v rows of D bf16 (k_scale, v_scale unused).
+ *   RMM_CACHE_MX : MXFP4.  k, v rows of D/2 bytes, two e2m1 codes each (values 0,
+ *                  .5, 1, 1.5, 2, 3, 4, 6 and their negatives), the even dim in the
+ *                  low half; k_scale, v_scale rows of D/32 bytes s, one per 32
+ *                  dims: the codes stand for 2^(s - 127) times their value, and
+ *                  for NaN when s is 255.
+ * The slot of a token is page * page_size + its place in the page.
+ * page_size is a power of two, 16 to 1024; D is 64 or 128; pointers and strides
+ * are multiples of 16 bytes; n_pages * page_size < 2^31.
+ */
+typedef enum rmm_cache_type {
+    RMM_CACHE_BF = 0,
+    RMM_CACHE_MX = 1
+} rmm_cache_type_t;
+typedef struct rmm_kv_cache {
+    rmm_cache_type_t type;
+    void *k, *v, *k_scale, *v_scale;
+    int64_t n_pages, page_size, Hkv, D;
+    int64_t k_stride, v_stride, k_scale_stride, v_scale_stride;
+} rmm_kv_cache_t;
+
+/*
+ * Appends T tokens' keys and values to the cache, the keys normed and rotated
+ * on the way (as rmm_qk_norm_rope), and optionally norms and rotates their
+ * queries: a decode step's whole pass between the projections and the
+ * attention.
+ *
+ * k, v      : [T] bf16, Hkv heads (batch_stride unused).   q, q_out: H heads, or
+ *             both NULL.  gamma_q, gamma_k, eps, rope, positions [T]: as
+ *             rmm_qk_norm_rope (values are neither normed nor rotated).
+ * slots     : int32 [T]; a token whose slot is outside the cache (e.g. -1) is
+ *             not appended.  Slots of one call should differ: of tokens with the same
+ *             slot, each 8-element piece is some one's.
+ * RMM_CACHE_MX: each group of 32 dims takes the smallest scale at which its
+ *             largest magnitude, rounded, is at most 6 (s kept within 8..252;
+ *             255 when the group holds a NaN or an infinity), and rounds each
+ *             value to the nearest code, ties to the even one -- the keys from
+ *             their fp32 values.
+ * Only the T tokens' rows of the cache are written.
+ * Errors    : as rmm_qk_norm_rope and for a cache that breaks the rules above.
+ */
+rmm_status_t rmm_kv_append(int64_t T, const rmm_heads_t *k, const rmm_heads_t *v, const int32_t *slots,
+                           const rmm_kv_cache_t *cache, const void *gamma_k, const rmm_heads_t *q,
+                           const rmm_heads_t *q_out, const void *gamma_q, float eps, const rmm_rope_t *rope,
+                           const int32_t *positions, hipStream_t stream);
+
+/*
+ * Reads T cached tokens back as bf16 rows (MXFP4 values are exact in bf16 for
+ * every scale rmm_kv_append writes); a slot outside the cache gives zeros.
+ * k, v : [T] heads, written (any strides: e.g. [Hkv][T][D] for
+ * rmm_reduced_attention).  Errors: as rmm_kv_append.
+ */
+rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, int64_t T, const rmm_heads_t *k,
+                           const rmm_heads_t *v, hipStream_t stream);
+
+/*
+ * Attention of new tokens over a paged cache, with the per-head reduced scores
+ * of rmm_reduced_attention when lists are given   (Sec. 3.3 "Attention"; App. A:
+ * in decoding a set follows its token).
+ *
+ * Sequence b < B has n = q_start[b+1] - q_start[b] new tokens, rows q_start[b] ..
+ * of q (q_start NULL: T == B, one each), and lengths[b] cached keys, key s at
+ * row s % page_size of page page_table[b*table_stride + s / page_size].  For
+ * new token j of it and query head h (kv head h / (H / Hkv)):
+ *   o[j][h] = sum over s of P[s] V[s],  P = softmax over the keys s it sees of
+ *             scale * sum over d in I of q[j][h][d] K[s][d]
+ * It sees s <= lengths[b] - n + j when causal (the new tokens are the cache's
+ * last n), else s < lengths[b] (e.g. an encoder's states).  A token that sees
+ * no key gets 0.  I = idx[(t*H + h)*k ..) for token t (rmm_select_tokens on the rows of
+ * q), or all dims when idx is NULL (k ignored).  A key value that is infinite
+ * or NaN in a dim outside I, or past what a token sees, has no effect on it.
+ * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
+ * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.
+ *
+ * Rows of o that belong to no sequence are left as they were.  q_start is
+ * ascending from 0 (what it says past T is cut off); a length < 0 counts as 0.  A length beyond max_pages *
+ * page_size, or a page number outside the cache among the pages a sequence
+ * uses, makes its outputs NaN.  Any dim outside [0, D) in a list is ignored.
+ *
+ * q, o      : [T] bf16, H heads (batch_stride unused; o may be q).
+ * page_table: int32 [B][table_stride], max_pages entries used per row.
+ * lengths   : int32 [B].   q_start: int32 [B+1] or NULL.   idx: int32 [T*H*k].
+ * workspace : rmm_paged_attention_workspace_size(T, B, H, Hkv, D) bytes, 256-byte
+ *             aligned (partial outputs; overwritten by every call).
+ * Errors    : INVALID_ARGUMENT for null pointers, T, B, max_pages < 1,
+ *             table_stride < max_pages, q_start NULL with T != B, H not a
+ *             multiple of the cache's Hkv, o's head count not H, k outside
+ *             [1, D], a misaligned workspace; UNSUPPORTED for a cache or
+ *             strides that break the rules above, max_pages * page_size > 2^30 or
+ *             T*H >= 2^31; WORKSPACE_TOO_SMALL.
+ */
+size_t rmm_paged_attention_workspace_size(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D);
+rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_cache_t *cache,
+                                 const int32_t *page_table, int64_t table_stride, int64_t max_pages,
+                                 const int32_t *lengths, int64_t B, const int32_t *q_start,
+                                 const int32_t *idx, int64_t k, float scale, int causal, const rmm_heads_t *o,
+                                 void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char *rmm_status_string(rmm_status_t status);
 

@@ -27,13 +27,16 @@ __all__ = [
     "rmm_decode_step_workspace_size", "rmm_decode_products", "rmm_decode_products_shared",
     "rmm_decode_products_shared_workspace_size", "rmm_decode_step_shared", "DecodeGroup",
     "rmm_reduced_qk_rowstats",
-    "rmm_attention_weights_kmajor_rowstats", "EXPORTED_SYMBOLS",
+    "rmm_attention_weights_kmajor_rowstats", "RMM_CACHE_BF", "RMM_CACHE_MX", "Rope", "rope_tables", "KvCache",
+    "kv_cache", "rmm_qk_norm_rope", "rmm_qk_norm_rope_workspace_size", "rmm_kv_append", "rmm_kv_gather",
+    "rmm_paged_attention", "rmm_paged_attention_workspace_size", "EXPORTED_SYMBOLS",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librmm.so")
 
 RMM_F32, RMM_BF16 = 0, 1
 RMM_OP_SCORE, RMM_OP_SELECT, RMM_OP_LINEAR, RMM_OP_ATTENTION, RMM_OP_PV = 0, 1, 2, 3, 4
+RMM_CACHE_BF, RMM_CACHE_MX = 0, 1
 
 _p = ctypes.c_void_p
 _i64 = ctypes.c_int64
@@ -43,6 +46,28 @@ class DecodeGroup(ctypes.Structure):
     """rmm_decode_group_t: one projection group of a decode step."""
     _fields_ = [("X", _p), ("W", _p), ("idx", _p), ("Y", _p), ("K", _i64), ("N", _i64),
                 ("k", _i64), ("ldx", _i64), ("ldw", _i64), ("ldy", _i64)]
+
+
+class _Heads(ctypes.Structure):
+    """rmm_heads_t"""
+    _fields_ = [("data", _p), ("n", _i64), ("batch_stride", _i64), ("token_stride", _i64),
+                ("head_stride", _i64)]
+
+
+class _RopeTables(ctypes.Structure):
+    """rmm_rope_t"""
+    _fields_ = [("cos", _p), ("sin", _p), ("n_pos", _i64), ("rot", _i64), ("interleaved", ctypes.c_int)]
+
+
+class _KvCacheC(ctypes.Structure):
+    """rmm_kv_cache_t"""
+    _fields_ = [("type", ctypes.c_int), ("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p),
+                ("n_pages", _i64), ("page_size", _i64), ("Hkv", _i64), ("D", _i64), ("k_stride", _i64),
+                ("v_stride", _i64), ("k_scale_stride", _i64), ("v_scale_stride", _i64)]
+
+
+_ph, _pr, _pc = ctypes.POINTER(_Heads), ctypes.POINTER(_RopeTables), ctypes.POINTER(_KvCacheC)
+
 _SIGS = {
     "rmm_retained_count": (_i64, [ctypes.c_double, _i64]),
     "rmm_workspace_size": (ctypes.c_size_t, [ctypes.c_int, _i64, _i64, _i64, _i64]),
@@ -107,6 +132,15 @@ _SIGS = {
                                                     _i64, _i64, _i64, _i64, ctypes.c_float,
                                                     ctypes.c_int, _p, _i64, _p, _p, ctypes.c_size_t,
                                                     _p]),
+    "rmm_qk_norm_rope_workspace_size": (ctypes.c_size_t, [_i64, _i64, _i64, _i64]),
+    "rmm_qk_norm_rope": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _i64, _ph, _ph, _ph, _ph, _p, _p,
+                                        ctypes.c_float, _pr, _p, _p, _p, ctypes.c_size_t, _p]),
+    "rmm_kv_append": (ctypes.c_int, [_i64, _ph, _ph, _p, _pc, _p, _ph, _ph, _p, ctypes.c_float, _pr, _p,
+                                     _p]),
+    "rmm_kv_gather": (ctypes.c_int, [_pc, _p, _i64, _ph, _ph, _p]),
+    "rmm_paged_attention_workspace_size": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i64]),
+    "rmm_paged_attention": (ctypes.c_int, [_i64, _ph, _pc, _p, _i64, _i64, _p, _i64, _p, _p, _i64,
+                                           ctypes.c_float, ctypes.c_int, _ph, _p, ctypes.c_size_t, _p]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -857,3 +891,242 @@ def rmm_decode_step(groups, workspace: torch.Tensor | None = None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check("rmm_decode_step", lib.rmm_decode_step(arr, len(groups), B, _ptr(workspace), ws_bytes,
                                                   _stream(d, stream)))
+
+
+# ------------------------------------------- rotation and the paged cache
+
+def rope_tables(n_pos: int, rot: int, theta: float = 10000.0, device="cuda"):
+    """(cos, sin) float32 [n_pos, rot/2] of the angles pos * theta^(-2i/rot),
+    evaluated in float64 (made once at load time)."""
+    if rot < 2 or rot % 2 or n_pos < 1:
+        raise ValueError("rot must be even and positive, n_pos at least 1")
+    f = float(theta) ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    a = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * f
+    return a.cos().float(), a.sin().float()
+
+
+class Rope:
+    """The position rotation of a model: cos and sin tables (float32 [n_pos,
+    rot/2]); pairs (i, i + rot/2), or (2i, 2i + 1) when interleaved."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False):
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must be [n_pos, rot/2]")
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32:
+            raise TypeError("cos and sin must be float32")
+        if not (cos.is_contiguous() and sin.is_contiguous()):
+            raise ValueError("cos and sin must be contiguous")
+        _dev(cos, sin)
+        self.cos, self.sin, self.interleaved = cos, sin, bool(interleaved)
+        self._c = _RopeTables(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(self.interleaved))
+
+
+class KvCache:
+    """A paged key/value cache over caller-made tensors (pages may be strided,
+    each page contiguous): bf16 k, v [n_pages, Hkv, page_size, D]; or MXFP4
+    uint8 k, v [n_pages, Hkv, page_size, D/2] with uint8 k_scale, v_scale
+    [n_pages, Hkv, page_size, D/32]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None):
+        mx = k.dtype == torch.uint8
+        if k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.uint8):
+            raise TypeError("k and v must both be bfloat16, or both uint8 (MXFP4 codes)")
+        if (k_scale is None) != (not mx) or (v_scale is None) != (not mx):
+            raise ValueError("an MXFP4 cache takes k_scale and v_scale, a bf16 cache neither")
+        if k.dim() != 4 or k.shape != v.shape:
+            raise ValueError("k and v must be [n_pages, Hkv, page_size, row]")
+        n_pages, Hkv, page_size, row = k.shape
+        D = 2 * row if mx else row
+        held = (k, v, k_scale, v_scale) if mx else (k, v)
+        if mx:
+            for t in held[2:]:
+                if t.dtype != torch.uint8 or tuple(t.shape) != (n_pages, Hkv, page_size, D // 32):
+                    raise ValueError("scales must be uint8 [n_pages, Hkv, page_size, D/32]")
+        for t in held:
+            if t.stride(3) != 1 or t.stride(2) != t.shape[3] or \
+                    (Hkv > 1 and t.stride(1) != page_size * t.shape[3]):
+                raise ValueError("each page must be contiguous")
+        self.device = _dev(*held)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.Hkv, self.page_size, self.D, self.mx = n_pages, Hkv, page_size, D, mx
+        strides = [t.stride(0) * t.element_size() for t in held] + [0, 0]
+        self._c = _KvCacheC(RMM_CACHE_MX if mx else RMM_CACHE_BF, k.data_ptr(), v.data_ptr(), _ptr(k_scale),
+                            _ptr(v_scale), n_pages, page_size, Hkv, D, *strides[:4])
+
+
+def kv_cache(n_pages: int, Hkv: int, page_size: int, D: int, mx: bool = False, device="cuda") -> KvCache:
+    """A cache of zeros: bf16, or MXFP4 with mx."""
+    if not mx:
+        return KvCache(*(torch.zeros(n_pages, Hkv, page_size, D, dtype=torch.bfloat16, device=device)
+                         for _ in range(2)))
+    return KvCache(*(torch.zeros(n_pages, Hkv, page_size, w, dtype=torch.uint8, device=device)
+                     for w in (D // 2, D // 2, D // 32, D // 32)))
+
+
+def _heads(t: torch.Tensor, name: str, batched: bool, head_dim: int):
+    """rmm_heads_t of a tensor whose last axis is contiguous: head axis
+    `head_dim`, token axis the other of the last three but one, batch axis 0."""
+    if t.dim() != (4 if batched else 3) or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be {'4' if batched else '3'}-D with a contiguous last axis")
+    tok = (3 if batched else 1) - head_dim
+
+    def step(axis):                       # an axis of one entry is never stepped along
+        return t.stride(axis) if t.shape[axis] > 1 else 0
+    return ctypes.byref(_Heads(t.data_ptr(), t.shape[head_dim], step(0) if batched else 0, step(tok),
+                               step(head_dim)))
+
+
+def _vec(t: torch.Tensor | None, n: int, dtype, name: str):
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return _ptr(t)
+
+
+def _given(*ts):
+    return [t for t in ts if t is not None]
+
+
+def _rope_args(rope, positions, T: int):
+    if rope is None:
+        return None, None
+    if positions is None:
+        raise ValueError("a rotation needs positions")
+    return ctypes.byref(rope._c), _vec(positions, T, torch.int32, "positions")
+
+
+def rmm_qk_norm_rope_workspace_size(batch: int, H: int, L: int, D: int) -> int:
+    return int(lib.rmm_qk_norm_rope_workspace_size(int(batch), int(H), int(L), int(D)))
+
+
+def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor | None = None,
+                     rope: Rope | None = None, K: torch.Tensor | None = None, Ko: torch.Tensor | None = None,
+                     gamma_q: torch.Tensor | None = None, gamma_k: torch.Tensor | None = None, eps: float = 1e-6,
+                     energy: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                     stream=None) -> torch.Tensor:
+    """Per-head RMSNorm (with gamma_q, gamma_k [D]) and position rotation of Q
+    [batch, L, H, D] into Qo [batch, H, L, D], and of K [batch, L, Hkv, D] into Ko
+    [batch, Hkv, L, D]; any strides with contiguous heads (slices of a
+    projection's rows, transposed views).  positions: int32 [batch*L].  energy
+    (float64 [batch*H*D]) receives the column energies of each head of Qo.
+    `workspace` (uint8, rmm_qk_norm_rope_workspace_size(...) bytes) is allocated
+    here when energy is wanted and it is not given."""
+    if Q.dim() != 4 or Qo.dim() != 4 or (K is None) != (Ko is None):
+        raise ValueError("Q must be [batch, L, H, D], Qo [batch, H, L, D]; K and Ko come together")
+    batch, L, H, D = Q.shape
+    if tuple(Qo.shape) != (batch, H, L, D):
+        raise ValueError("Qo must be [batch, H, L, D]")
+    if K is not None and (K.dim() != 4 or tuple(K.shape) != (batch, L, K.shape[2], D)
+                          or tuple(Ko.shape) != (batch, K.shape[2], L, D)):
+        raise ValueError("K must be [batch, L, Hkv, D], Ko [batch, Hkv, L, D]")
+    held = _given(Q, Qo, K, Ko, gamma_q, gamma_k)
+    if any(t.dtype != Q.dtype for t in held):
+        raise TypeError("Q, K, their outputs and the norm weights must share one dtype")
+    tables = [] if rope is None else [rope.cos, rope.sin]
+    d = _dev(*held, *_given(positions, energy, workspace), *tables)
+    rp, pp = _rope_args(rope, positions, batch * L)
+    if energy is not None and workspace is None:
+        need = rmm_qk_norm_rope_workspace_size(batch, H, L, D)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=d)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with torch.cuda.device(d):
+        _check("rmm_qk_norm_rope", lib.rmm_qk_norm_rope(
+            _dtype_code(Q), batch, L, D, _heads(Q, "Q", True, 2), _heads(Qo, "Qo", True, 1),
+            None if K is None else _heads(K, "K", True, 2), None if K is None else _heads(Ko, "Ko", True, 1),
+            _vec(gamma_q, D, Q.dtype, "gamma_q"), _vec(gamma_k, D, Q.dtype, "gamma_k"), float(eps), rp, pp,
+            _vec(energy, batch * H * D, torch.float64, "energy"), _ptr(workspace), ws_bytes, _stream(d, stream)))
+    return Qo
+
+
+def rmm_kv_append(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, cache: KvCache,
+                  positions: torch.Tensor | None = None, rope: Rope | None = None,
+                  gamma_k: torch.Tensor | None = None, eps: float = 1e-6, Q: torch.Tensor | None = None,
+                  Qo: torch.Tensor | None = None, gamma_q: torch.Tensor | None = None, stream=None) -> KvCache:
+    """Appends K and V [T, Hkv, D] (bf16) at the slots (int32 [T]: page *
+    page_size + place; outside the cache, e.g. -1: not appended), K normed
+    (gamma_k) and rotated (rope, positions int32 [T]) on the way; with Q and Qo
+    [T, H, D] the tokens' queries are normed (gamma_q) and rotated in the same
+    launch."""
+    if (Q is None) != (Qo is None):
+        raise ValueError("Q and Qo come together")
+    if K.dim() != 3 or tuple(K.shape) != (K.shape[0], cache.Hkv, cache.D) or V.shape != K.shape:
+        raise ValueError("K and V must be [T, Hkv, D] of the cache's Hkv and D")
+    T, D = K.shape[0], cache.D
+    if Q is not None and (Q.dim() != 3 or tuple(Q.shape) != (T, Q.shape[1], D) or Qo.shape != Q.shape):
+        raise ValueError("Q and Qo must be [T, H, D]")
+    held = _given(K, V, Q, Qo, gamma_q, gamma_k)
+    if any(t.dtype != torch.bfloat16 for t in held):
+        raise TypeError("K, V, Q, Qo and the norm weights must be bfloat16")
+    tables = [] if rope is None else [rope.cos, rope.sin]
+    d = _dev(*held, slots, cache.k, *_given(positions), *tables)
+    rp, pp = _rope_args(rope, positions, T)
+    with torch.cuda.device(d):
+        _check("rmm_kv_append", lib.rmm_kv_append(
+            T, _heads(K, "K", False, 1), _heads(V, "V", False, 1), _vec(slots, T, torch.int32, "slots"),
+            ctypes.byref(cache._c), _vec(gamma_k, D, torch.bfloat16, "gamma_k"),
+            None if Q is None else _heads(Q, "Q", False, 1), None if Q is None else _heads(Qo, "Qo", False, 1),
+            _vec(gamma_q, D, torch.bfloat16, "gamma_q"), float(eps), rp, pp, _stream(d, stream)))
+    return cache
+
+
+def rmm_kv_gather(cache: KvCache, slots: torch.Tensor, K: torch.Tensor, V: torch.Tensor, stream=None):
+    """Reads the tokens at the slots (int32 [T]) back into bf16 K and V [T, Hkv,
+    D] (any strides with contiguous heads; zeros for a slot outside the cache)."""
+    T = slots.numel()
+    for t, n in ((K, "K"), (V, "V")):
+        if tuple(t.shape) != (T, cache.Hkv, cache.D):
+            raise ValueError(f"{n} must be [T, Hkv, D]")
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{n} must be bfloat16")
+    d = _dev(K, V, slots, cache.k)
+    with torch.cuda.device(d):
+        _check("rmm_kv_gather", lib.rmm_kv_gather(
+            ctypes.byref(cache._c), _vec(slots, T, torch.int32, "slots"), T, _heads(K, "K", False, 1),
+            _heads(V, "V", False, 1), _stream(d, stream)))
+    return K, V
+
+
+def rmm_paged_attention_workspace_size(T: int, B: int, H: int, Hkv: int, D: int) -> int:
+    return int(lib.rmm_paged_attention_workspace_size(int(T), int(B), int(H), int(Hkv), int(D)))
+
+
+def rmm_paged_attention(Q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, lengths: torch.Tensor,
+                        O: torch.Tensor, q_start: torch.Tensor | None = None, idx: torch.Tensor | None = None,
+                        causal: bool = True, scale: float | None = None, workspace: torch.Tensor | None = None,
+                        stream=None) -> torch.Tensor:
+    """Attention of the new tokens Q [T, H, D] over the cache into O [T, H, D].
+    Sequence b holds lengths[b] keys (int32 [B]) in the pages page_table[b]
+    (int32 [B, max_pages], rows contiguous) and has the new tokens q_start[b] ..
+    q_start[b+1]-1 (int32 [B+1]; None: one each).  Causal: they are its last ones.
+    idx (int32 [T, H, k]): the dims each (token, head) keeps.  `workspace`
+    (uint8, rmm_paged_attention_workspace_size(...) bytes, 256-byte aligned) is
+    allocated here when not given."""
+    if Q.dim() != 3 or O.shape != Q.shape or Q.shape[2] != cache.D:
+        raise ValueError("Q and O must be [T, H, D] of the cache's D")
+    T, H, D = Q.shape
+    if not (Q.dtype == O.dtype == torch.bfloat16):
+        raise TypeError("Q and O must be bfloat16")
+    B = lengths.numel()
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or \
+            page_table.stride(1) != 1:
+        raise ValueError("page_table must be int32 [B, max_pages] with contiguous rows")
+    k = 0
+    if idx is not None:
+        if idx.dtype != torch.int32 or not idx.is_contiguous() or idx.numel() == 0 or idx.numel() % (T * H):
+            raise ValueError("idx must be contiguous int32 [T, H, k]")
+        k = idx.numel() // (T * H)
+    if scale is None:
+        scale = D ** -0.5
+    d = _dev(Q, O, cache.k, page_table, lengths, *_given(q_start, idx, workspace))
+    if workspace is None:
+        workspace = torch.empty(max(rmm_paged_attention_workspace_size(T, B, H, cache.Hkv, D), 1),
+                                dtype=torch.uint8, device=d)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    stride = page_table.stride(0) if B > 1 else page_table.shape[1]
+    with torch.cuda.device(d):
+        _check("rmm_paged_attention", lib.rmm_paged_attention(
+            T, _heads(Q, "Q", False, 1), ctypes.byref(cache._c), page_table.data_ptr(), stride,
+            page_table.shape[1], _vec(lengths, B, torch.int32, "lengths"), B,
+            _vec(q_start, B + 1, torch.int32, "q_start"), _ptr(idx), k, float(scale), 1 if causal else 0,
+            _heads(O, "O", False, 1), workspace.data_ptr(), ws_bytes, _stream(d, stream)))
+    return O

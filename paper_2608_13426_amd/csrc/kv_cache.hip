@@ -1,0 +1,383 @@
+// Per-head norm and position rotation of queries and keys, and the paged
+// key/value cache: appending to it (the keys normed and rotated on the way) and
+// reading tokens back.
+//
+//   y   = x * r * gamma,  r = 1 / sqrt(mean x^2 + eps)                 (optional)
+//   out = pairs (a, b) of y -> (a cos - b sin, b cos + a sin), cos and sin of the
+//         token's position and the pair's index; the dims past `rot` pass through
+//
+// One pass, bound by reading and writing each element once.  A head's D values
+// lie in D / 16 lanes, two 8-element pieces per lane chosen so that a rotation
+// pair never leaves its lane: no exchange but the norm's sum.  A wave takes
+// 1024 / D heads of one token (they share its cos and sin), a workgroup four
+// tokens at a time.
+//
+// Numerics: the mean square and its root in float64 (squares of bf16 are exact
+// there, so the order of the sum does not show), r rounded to fp32; every
+// product and sum of the norm and the rotation rounded separately in fp32 (no
+// fused multiply-add: the result is the same whatever the compiler fuses), one
+// rounding to the stored type.  4-bit codes are made from the fp32 value.
+//
+// Column energies of the rotated queries (the score of the per-head
+// selection): each lane keeps float64 sums of its 16 columns over its tokens,
+// the workgroup's four waves are added in order, a second kernel adds the
+// workgroups' sums in order.
+#include <algorithm>
+
+#include "device_common.h"
+#include "kernels.h"
+#include "kv_cache.h"
+
+namespace rmm {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// ---- 8 elements of a head
+__device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
+    const uint4 q = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+// stores the rounded values and leaves them in x
+__device__ __forceinline__ void store8(uint16_t *p, float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float *p, float (&x)[8]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// ---- 4-bit groups (MXFP4: 32 elements, one power-of-two scale)
+// scale byte of a group with largest magnitude amax: the smallest scale at
+// which amax rounds to at most 6 (magnitudes from 7 on round to 8), kept in
+// 8 .. 252 so that every value is a normal bf16; 255 (NaN) when amax is not finite
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits) {
+    if (amax_bits >= 0x7f800000u) return 255u;
+    const int e = static_cast<int>(amax_bits >> 23) - 2 + ((amax_bits & 0x7fffffu) >= 0x600000u ? 1 : 0);
+    return static_cast<uint32_t>(min(max(e, 8), 252));
+}
+// round to nearest, ties to the even code, magnitudes over 6 to 6
+__device__ __forceinline__ uint32_t mx_codes8(const float (&x)[8], float scale) {
+    uint32_t w = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+#endif
+    return w;
+}
+
+struct Piece {
+    int c1, c2, on;      // the lane's two 8-element pieces; whether they rotate with each other / inside
+};
+// Pieces of lane j of a head (D / 16 lanes).  Halves: pieces c and c + rot/16
+// hold the pairs (i, i + rot/2).  Adjacent pairs lie inside a piece.  The rest
+// is dealt out in order.
+template <int D>
+__device__ __forceinline__ Piece piece_of(int j, int rot, int interleaved) {
+    const int h = interleaved ? D / 16 : rot / 16;
+    if (interleaved || j < h) return {j, j + h, 1};
+    const int n = D / 8 - 2 * h, r = j - h;
+    return {2 * h + r, 2 * h + n / 2 + r, 0};
+}
+
+__device__ __forceinline__ void turn(float &a, float &b, float c, float s) {
+#pragma clang fp contract(off)
+    const float x = a * c - b * s, y = b * c + a * s;
+    a = x;
+    b = y;
+}
+
+}  // namespace
+
+// KV: 0 no cache, 1 bf16 cache, 2 4-bit cache
+template <typename T, int D, int KV, bool NORM, bool ENERGY>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, int64_t blocks) {
+    constexpr int LPH = D / 16, VPW = 64 / LPH;            // lanes per head, heads per wave
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j = lane % LPH, nv = a.q.n + a.k.n + a.v.n;
+    const int vec = static_cast<int>(blockIdx.y) * VPW + lane / LPH;
+    const bool act = vec < nv;
+    // which list the lane's head is in
+    const int kind = !act ? 3 : vec < a.q.n ? 0 : vec < a.q.n + a.k.n ? 1 : 2;
+    const int head = kind == 0 ? vec : kind == 1 ? vec - a.q.n : kind == 2 ? vec - a.q.n - a.k.n : 0;
+    const Piece pc = piece_of<D>(j, a.rot, a.interleaved);
+    // idle lanes read the first head along
+    const bool fq = kind == 0 || (kind == 3 && a.q.n > 0), fv = kind == 2;
+    const int64_t isb = fq ? a.q.sb : fv ? a.v.sb : a.k.sb, ist = fq ? a.q.st : fv ? a.v.st : a.k.st;
+    const T *in = static_cast<const T *>(fq ? a.q.p : fv ? a.v.p : a.k.p) + head * (fq ? a.q.sh : fv ? a.v.sh : a.k.sh);
+    const int64_t osb = kind == 0 ? a.qo.sb : a.ko.sb, ost = kind == 0 ? a.qo.st : a.ko.st;
+    T *out = static_cast<T *>(kind == 0 ? a.qo.p : a.ko.p) + head * (kind == 0 ? a.qo.sh : a.ko.sh);
+    const bool direct = kind == 0 || (kind == 1 && KV == 0);
+
+    float g1[8], g2[8];
+    const void *gam = kind == 0 ? a.gq : kind == 1 ? a.gk : nullptr;
+    if constexpr (NORM) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g1[i] = g2[i] = 1.f;
+        if (gam) {
+            load8(static_cast<const T *>(gam) + 8 * pc.c1, g1);
+            load8(static_cast<const T *>(gam) + 8 * pc.c2, g2);
+        }
+    }
+    double e1[8], e2[8];
+    if constexpr (ENERGY) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e1[i] = e2[i] = 0.0;
+    }
+    __shared__ __attribute__((aligned(16))) uint32_t amax_of[KV == 2 ? kThreads * 2 : 4];
+
+    // tokens of this workgroup: block `blk` of the batch entry (without
+    // energies the whole call is one entry of T tokens)
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) / blocks, blk = static_cast<int64_t>(blockIdx.x) % blocks;
+    const int64_t per = ENERGY ? a.L : a.T;
+    const int64_t t_end = min(per, (blk + 1) * TB);
+    for (int64_t tt = blk * TB + wave; tt < t_end; tt += kWaves) {
+        const int64_t t = unit * per + tt;                 // wave-uniform
+        const int64_t b = ENERGY ? unit : static_cast<int64_t>(static_cast<uint32_t>(t) / static_cast<uint32_t>(a.L));
+        const int64_t l = t - b * a.L;
+        float x1[8], x2[8];
+        load8(in + b * isb + l * ist + 8 * pc.c1, x1);
+        load8(in + b * isb + l * ist + 8 * pc.c2, x2);
+        if constexpr (NORM) {
+#pragma clang fp contract(off)
+            double ss = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double u = x1[i], v = x2[i];
+                ss = ss + u * u;
+                ss = ss + v * v;
+            }
+            ss += dpp_f64<0xB1>(ss);
+            ss += dpp_f64<0x4E>(ss);
+            if constexpr (LPH == 8) ss += dpp_f64<0x141>(ss);
+            const float r = static_cast<float>(1.0 / sqrt(ss / D + static_cast<double>(a.eps)));
+            if (gam) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x1[i] = x1[i] * r * g1[i];
+                    x2[i] = x2[i] * r * g2[i];
+                }
+            }
+        }
+        if (a.rot) {
+            // a position outside the tables gives NaN
+            const int p = a.pos[t];
+            const bool ok = p >= 0 && p < a.n_pos;
+            const int64_t row = static_cast<int64_t>(ok ? p : 0) * (a.rot / 2);
+            const float *cs = a.cs + row, *sn = a.sn + row;
+            const float bad = ok ? 1.f : __builtin_nanf("");
+            if (kind < 2) {
+                if (a.interleaved) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float(&x)[8] = h ? x2 : x1;
+                        const int c = h ? pc.c2 : pc.c1;
+                        if (8 * c < a.rot) {
+                            const float4 cc = *reinterpret_cast<const float4 *>(cs + 4 * c);
+                            const float4 ss = *reinterpret_cast<const float4 *>(sn + 4 * c);
+                            turn(x[0], x[1], cc.x * bad, ss.x * bad);
+                            turn(x[2], x[3], cc.y * bad, ss.y * bad);
+                            turn(x[4], x[5], cc.z * bad, ss.z * bad);
+                            turn(x[6], x[7], cc.w * bad, ss.w * bad);
+                        }
+                    }
+                } else if (pc.on) {
+                    float cc[8], ss[8];
+                    load8(cs + 8 * pc.c1, cc);
+                    load8(sn + 8 * pc.c1, ss);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) turn(x1[i], x2[i], cc[i] * bad, ss[i] * bad);
+                }
+            }
+        }
+        if (act && direct) {
+            T *o = out + b * osb + l * ost;
+            store8(o + 8 * pc.c1, x1);
+            store8(o + 8 * pc.c2, x2);
+            if constexpr (ENERGY) {
+                if (kind == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const double u = x1[i], v = x2[i];
+                        e1[i] += u * u;
+                        e2[i] += v * v;
+                    }
+                }
+            }
+        }
+        if constexpr (KV != 0) {
+            const int slot = a.slots[t];
+            const int page = slot >> a.kv.lg_page, off = slot & ((1 << a.kv.lg_page) - 1);
+            const bool held = slot >= 0 && page < a.kv.n_pages && (kind == 1 || kind == 2);
+            const int64_t row = (static_cast<int64_t>(head) << a.kv.lg_page) + off;
+            if constexpr (KV == 1) {
+                if (held) {
+                    uint8_t *pg = kind == 1 ? a.kv.k + page * a.kv.k_page : a.kv.v + page * a.kv.v_page;
+                    uint16_t *o = reinterpret_cast<uint16_t *>(pg) + row * D;
+                    store8(o + 8 * pc.c1, x1);
+                    store8(o + 8 * pc.c2, x2);
+                }
+            } else {
+                // magnitudes as bit patterns: they order as numbers, NaN above infinity
+                uint32_t m1 = 0, m2 = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    m1 = max(m1, __float_as_uint(x1[i]) & 0x7fffffffu);
+                    m2 = max(m2, __float_as_uint(x2[i]) & 0x7fffffffu);
+                }
+                // the pieces' maxima meet in the wave's own corner of LDS: a
+                // group's four pieces can lie in any of the head's lanes
+                uint32_t *mine = amax_of + (threadIdx.x / LPH) * (2 * LPH);
+                __builtin_amdgcn_wave_barrier();
+                mine[pc.c1] = m1;
+                mine[pc.c2] = m2;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                const uint4 q1 = *reinterpret_cast<const uint4 *>(mine + (pc.c1 & ~3));
+                const uint4 q2 = *reinterpret_cast<const uint4 *>(mine + (pc.c2 & ~3));
+                const uint32_t s1 = mx_scale_byte(max(max(q1.x, q1.y), max(q1.z, q1.w)));
+                const uint32_t s2 = mx_scale_byte(max(max(q2.x, q2.y), max(q2.z, q2.w)));
+                const uint32_t w1 = s1 == 255u ? 0u : mx_codes8(x1, __uint_as_float(s1 << 23));
+                const uint32_t w2 = s2 == 255u ? 0u : mx_codes8(x2, __uint_as_float(s2 << 23));
+                if (held) {
+                    uint8_t *pg = kind == 1 ? a.kv.k + page * a.kv.k_page : a.kv.v + page * a.kv.v_page;
+                    uint8_t *sg = kind == 1 ? a.kv.ks + page * a.kv.ks_page : a.kv.vs + page * a.kv.vs_page;
+                    uint32_t *o = reinterpret_cast<uint32_t *>(pg + row * (D / 2));
+                    o[pc.c1] = w1;
+                    o[pc.c2] = w2;
+                    uint8_t *so = sg + row * (D / 32);
+                    if ((pc.c1 & 3) == 0) so[pc.c1 >> 2] = static_cast<uint8_t>(s1);
+                    if ((pc.c2 & 3) == 0) so[pc.c2 >> 2] = static_cast<uint8_t>(s2);
+                }
+            }
+        }
+    }
+
+    if constexpr (ENERGY) {
+        __shared__ double part[kWaves][64 * 16];
+        double *mine = part[wave] + (lane / LPH) * D;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            mine[8 * pc.c1 + i] = e1[i];
+            mine[8 * pc.c2 + i] = e2[i];
+        }
+        __syncthreads();
+        const int HD = a.q.n * D, c0 = static_cast<int>(blockIdx.y) * VPW * D;
+        double *o = a.partials + (unit * blocks + blk) * HD;
+        for (int i = threadIdx.x; i < VPW * D && c0 + i < HD; i += kThreads)
+            o[c0 + i] = ((part[0][i] + part[1][i]) + part[2][i]) + part[3][i];
+    }
+}
+
+// Cached tokens as bf16 rows: one thread per 8 elements
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const int32_t *__restrict__ slots, int64_t n8,
+                                                             Heads k, Heads v) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= n8) return;
+    const int c = static_cast<int>(i % (D / 8)), hv = static_cast<int>(i / (D / 8) % (2 * kv.Hkv));
+    const int64_t t = i / (D / 8) / (2 * kv.Hkv);
+    const bool key = hv < kv.Hkv;
+    const int head = key ? hv : hv - kv.Hkv, slot = slots[t];
+    const int page = slot >> kv.lg_page, off = slot & ((1 << kv.lg_page) - 1);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (slot >= 0 && page < kv.n_pages) {
+        const uint8_t *pg = key ? kv.k + page * kv.k_page : kv.v + page * kv.v_page;
+        const int64_t row = (static_cast<int64_t>(head) << kv.lg_page) + off;
+        if (!kv.mx) {
+            w = reinterpret_cast<const uint4 *>(pg + row * (2 * D))[c];
+        } else {
+            const uint8_t *sg = key ? kv.ks + page * kv.ks_page : kv.vs + page * kv.vs_page;
+            const uint32_t q = reinterpret_cast<const uint32_t *>(pg + row * (D / 2))[c];
+            const float s = __uint_as_float(static_cast<uint32_t>(sg[row * (D / 32) + (c >> 2)]) << 23);
+#if defined(__HIP_DEVICE_COMPILE__)
+            w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 0));
+            w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 1));
+            w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 2));
+            w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 3));
+#else
+            (void)q; (void)s;
+#endif
+        }
+    }
+    const Heads &d = key ? k : v;
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(d.p) + t * d.st + head * d.sh + 8 * c) = w;
+}
+
+namespace {
+
+// Tokens per workgroup: few while there are too few workgroups to fill the
+// CUs, more where the sums of squares (one float64 row of columns per
+// workgroup) would be traffic of their own
+int rotate_tokens(int64_t T, int64_t heads, int D) {
+    const int64_t groups = (heads + 1024 / D - 1) / (1024 / D);
+    int tb = kWaves;
+    while (tb < 64 && T / (2 * tb) * groups >= 1024) tb *= 2;
+    return tb;
+}
+
+template <typename T, int D, int KV, bool ENERGY>
+hipError_t launch(const RotateArgs &a, hipStream_t stream) {
+    const int nv = a.q.n + a.k.n + a.v.n, groups = (nv + 1024 / D - 1) / (1024 / D);
+    const int TB = rotate_tokens(a.T, ENERGY ? a.q.n : nv, D);
+    const int64_t per = ENERGY ? a.L : a.T, blocks = (per + TB - 1) / TB, units = ENERGY ? a.T / a.L : 1;
+    const dim3 grid(static_cast<uint32_t>(units * blocks), static_cast<uint32_t>(groups));
+    if (a.gq || a.gk) rotate_kernel<T, D, KV, true, ENERGY><<<grid, kThreads, 0, stream>>>(a, TB, blocks);
+    else rotate_kernel<T, D, KV, false, ENERGY><<<grid, kThreads, 0, stream>>>(a, TB, blocks);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t rotate_blocks(int64_t batch, int64_t L, int64_t heads, int D) {
+    const int TB = rotate_tokens(batch * L, heads, D);
+    return (L + TB - 1) / TB;
+}
+
+hipError_t launch_rotate(const RotateArgs &a, bool bf16, int D, hipStream_t stream) {
+    const bool e = a.partials != nullptr;
+    if (bf16) {
+        if (D == 128) return e ? launch<uint16_t, 128, 0, true>(a, stream) : launch<uint16_t, 128, 0, false>(a, stream);
+        return e ? launch<uint16_t, 64, 0, true>(a, stream) : launch<uint16_t, 64, 0, false>(a, stream);
+    }
+    if (D == 128) return e ? launch<float, 128, 0, true>(a, stream) : launch<float, 128, 0, false>(a, stream);
+    return e ? launch<float, 64, 0, true>(a, stream) : launch<float, 64, 0, false>(a, stream);
+}
+
+hipError_t launch_kv_append(const RotateArgs &a, int D, hipStream_t stream) {
+    if (a.kv.mx)
+        return D == 128 ? launch<uint16_t, 128, 2, false>(a, stream) : launch<uint16_t, 64, 2, false>(a, stream);
+    return D == 128 ? launch<uint16_t, 128, 1, false>(a, stream) : launch<uint16_t, 64, 1, false>(a, stream);
+}
+
+hipError_t launch_kv_gather(const KvPages &kv, const int32_t *slots, int64_t T, const Heads &k, const Heads &v, int D,
+                            hipStream_t stream) {
+    const int64_t n8 = T * 2 * kv.Hkv * (D / 8);
+    const dim3 grid(static_cast<uint32_t>((n8 + kThreads - 1) / kThreads));
+    if (D == 128) kv_gather_kernel<128><<<grid, kThreads, 0, stream>>>(kv, slots, n8, k, v);
+    else kv_gather_kernel<64><<<grid, kThreads, 0, stream>>>(kv, slots, n8, k, v);
+    return hipGetLastError();
+}
+
+}  // namespace rmm
