@@ -842,8 +842,9 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * It sees s <= lengths[b] - n + j when causal (the new tokens are the cache's
  * last n), else s < lengths[b] (e.g. an encoder's states).  A token that sees
  * no key gets 0.  I = idx[(t*H + h)*k ..) for token t (rmm_select_tokens on the rows of
- * q), or all dims when idx is NULL (k ignored).  A key value that is infinite
- * or NaN in a dim outside I, or past what a token sees, has no effect on it.
+ * q), or all dims when idx is NULL (k ignored).  A key or value that is
+ * infinite or NaN in a dim outside I, or past what a token sees, does not reach
+ * it (only the order of its sums may change).
  * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
  * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.
  *
@@ -861,8 +862,10 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  *             table_stride < max_pages, q_start NULL with T != B, H not a
  *             multiple of the cache's Hkv, o's head count not H, k outside
  *             [1, D], a misaligned workspace; UNSUPPORTED for a cache or
- *             strides that break the rules above, max_pages * page_size > 2^30 or
- *             T*H >= 2^31; WORKSPACE_TOO_SMALL.
+ *             strides that break the rules above, max_pages * page_size > 2^30,
+ *             T*H >= 2^31, or so many tokens against so long a table that
+ *             their key blocks number 2^31 (T*H * max_pages*page_size below 2^39 is always
+ *             taken); WORKSPACE_TOO_SMALL.
  */
 size_t rmm_paged_attention_workspace_size(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D);
 rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_cache_t *cache,

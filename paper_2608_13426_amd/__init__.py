@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -66,7 +67,9 @@ class _KvCacheC(ctypes.Structure):
                 ("v_stride", _i64), ("k_scale_stride", _i64), ("v_scale_stride", _i64)]
 
 
-_ph, _pr, _pc = ctypes.POINTER(_Heads), ctypes.POINTER(_RopeTables), ctypes.POINTER(_KvCacheC)
+# these structs are only read by the library: the binding passes each packed into bytes
+_HEADS_BYTES, _ROPE_BYTES = struct.Struct("@Pqqqq"), struct.Struct("@PPqqi4x")
+assert _HEADS_BYTES.size == ctypes.sizeof(_Heads) and _ROPE_BYTES.size == ctypes.sizeof(_RopeTables)
 
 _SIGS = {
     "rmm_retained_count": (_i64, [ctypes.c_double, _i64]),
@@ -133,14 +136,14 @@ _SIGS = {
                                                     ctypes.c_int, _p, _i64, _p, _p, ctypes.c_size_t,
                                                     _p]),
     "rmm_qk_norm_rope_workspace_size": (ctypes.c_size_t, [_i64, _i64, _i64, _i64]),
-    "rmm_qk_norm_rope": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _i64, _ph, _ph, _ph, _ph, _p, _p,
-                                        ctypes.c_float, _pr, _p, _p, _p, ctypes.c_size_t, _p]),
-    "rmm_kv_append": (ctypes.c_int, [_i64, _ph, _ph, _p, _pc, _p, _ph, _ph, _p, ctypes.c_float, _pr, _p,
+    "rmm_qk_norm_rope": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _i64, _p, _p, _p, _p, _p, _p,
+                                        ctypes.c_float, _p, _p, _p, _p, ctypes.c_size_t, _p]),
+    "rmm_kv_append": (ctypes.c_int, [_i64, _p, _p, _p, _p, _p, _p, _p, _p, ctypes.c_float, _p, _p,
                                      _p]),
-    "rmm_kv_gather": (ctypes.c_int, [_pc, _p, _i64, _ph, _ph, _p]),
+    "rmm_kv_gather": (ctypes.c_int, [_p, _p, _i64, _p, _p, _p]),
     "rmm_paged_attention_workspace_size": (ctypes.c_size_t, [_i64, _i64, _i64, _i64, _i64]),
-    "rmm_paged_attention": (ctypes.c_int, [_i64, _ph, _pc, _p, _i64, _i64, _p, _i64, _p, _p, _i64,
-                                           ctypes.c_float, ctypes.c_int, _ph, _p, ctypes.c_size_t, _p]),
+    "rmm_paged_attention": (ctypes.c_int, [_i64, _p, _p, _p, _i64, _i64, _p, _i64, _p, _p, _i64,
+                                           ctypes.c_float, ctypes.c_int, _p, _p, ctypes.c_size_t, _p]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -894,6 +897,10 @@ def rmm_decode_step(groups, workspace: torch.Tensor | None = None, stream=None):
 
 
 # ------------------------------------------- rotation and the paged cache
+#
+# A decode step makes these calls once per layer on small tensors, so the
+# binding reads each tensor's sizes and strides once and builds no objects
+# that it does not pass on.
 
 def rope_tables(n_pos: int, rot: int, theta: float = 10000.0, device="cuda"):
     """(cos, sin) float32 [n_pos, rot/2] of the angles pos * theta^(-2i/rot),
@@ -918,7 +925,8 @@ class Rope:
             raise ValueError("cos and sin must be contiguous")
         _dev(cos, sin)
         self.cos, self.sin, self.interleaved = cos, sin, bool(interleaved)
-        self._c = _RopeTables(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(self.interleaved))
+        self._c = _ROPE_BYTES.pack(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1],
+                                   int(self.interleaved))
 
 
 class KvCache:
@@ -939,10 +947,9 @@ class KvCache:
         n_pages, Hkv, page_size, row = k.shape
         D = 2 * row if mx else row
         held = (k, v, k_scale, v_scale) if mx else (k, v)
-        if mx:
-            for t in held[2:]:
-                if t.dtype != torch.uint8 or tuple(t.shape) != (n_pages, Hkv, page_size, D // 32):
-                    raise ValueError("scales must be uint8 [n_pages, Hkv, page_size, D/32]")
+        for t in held[2:]:
+            if t.dtype != torch.uint8 or tuple(t.shape) != (n_pages, Hkv, page_size, D // 32):
+                raise ValueError("scales must be uint8 [n_pages, Hkv, page_size, D/32]")
         for t in held:
             if t.stride(3) != 1 or t.stride(2) != t.shape[3] or \
                     (Hkv > 1 and t.stride(1) != page_size * t.shape[3]):
@@ -951,8 +958,8 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.Hkv, self.page_size, self.D, self.mx = n_pages, Hkv, page_size, D, mx
         strides = [t.stride(0) * t.element_size() for t in held] + [0, 0]
-        self._c = _KvCacheC(RMM_CACHE_MX if mx else RMM_CACHE_BF, k.data_ptr(), v.data_ptr(), _ptr(k_scale),
-                            _ptr(v_scale), n_pages, page_size, Hkv, D, *strides[:4])
+        self._c = bytes(_KvCacheC(RMM_CACHE_MX if mx else RMM_CACHE_BF, k.data_ptr(), v.data_ptr(), _ptr(k_scale),
+                                  _ptr(v_scale), n_pages, page_size, Hkv, D, *strides[:4]))
 
 
 def kv_cache(n_pages: int, Hkv: int, page_size: int, D: int, mx: bool = False, device="cuda") -> KvCache:
@@ -964,35 +971,77 @@ def kv_cache(n_pages: int, Hkv: int, page_size: int, D: int, mx: bool = False, d
                      for w in (D // 2, D // 2, D // 32, D // 32)))
 
 
-def _heads(t: torch.Tensor, name: str, batched: bool, head_dim: int):
-    """rmm_heads_t of a tensor whose last axis is contiguous: head axis
-    `head_dim`, token axis the other of the last three but one, batch axis 0."""
-    if t.dim() != (4 if batched else 3) or t.stride(-1) != 1:
-        raise ValueError(f"{name} must be {'4' if batched else '3'}-D with a contiguous last axis")
-    tok = (3 if batched else 1) - head_dim
+def _device_index(*ts) -> int:
+    """The one GPU that the given tensors (None: not given) live on."""
+    d = -1
+    for t in ts:
+        if t is not None:
+            i = t.get_device()
+            if i < 0:
+                raise ValueError("librmm tensors must live on the GPU")
+            if d < 0:
+                d = i
+            elif i != d:
+                raise ValueError("all tensors must be on one device")
+    return d
 
-    def step(axis):                       # an axis of one entry is never stepped along
-        return t.stride(axis) if t.shape[axis] > 1 else 0
-    return ctypes.byref(_Heads(t.data_ptr(), t.shape[head_dim], step(0) if batched else 0, step(tok),
-                               step(head_dim)))
+
+def _heads(t: torch.Tensor, shape, dtype, name: str, what: str, batched: bool = False, head_first: bool = False):
+    """rmm_heads_t of [T, heads, D] (batched: [batch, L, heads, D], or with
+    head_first [batch, heads, L, D]), checked; strides of axes of one entry are
+    never used."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {what}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    if not batched:
+        return _HEADS_BYTES.pack(t.data_ptr(), shape[1], 0, st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0)
+    tok, head = (2, 1) if head_first else (1, 2)
+    return _HEADS_BYTES.pack(t.data_ptr(), shape[head], st[0] if shape[0] > 1 else 0, st[tok] if shape[tok] > 1 else 0,
+                             st[head] if shape[head] > 1 else 0)
 
 
 def _vec(t: torch.Tensor | None, n: int, dtype, name: str):
-    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _given(*ts):
-    return [t for t in ts if t is not None]
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _rope_args(rope, positions, T: int):
+def _run(fn: str, device: int, stream, *args):
+    """The call on `device`, on its current stream unless one is given."""
+    s = _raw_stream(device) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == device:
+        status = getattr(lib, fn)(*args, s)
+    else:
+        with torch.cuda.device(device):
+            status = getattr(lib, fn)(*args, s)
+    if status != 0:
+        raise RmmError(fn, status)
+
+
+def _workspace(n: int, like: torch.Tensor, stream) -> torch.Tensor:
+    """A workspace of this call, not reused before the call's stream is done with it."""
+    ws = torch.empty(max(n, 1), dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
+def _positions(rope, positions, T: int):
     if rope is None:
-        return None, None
+        return None
     if positions is None:
         raise ValueError("a rotation needs positions")
-    return ctypes.byref(rope._c), _vec(positions, T, torch.int32, "positions")
+    return _vec(positions, T, torch.int32, "positions")
 
 
 def rmm_qk_norm_rope_workspace_size(batch: int, H: int, L: int, D: int) -> int:
@@ -1011,30 +1060,28 @@ def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor 
     (float64 [batch*H*D]) receives the column energies of each head of Qo.
     `workspace` (uint8, rmm_qk_norm_rope_workspace_size(...) bytes) is allocated
     here when energy is wanted and it is not given."""
-    if Q.dim() != 4 or Qo.dim() != 4 or (K is None) != (Ko is None):
-        raise ValueError("Q must be [batch, L, H, D], Qo [batch, H, L, D]; K and Ko come together")
+    if Q.dim() != 4 or (K is None) != (Ko is None) or (K is not None and K.dim() != 4):
+        raise ValueError("Q must be [batch, L, H, D] and K [batch, L, Hkv, D]; K and Ko come together")
     batch, L, H, D = Q.shape
-    if tuple(Qo.shape) != (batch, H, L, D):
-        raise ValueError("Qo must be [batch, H, L, D]")
-    if K is not None and (K.dim() != 4 or tuple(K.shape) != (batch, L, K.shape[2], D)
-                          or tuple(Ko.shape) != (batch, K.shape[2], L, D)):
-        raise ValueError("K must be [batch, L, Hkv, D], Ko [batch, Hkv, L, D]")
-    held = _given(Q, Qo, K, Ko, gamma_q, gamma_k)
-    if any(t.dtype != Q.dtype for t in held):
-        raise TypeError("Q, K, their outputs and the norm weights must share one dtype")
-    tables = [] if rope is None else [rope.cos, rope.sin]
-    d = _dev(*held, *_given(positions, energy, workspace), *tables)
-    rp, pp = _rope_args(rope, positions, batch * L)
-    if energy is not None and workspace is None:
-        need = rmm_qk_norm_rope_workspace_size(batch, H, L, D)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=d)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with torch.cuda.device(d):
-        _check("rmm_qk_norm_rope", lib.rmm_qk_norm_rope(
-            _dtype_code(Q), batch, L, D, _heads(Q, "Q", True, 2), _heads(Qo, "Qo", True, 1),
-            None if K is None else _heads(K, "K", True, 2), None if K is None else _heads(Ko, "Ko", True, 1),
-            _vec(gamma_q, D, Q.dtype, "gamma_q"), _vec(gamma_k, D, Q.dtype, "gamma_k"), float(eps), rp, pp,
-            _vec(energy, batch * H * D, torch.float64, "energy"), _ptr(workspace), ws_bytes, _stream(d, stream)))
+    dt = Q.dtype
+    code = _dtype_code(Q)
+    q = _heads(Q, (batch, L, H, D), dt, "Q", "[batch, L, H, D]", True)
+    qo = _heads(Qo, (batch, H, L, D), dt, "Qo", "[batch, H, L, D]", True, True)
+    k = ko = None
+    if K is not None:
+        Hkv = K.shape[2]
+        k = _heads(K, (batch, L, Hkv, D), dt, "K", "[batch, L, Hkv, D]", True)
+        ko = _heads(Ko, (batch, Hkv, L, D), dt, "Ko", "[batch, Hkv, L, D]", True, True)
+    d = _device_index(Q, Qo, K, Ko, gamma_q, gamma_k, None if rope is None else rope.cos, positions, energy, workspace)
+    ws_bytes = 0
+    if energy is not None:
+        if workspace is None:
+            workspace = _workspace(rmm_qk_norm_rope_workspace_size(batch, H, L, D), Q, stream)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _run("rmm_qk_norm_rope", d, stream, code, batch, L, D, q, qo, k, ko, _vec(gamma_q, D, dt, "gamma_q"),
+         _vec(gamma_k, D, dt, "gamma_k"), eps, None if rope is None else rope._c,
+         _positions(rope, positions, batch * L), _vec(energy, batch * H * D, torch.float64, "energy"),
+         _ptr(workspace), ws_bytes)
     return Qo
 
 
@@ -1047,25 +1094,19 @@ def rmm_kv_append(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, cache: 
     (gamma_k) and rotated (rope, positions int32 [T]) on the way; with Q and Qo
     [T, H, D] the tokens' queries are normed (gamma_q) and rotated in the same
     launch."""
-    if (Q is None) != (Qo is None):
-        raise ValueError("Q and Qo come together")
-    if K.dim() != 3 or tuple(K.shape) != (K.shape[0], cache.Hkv, cache.D) or V.shape != K.shape:
-        raise ValueError("K and V must be [T, Hkv, D] of the cache's Hkv and D")
-    T, D = K.shape[0], cache.D
-    if Q is not None and (Q.dim() != 3 or tuple(Q.shape) != (T, Q.shape[1], D) or Qo.shape != Q.shape):
-        raise ValueError("Q and Qo must be [T, H, D]")
-    held = _given(K, V, Q, Qo, gamma_q, gamma_k)
-    if any(t.dtype != torch.bfloat16 for t in held):
-        raise TypeError("K, V, Q, Qo and the norm weights must be bfloat16")
-    tables = [] if rope is None else [rope.cos, rope.sin]
-    d = _dev(*held, slots, cache.k, *_given(positions), *tables)
-    rp, pp = _rope_args(rope, positions, T)
-    with torch.cuda.device(d):
-        _check("rmm_kv_append", lib.rmm_kv_append(
-            T, _heads(K, "K", False, 1), _heads(V, "V", False, 1), _vec(slots, T, torch.int32, "slots"),
-            ctypes.byref(cache._c), _vec(gamma_k, D, torch.bfloat16, "gamma_k"),
-            None if Q is None else _heads(Q, "Q", False, 1), None if Q is None else _heads(Qo, "Qo", False, 1),
-            _vec(gamma_q, D, torch.bfloat16, "gamma_q"), float(eps), rp, pp, _stream(d, stream)))
+    if (Q is None) != (Qo is None) or K.dim() != 3 or (Q is not None and Q.dim() != 3):
+        raise ValueError("K and V must be [T, Hkv, D], Q and Qo (together) [T, H, D]")
+    T, D, bf = K.shape[0], cache.D, torch.bfloat16
+    q = qo = None
+    if Q is not None:
+        shape = (T, Q.shape[1], D)
+        q, qo = _heads(Q, shape, bf, "Q", "[T, H, D]"), _heads(Qo, shape, bf, "Qo", "[T, H, D]")
+    shape = (T, cache.Hkv, D)
+    d = _device_index(K, V, slots, cache.k, Q, Qo, gamma_q, gamma_k, None if rope is None else rope.cos, positions)
+    _run("rmm_kv_append", d, stream, T, _heads(K, shape, bf, "K", "[T, Hkv, D] of the cache's Hkv and D"),
+         _heads(V, shape, bf, "V", "[T, Hkv, D] of the cache's Hkv and D"), _vec(slots, T, torch.int32, "slots"),
+         cache._c, _vec(gamma_k, D, bf, "gamma_k"), q, qo, _vec(gamma_q, D, bf, "gamma_q"), eps,
+         None if rope is None else rope._c, _positions(rope, positions, T))
     return cache
 
 
@@ -1073,16 +1114,10 @@ def rmm_kv_gather(cache: KvCache, slots: torch.Tensor, K: torch.Tensor, V: torch
     """Reads the tokens at the slots (int32 [T]) back into bf16 K and V [T, Hkv,
     D] (any strides with contiguous heads; zeros for a slot outside the cache)."""
     T = slots.numel()
-    for t, n in ((K, "K"), (V, "V")):
-        if tuple(t.shape) != (T, cache.Hkv, cache.D):
-            raise ValueError(f"{n} must be [T, Hkv, D]")
-        if t.dtype != torch.bfloat16:
-            raise TypeError(f"{n} must be bfloat16")
-    d = _dev(K, V, slots, cache.k)
-    with torch.cuda.device(d):
-        _check("rmm_kv_gather", lib.rmm_kv_gather(
-            ctypes.byref(cache._c), _vec(slots, T, torch.int32, "slots"), T, _heads(K, "K", False, 1),
-            _heads(V, "V", False, 1), _stream(d, stream)))
+    shape = (T, cache.Hkv, cache.D)
+    _run("rmm_kv_gather", _device_index(K, V, slots, cache.k), stream, cache._c,
+         _vec(slots, T, torch.int32, "slots"), T, _heads(K, shape, torch.bfloat16, "K", "[T, Hkv, D]"),
+         _heads(V, shape, torch.bfloat16, "V", "[T, Hkv, D]"))
     return K, V
 
 
@@ -1101,32 +1136,28 @@ def rmm_paged_attention(Q: torch.Tensor, cache: KvCache, page_table: torch.Tenso
     idx (int32 [T, H, k]): the dims each (token, head) keeps.  `workspace`
     (uint8, rmm_paged_attention_workspace_size(...) bytes, 256-byte aligned) is
     allocated here when not given."""
-    if Q.dim() != 3 or O.shape != Q.shape or Q.shape[2] != cache.D:
-        raise ValueError("Q and O must be [T, H, D] of the cache's D")
-    T, H, D = Q.shape
-    if not (Q.dtype == O.dtype == torch.bfloat16):
-        raise TypeError("Q and O must be bfloat16")
+    if Q.dim() != 3:
+        raise ValueError("Q must be [T, H, D]")
+    T, H, _ = Q.shape
+    D, bf = cache.D, torch.bfloat16
     B = lengths.numel()
-    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or \
-            page_table.stride(1) != 1:
+    width = page_table.shape[-1]
+    if page_table.dtype != torch.int32 or tuple(page_table.shape) != (B, width) or page_table.stride(1) != 1:
         raise ValueError("page_table must be int32 [B, max_pages] with contiguous rows")
     k = 0
     if idx is not None:
-        if idx.dtype != torch.int32 or not idx.is_contiguous() or idx.numel() == 0 or idx.numel() % (T * H):
+        n = idx.numel()
+        if idx.dtype != torch.int32 or not idx.is_contiguous() or n == 0 or n % (T * H):
             raise ValueError("idx must be contiguous int32 [T, H, k]")
-        k = idx.numel() // (T * H)
+        k = n // (T * H)
     if scale is None:
         scale = D ** -0.5
-    d = _dev(Q, O, cache.k, page_table, lengths, *_given(q_start, idx, workspace))
+    d = _device_index(Q, O, cache.k, page_table, lengths, q_start, idx, workspace)
     if workspace is None:
-        workspace = torch.empty(max(rmm_paged_attention_workspace_size(T, B, H, cache.Hkv, D), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _workspace(rmm_paged_attention_workspace_size(T, B, H, cache.Hkv, D), Q, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
-    stride = page_table.stride(0) if B > 1 else page_table.shape[1]
-    with torch.cuda.device(d):
-        _check("rmm_paged_attention", lib.rmm_paged_attention(
-            T, _heads(Q, "Q", False, 1), ctypes.byref(cache._c), page_table.data_ptr(), stride,
-            page_table.shape[1], _vec(lengths, B, torch.int32, "lengths"), B,
-            _vec(q_start, B + 1, torch.int32, "q_start"), _ptr(idx), k, float(scale), 1 if causal else 0,
-            _heads(O, "O", False, 1), workspace.data_ptr(), ws_bytes, _stream(d, stream)))
+    _run("rmm_paged_attention", d, stream, T, _heads(Q, (T, H, D), bf, "Q", "[T, H, D] of the cache's D"), cache._c,
+         page_table.data_ptr(), page_table.stride(0) if B > 1 else width, width,
+         _vec(lengths, B, torch.int32, "lengths"), B, _vec(q_start, B + 1, torch.int32, "q_start"), _ptr(idx), k,
+         float(scale), 1 if causal else 0, _heads(O, (T, H, D), bf, "O", "[T, H, D]"), workspace.data_ptr(), ws_bytes)
     return O

@@ -187,7 +187,7 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
     if (a.q.n % a.kv.Hkv || a.o.n != a.q.n) return RMM_ERR_INVALID_ARGUMENT;
     if (idx && (k < 1 || k > cache->D)) return RMM_ERR_INVALID_ARGUMENT;
     if (T > kInt32Max / a.q.n || B > kInt32Max - 64 || max_pages > (int64_t(1) << 30) / cache->page_size ||
-        !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(q_start, 4) || !aligned(idx, 4))
+        !rmm::paged_line_fits(T, B, a.q.n, a.kv.Hkv, max_pages * cache->page_size) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(q_start, 4) || !aligned(idx, 4))
         return RMM_ERR_UNSUPPORTED;
     const size_t need = rmm_paged_attention_workspace_size(T, B, a.q.n, a.kv.Hkv, cache->D);
     if (!workspace || workspace_bytes < need) return RMM_ERR_WORKSPACE_TOO_SMALL;

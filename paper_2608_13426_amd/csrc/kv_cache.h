@@ -52,9 +52,11 @@ struct PagedArgs {
     int64_t T;
     float c;                               // scale * log2(e)
     int causal;
-    float *part_o, *part_ml;               // partial outputs and (max, sum) of split units
+    void *pieces;                          // what joins the pieces of cut units
+    float *part_o, *part_ml;               // their outputs, their (max, sum)
     int nw;                                // workgroups
 };
+bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys);
 size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D);
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream);
 

@@ -3,23 +3,27 @@
 //   O[t][h] = softmax(scale * Q[t][h][I] . K[s][g][I]) V[s][g],  s the positions the
 //   token sees, I all dims or the (token, head)'s retained ones
 //
-// A unit is one (sequence, kv head, tile of 16 * R query rows); a query row is
-// one (new token, query head of the kv head), so the heads of a group share
-// every key read.  The 32-key chunks of all units lie on one line that is cut
-// into equal runs, one per workgroup: lengths are only known on the device, and
-// a batch with one long sequence still loads from every CU.  A unit inside one
-// workgroup is written at once; the pieces of a cut one go to the workspace as
-// (maximum, sum, unnormalised output) and a second launch joins them in order.
+// A query row is one (new token, query head of a kv head): the heads of a group
+// share every key read.  A unit is one (sequence, kv head, tile of query rows).
 //
-// Inside a workgroup the four waves take chunks in turn and meet only at the
-// end of a unit.  Keys and values go from memory to registers to the matrix
-// cores without LDS: S^T = K Q^T takes 16 key rows as loaded (v_mfma_f32_16x16x32,
-// a lane holds 8 dims of one key), its result has a query row per lane and,
-// with key 8 g + 4 tb + i at row 4 g + i of tile tb, exactly the eight keys per lane group
-// that O^T = V^T P^T takes as its contraction, so the weights stay in place; the value rows are
-// turned 8 x 8 in registers (v_perm).  4-bit codes become bf16 with
-// v_cvt_scalef32_pk_bf16_fp4 (exact, the scale included).
+//   up to 16 rows (a decode step): paged_few_kernel, 16-row tiles.  The four waves
+//   of a workgroup take 32-key chunks in turn; keys and values go from memory to
+//   registers to the matrix cores without LDS.  Bound by reading the cache.
+//   more rows (drafted tokens, prompt chunks): paged_rows_kernel, 32 rows per wave,
+//   64-key tiles staged once per workgroup in an LDS ring.
+//
+// Lengths are known on the device only, and a batch may hold one long sequence
+// among short ones, so the work is cut there: the key blocks of all units lie on
+// one line, which is cut into equal runs, one per workgroup.  A unit inside one
+// run is written at once; the pieces of a cut one go to the workspace as (maximum,
+// sum, unnormalised output) and a second launch joins them in order.  Where every
+// unit is short (kShort blocks) the line is cut between units instead.
+//
+// With the causal mask a unit ends at the last key that any of its rows sees.
+// Row tiles are laid on the line in pairs of one early and one late tile, which
+// have the same number of blocks (to within the two that the pair's length allows).
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kernels.h"
@@ -30,10 +34,8 @@ namespace rmm {
 namespace {
 
 namespace pg {
-constexpr int kThreads = 256, kWaves = 4, TK = 32;
 constexpr float kTau = 8.f;               // lazy-rescale threshold, log2 units
-constexpr int kMinChunks = 8;             // chunks per workgroup at least
-constexpr int kMaxGroups = 512;           // workgroups: two per CU
+constexpr int kShort = 16;                // units of at most this many blocks are not cut
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
 template <typename F>
@@ -46,6 +48,17 @@ __device__ __forceinline__ float across_rows(float x, F f) {
 #endif
     return x;
 }
+// f over the lanes l, l ^ 32
+template <typename F>
+__device__ __forceinline__ float across_halves(float x, F f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+#endif
+    return x;
+}
+__device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
 
 __device__ __forceinline__ f32x4_t mfma(const uint4 a, const uint4 b, const f32x4_t c) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -55,7 +68,15 @@ __device__ __forceinline__ f32x4_t mfma(const uint4 a, const uint4 b, const f32x
     return c;
 #endif
 }
-// two codes (byte B of w) as packed bf16
+__device__ __forceinline__ f32x16_t mfma(const uint4 a, const uint4 b, const f32x16_t c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                   0, 0, 0);
+#else
+    return c;
+#endif
+}
+// two codes (byte B of w) as packed bf16, exact
 template <int B>
 __device__ __forceinline__ uint32_t unpack_mx(uint32_t w, float scale) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -64,539 +85,1131 @@ __device__ __forceinline__ uint32_t unpack_mx(uint32_t w, float scale) {
     return 0;
 #endif
 }
+__device__ __forceinline__ uint4 unpack_mx8(uint32_t w, float scale) {
+    return make_uint4(unpack_mx<0>(w, scale), unpack_mx<1>(w, scale), unpack_mx<2>(w, scale), unpack_mx<3>(w, scale));
+}
 __device__ __forceinline__ float exp_two(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// One sequence's share of the line of chunks
-struct Seq {
-    int q0, n, len, tiles, chunks;        // first token, new tokens, keys, row tiles, chunks per unit (0: no work)
-    bool bad;                             // longer than its row of the page table
-};
-__device__ __forceinline__ Seq seq_of(const PagedArgs &a, int b, int grp, int rows) {
-    Seq s;
-    int q1;
-    if (a.q_start) {
-        s.q0 = min(max(a.q_start[b], 0), static_cast<int>(a.T));
-        q1 = min(a.q_start[b + 1], static_cast<int>(a.T));
-    } else {
-        s.q0 = b;
-        q1 = b + 1;
-    }
-    s.n = max(q1 - s.q0, 0);
-    const int64_t cap = static_cast<int64_t>(a.width) << a.kv.lg_page;
-    s.len = max(a.lens[b], 0);
-    s.bad = s.len > cap;
-    if (s.bad) s.len = static_cast<int>(cap);
-    s.tiles = static_cast<int>((static_cast<int64_t>(s.n) * grp + rows - 1) / rows);
-    s.chunks = s.n > 0 ? max((s.len + TK - 1) / TK, 1) : 0;
-    return s;
-}
-__device__ __forceinline__ int64_t seq_work(const PagedArgs &a, const Seq &s) {
-    return static_cast<int64_t>(s.tiles) * s.chunks * a.kv.Hkv;
-}
-
-__device__ __forceinline__ int64_t shfl_up64(int64_t x, int d) { return __shfl_up(static_cast<long long>(x), d, 64); }
-
-// Sum of all sequences' work, the same in every lane
-__device__ __forceinline__ int64_t total_work(const PagedArgs &a, int grp, int rows) {
-    int64_t w = 0;
-    for (int b = threadIdx.x & 63; b < a.B; b += 64) w += seq_work(a, seq_of(a, b, grp, rows));
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(static_cast<long long>(w), d, 64);
+// of 8 bf16 values (w), those at the set bits of m
+__device__ __forceinline__ uint4 keep8(uint4 w, uint32_t m) {
+    w.x &= (m & 1 ? 0xffffu : 0u) | (m & 2 ? 0xffff0000u : 0u);
+    w.y &= (m & 4 ? 0xffffu : 0u) | (m & 8 ? 0xffff0000u : 0u);
+    w.z &= (m & 16 ? 0xffffu : 0u) | (m & 32 ? 0xffff0000u : 0u);
+    w.w &= (m & 64 ? 0xffffu : 0u) | (m & 128 ? 0xffff0000u : 0u);
     return w;
 }
-// The sequence whose chunks hold position x of the line, and where they begin
-__device__ __forceinline__ int find_seq(const PagedArgs &a, int grp, int rows, int64_t x, int64_t *start) {
-    int64_t base = 0;
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int b = b0 + lane;
-        const int64_t w = b < a.B ? seq_work(a, seq_of(a, b, grp, rows)) : 0;
-        int64_t s = w;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t y = shfl_up64(s, d);
-            if (lane >= d) s += y;
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// a / b of non-negative values
+__device__ __forceinline__ int quot(int a, int b) {
+    return uniform(static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)));
+}
+// inclusive prefix sum over the wave's lanes
+__device__ __forceinline__ int prefix_sum(int x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // lane 15 of a row to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // lane 31 to the upper half
+#endif
+    return x;
+}
+
+// ---- the line.  TK keys per block, ROWS query rows per unit.  The host keeps its
+// length below 2^31 (line_fits).
+struct Seq {
+    int q0, n, len;                       // first token, new tokens, keys
+    int bad;                              // longer than its row of the page table
+};
+template <int TK, int ROWS>
+struct Plan {
+    int grp, causal, Hkv;
+    bool whole;                           // units count one each (all are short)
+
+    __device__ __forceinline__ Seq load(const PagedArgs &a, int b) const {
+        Seq s;
+        int q1;
+        if (a.q_start) {
+            s.q0 = min(max(a.q_start[b], 0), static_cast<int>(a.T));
+            q1 = min(a.q_start[b + 1], static_cast<int>(a.T));
+        } else {
+            s.q0 = b;
+            q1 = b + 1;
         }
-        const uint64_t past = __ballot(base + s > x);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            *start = base + __shfl(static_cast<long long>(s - w), l, 64);
-            return b0 + l;
-        }
-        base += __shfl(static_cast<long long>(s), 63, 64);
+        s.n = max(q1 - s.q0, 0);
+        const int cap = a.width << a.kv.lg_page, len = max(a.lens[b], 0);
+        s.bad = len > cap;
+        s.len = min(len, cap);
+        return s;
     }
-    *start = base;
-    return a.B;
+    __device__ __forceinline__ int tiles(const Seq &s) const {
+        return static_cast<int>((static_cast<uint32_t>(s.n * grp) + ROWS - 1) / ROWS);
+    }
+    // keys that some row of a tile sees (at most; the last token of the tile given)
+    __device__ __forceinline__ int keys(const Seq &s, int last_tok) const {
+        return causal ? min(max(s.len - s.n + last_tok + 1, 0), s.len) : s.len;
+    }
+    __device__ __forceinline__ int last_token(const Seq &s, int tile) const {
+        return min(static_cast<int>((static_cast<uint32_t>(tile) * ROWS + ROWS - 1) / static_cast<uint32_t>(grp)), s.n - 1);
+    }
+    __device__ __forceinline__ int blocks(const Seq &s, int tile) const {
+        return max((keys(s, last_token(s, tile)) + TK - 1) / TK, 1);
+    }
+    __device__ __forceinline__ int weight(const Seq &s, int tile) const { return whole ? 1 : blocks(s, tile); }
+    // length on the line of a pair of tiles (p, 2 np - 1 - p)
+    __device__ __forceinline__ int pair(const Seq &s, int np) const {
+        if (whole) return 2;
+        if (np == 1 || !causal) return blocks(s, 0) + blocks(s, 2 * np - 1);
+        const int tok = static_cast<int>((static_cast<uint32_t>(np) * 2 * ROWS - 1) / static_cast<uint32_t>(grp));    // of a full last tile
+        const int k = min(max(s.len - s.n + tok + 1, 1), s.len + ROWS);
+        return blocks(s, 0) + (k + TK - 1) / TK + 2;
+    }
+    // a sequence's share of the line per kv head
+    __device__ __forceinline__ int head_work(const Seq &s) const {
+        const int t = tiles(s), np = t >> 1;
+        int w = np > 0 ? np * pair(s, np) : 0;
+        if (t & 1) w += weight(s, t - 1);
+        return w;
+    }
+    __device__ __forceinline__ int work(const Seq &s) const { return head_work(s) * Hkv; }
+    __device__ __forceinline__ int longest(const Seq &s) const {
+        return s.n > 0 ? blocks(s, tiles(s) - 1) : 0;
+    }
+};
+
+// A workgroup's place on the line
+template <int TK, int ROWS>
+struct Walk {
+    Plan<TK, ROWS> pl;
+    int x, begin, end, run;               // position, the workgroup's run, run length
+    int b, f;                             // the sequence at x, where it begins
+    Seq s;
+    // the unit at x
+    int kvh, tile, c0, c1;                // blocks [c0, c1) of it are in the run
+    int u0, u1;                           // its place on the line
+
+    // false: no work for this workgroup
+    __device__ __forceinline__ bool init(const PagedArgs &a, int wg, int min_run) {
+        const int lane = threadIdx.x & 63;
+        pl.grp = a.q.n / a.kv.Hkv;
+        pl.causal = a.causal;
+        pl.Hkv = a.kv.Hkv;
+        // whether all units are short, then the line's length: lane l looks at
+        // sequences l, l + 64, ...
+        Seq mine = {0, 0, 0, 0};
+        if (lane < a.B) mine = pl.load(a, lane);
+        int most = pl.longest(mine);
+        for (int i = lane + 64; i < a.B; i += 64) most = max(most, pl.longest(pl.load(a, i)));
+        pl.whole = __ballot(most > kShort) == 0;
+        const int w0 = pl.work(mine), sum0 = prefix_sum(w0);
+        int rest = 0;
+        for (int i = lane + 64; i < a.B; i += 64) rest += pl.work(pl.load(a, i));
+        int total = __builtin_amdgcn_readlane(sum0, 63);
+        if (a.B > 64) total += __builtin_amdgcn_readlane(prefix_sum(rest), 63);
+        run = quot(total + a.nw - 1, a.nw);
+        run = pl.whole ? max(run, 1) : (max(run, min_run) + 3) / 4 * 4;
+        const int64_t at = static_cast<int64_t>(wg) * run;
+        if (at >= total) return false;
+        begin = x = static_cast<int>(at);
+        end = min(total - x, run) + x;
+        // the sequence at x
+        int base = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            Seq q = mine;
+            int w = w0, sum = sum0;
+            if (b0 > 0) {
+                q = b0 + lane < a.B ? pl.load(a, b0 + lane) : Seq{0, 0, 0, 0};
+                w = pl.work(q);
+                sum = prefix_sum(w);
+            }
+            const uint64_t past = __ballot(base + sum > x);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                b = b0 + l;
+                f = base + __builtin_amdgcn_readlane(sum - w, l);
+                s.q0 = __builtin_amdgcn_readlane(q.q0, l);
+                s.n = __builtin_amdgcn_readlane(q.n, l);
+                s.len = __builtin_amdgcn_readlane(q.len, l);
+                s.bad = __builtin_amdgcn_readlane(q.bad, l);
+                break;
+            }
+            base += __builtin_amdgcn_readlane(sum, 63);
+        }
+        return true;
+    }
+    // the unit at x (false: x is at no unit and has moved on, or at the end)
+    __device__ __forceinline__ bool locate(const PagedArgs &a) {
+        const int hw = pl.head_work(s);
+        if (x >= f + hw * pl.Hkv) {       // the next sequence with work
+            f += hw * pl.Hkv;
+            const Seq q = pl.load(a, ++b);
+            s = {uniform(q.q0), uniform(q.n), uniform(q.len), uniform(q.bad)};
+            return false;
+        }
+        kvh = quot(x - f, hw);
+        const int y = x - f - kvh * hw;
+        const int t = pl.tiles(s), np = t >> 1;
+        const int pr = np > 0 ? pl.pair(s, np) : 0;
+        int off;
+        if (y < np * pr) {
+            const int p = quot(y, pr);
+            off = y - p * pr;
+            tile = p;
+            const int wa = pl.weight(s, p);
+            if (off >= wa) {
+                tile = 2 * np - 1 - p;
+                const int wb = pl.weight(s, tile);
+                if (off >= wa + wb) {     // the rest of the pair's length is empty
+                    x += pr - off;
+                    return false;
+                }
+                off -= wa;
+            }
+        } else {
+            tile = t - 1;
+            off = y - np * pr;
+        }
+        u0 = x - off;
+        u1 = u0 + pl.weight(s, tile);
+        c0 = pl.whole ? 0 : off;
+        c1 = pl.whole ? pl.blocks(s, tile) : min(end, u1) - u0;
+        return true;
+    }
+    __device__ __forceinline__ void advance() { x = min(end, u1); }
+    __device__ __forceinline__ bool complete() const { return u0 >= begin && u1 <= end; }
+    // 1: the piece of a cut unit that begins in this run, 0: of one that began before it
+    __device__ __forceinline__ int part() const { return u0 >= begin ? 1 : 0; }
+};
+
+// What the joining launch needs to know of a workgroup's piece of a cut unit:
+// the unit's workgroups first .. first + n - 1 (n = 0: no piece), its rows
+struct PieceOf {
+    int n, first, rows, q0, kvh, row0, pad0, pad1;
+};
+// A workgroup has at most two pieces: of the unit its run begins inside of
+// (slot 0) and of the one it ends inside of (slot 1)
+template <int TK, int ROWS>
+__device__ __forceinline__ PieceOf piece_of(const Walk<TK, ROWS> &w, int rows) {
+    const int first = quot(w.u0, w.run), last = quot(w.u1 - 1, w.run);
+    return {last - first + 1, first, rows, w.s.q0, w.kvh, w.tile * ROWS, 0, 0};
 }
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
-    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(static_cast<uint64_t>(x) >> 32));
-    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+
+// dims d, d + 1 of a cached row
+template <int D, bool MX>
+__device__ __forceinline__ float2 cached_pair(const uint8_t *rows, const uint8_t *scales, int64_t row, int d) {
+    uint32_t w;
+    if constexpr (MX) w = unpack_mx<0>(rows[row * (D / 2) + d / 2], __uint_as_float(static_cast<uint32_t>(scales[row * (D / 32) + d / 32]) << 23));
+    else w = *reinterpret_cast<const uint32_t *>(rows + (row * D + d) * 2);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-// chunks per workgroup: a whole number of rounds of the four waves
-__device__ __forceinline__ int64_t run_length(int64_t total, int nw) {
-    const int64_t per = (total + nw - 1) / nw;
-    return max((per + kWaves - 1) / kWaves * kWaves, static_cast<int64_t>(kMinChunks));
+
+// Query rows first, first + step, ... of a unit over its keys [k0, k1), one row
+// per wave with nothing shared between rows: what the units that meet an
+// infinite or NaN value are redone with, since there a weight or a query of zero
+// does not silence a key or value that a row does not see.  put(row, m, l,
+// d, o): maximum, sum and two dims of a row's output, called by every lane that holds some.
+template <int D, bool MX, bool IDX, typename Put>
+__device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, int b, int kvh, int row0, int n_rows,
+                                             int first, int step, int k0, int k1, const uint32_t (*keep)[D / 32], Put put) {
+    const int lane = threadIdx.x & 63, grp = a.q.n / a.kv.Hkv, lg = a.kv.lg_page;
+    const int32_t *trow = a.table + b * a.table_ld;
+    const int d2 = 2 * lane;                               // the lane's output dims (D / 2 lanes)
+#pragma unroll 1
+    for (int r = first; r < n_rows; r += step) {
+        const int tok = (row0 + r) / grp, hd = kvh * grp + (row0 + r) % grp;
+        const int see = min(k1, a.causal ? sq.len - sq.n + tok + 1 : sq.len);
+        const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
+        float m = -__builtin_inff(), l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll 1
+        for (int key0 = k0; key0 < see; key0 += 64) {
+            const int key = key0 + lane, pid = key < see ? trow[key >> lg] : 0;
+            const int page = pid >= 0 && pid < a.kv.n_pages ? pid : 0;
+            const int64_t row = (static_cast<int64_t>(kvh) << lg) + (key & ((1 << lg) - 1));
+            float sc = -__builtin_inff();
+            if (key < see) {
+                const uint8_t *kp = a.kv.k + page * a.kv.k_page, *sp = a.kv.ks + page * a.kv.ks_page;
+                float x = 0.f;
+#pragma unroll 1
+                for (int d = 0; d < D; d += 2) {
+                    const float2 k = cached_pair<D, MX>(kp, sp, row, d);
+                    const uint32_t bits = IDX ? keep[r][d >> 5] >> (d & 31) : 3u;
+                    if (bits & 1) x += bf16_to_f32(qp[d]) * k.x;
+                    if (bits & 2) x += bf16_to_f32(qp[d + 1]) * k.y;
+                }
+                sc = x * a.c;
+            }
+            float mx = sc;
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i, 64));
+            const float mn = fmaxf(m, mx), use = mn == -__builtin_inff() ? 0.f : mn;
+            const float al = exp_two((m == -__builtin_inff() ? use : m) - use);
+            const float p = exp_two(sc - use);
+            l *= al;
+            o0 *= al;
+            o1 *= al;
+            m = mn;
+            float ps = p;
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) ps += __shfl_xor(ps, i, 64);
+            l += ps;
+            const float pr = bf16_to_f32(f32_to_bf16(p));
+#pragma unroll 1
+            for (int i = 0; i < min(64, see - key0); ++i) {
+                const float w = __shfl(pr, i, 64);
+                const int64_t pg = __shfl(page, i, 64);
+                const int64_t vrow = (static_cast<int64_t>(kvh) << lg) + ((key0 + i) & ((1 << lg) - 1));
+                if (d2 < D) {
+                    const float2 v = cached_pair<D, MX>(a.kv.v + pg * a.kv.v_page, a.kv.vs + pg * a.kv.vs_page, vrow, d2);
+                    o0 += w * v.x;
+                    o1 += w * v.y;
+                }
+            }
+        }
+        if (d2 < D) put(r, m, l, d2, o0, o1);
+    }
+}
+
+// The retained dims of a unit's rows as bits (16 lanes per row); dims outside [0, D) are ignored
+template <int D, int NT>
+__device__ __forceinline__ void read_lists(const PagedArgs &a, const Seq &sq, int kvh, int row0, int n_rows, uint32_t (*keep)[D / 32]) {
+    const int H = a.q.n, grp = H / a.kv.Hkv;
+    for (int r = threadIdx.x >> 4; r < n_rows; r += NT / 16) {
+        const int q = row0 + r;
+        const int32_t *list = a.idx + (static_cast<int64_t>(sq.q0 + q / grp) * H + kvh * grp + q % grp) * a.k;
+        for (int u = threadIdx.x & 15; u < a.k; u += 16) {
+            const int d = list[u];
+            if (d >= 0 && d < D) atomicOr(&keep[r][d >> 5], 1u << (d & 31));
+        }
+    }
+}
+
+// Consecutive runs of the line on one XCD (workgroups are dealt to the 8 XCDs
+// in turn), where units that share keys share its L2
+__device__ __forceinline__ int line_index(int nw) {
+    const int i = static_cast<int>(blockIdx.x);
+    return i % 8 * (nw / 8) + i / 8;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt_le() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 }  // namespace pg
 
+// ------------------------------------------------------------- few rows
+namespace few {
+constexpr int kWaves = 4, kThreads = 64 * kWaves, TK = 32, ROWS = 16;
+constexpr int kGroups = 512;              // workgroups: two per CU
+constexpr int kMinRun = 8;                // chunks: two rounds of the four waves
+}  // namespace few
+
 }  // namespace
 
+// S^T = K Q^T takes 16 key rows as they are loaded (v_mfma_f32_16x16x32: a lane
+// holds 8 dims of one key).  In its result a lane holds one query row, and with
+// key 8 g + 4 tb + i at row 4 g + i of key tile tb exactly the eight keys that
+// its lane group contributes to O^T = V^T P^T: the weights stay where they are.
+// The value rows, loaded as rows, are turned 8 x 8 in registers (v_perm).  4-bit
+// codes become bf16 with v_cvt_scalef32_pk_bf16_fp4 (exact, the scale included).
 // MX: 4-bit cache; IDX: scores over retained dims
-template <int D, bool MX, int R, bool IDX>
-__global__ __launch_bounds__(pg::kThreads, R == 1 ? 2 : 1) void paged_attn_kernel(PagedArgs a) {
+template <int D, bool MX, bool IDX>
+__global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a) {
     using namespace pg;
+    using namespace few;
     constexpr int KS = D / 32, DM = D / 16;               // contraction steps of S^T, MFMA rows of O^T
     constexpr int ROWB = MX ? D / 2 : D * 2, SROWB = D / 32;    // bytes per cached row, scale bytes per row
     constexpr int OLD = D + 4;                            // row stride of the joining buffer, floats
     __shared__ __attribute__((aligned(16))) float oj[kWaves][16][OLD];
     __shared__ float ml[kWaves][16][2];
-    __shared__ uint32_t keep[IDX ? 16 * R : 1][KS];
+    __shared__ int state[kWaves];                         // bit 0: a page or length out of range, bit 1: to be redone
+    __shared__ uint32_t keep[IDX ? 16 : 1][KS];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int H = a.q.n, Hkv = a.kv.Hkv, grp = H / Hkv;
-
-    const int64_t total = uniform64(total_work(a, grp, 16 * R));
-    const int64_t run = run_length(total, a.nw);
-    int64_t x = blockIdx.x * run;
-    const int64_t x_end = min(total, x + run);
-    if (x >= x_end) return;
-    int64_t f = 0;
-    int b = __builtin_amdgcn_readfirstlane(find_seq(a, grp, 16 * R, x, &f));
-    f = uniform64(f);
-    const int64_t x_begin = x;
+    const int H = a.q.n, grp = H / a.kv.Hkv;
     const int lg = a.kv.lg_page, ps = 1 << lg;
+    const int wg = line_index(a.nw);
 
-    while (x < x_end) {
-        const Seq sq = seq_of(a, b, grp, 16 * R);
-        const int64_t end_b = f + seq_work(a, sq);
-        if (x >= end_b) {                                  // next sequence (an empty one has no chunks)
-            f = end_b;
-            ++b;
+    int held = 0;                                          // which of the two pieces there are
+    Walk<TK, ROWS> w;
+    bool more = w.init(a, wg, kMinRun);
+    while (more) {
+        if (!w.locate(a)) {
+            more = w.x < w.end;
             continue;
         }
-        const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>((x - f) / sq.chunks));
-        const int64_t u0 = f + static_cast<int64_t>(unit) * sq.chunks;
-        const int c0 = static_cast<int>(x - u0);
-        const int64_t u_end = u0 + sq.chunks;
-        const int c1 = static_cast<int>(min(x_end, u_end) - u0);
-        const int kvh = unit / sq.tiles, tile = unit % sq.tiles;
-        const int row0 = tile * 16 * R, n_rows = min(16 * R, sq.n * grp - row0);
-        const int64_t ubegin = u0;
+        const Seq sq = w.s;
+        const int kvh = w.kvh, row0 = w.tile * ROWS, n_rows = min(ROWS, sq.n * grp - row0);
 
         // ---- the unit's query rows
         if constexpr (IDX) {
-            for (int i = tid; i < 16 * R * KS; i += kThreads) (&keep[0][0])[i] = 0;
+            for (int i = tid; i < 16 * KS; i += kThreads) (&keep[0][0])[i] = 0;
             __syncthreads();
-            for (int i = tid; i < n_rows * a.k; i += kThreads) {
-                const int r = i / a.k, u = i - r * a.k, rho = row0 + r;
-                const int d = a.idx[(static_cast<int64_t>(sq.q0 + rho / grp) * H + kvh * grp + rho % grp) * a.k + u];
-                if (d >= 0 && d < D) atomicOr(&keep[r][d >> 5], 1u << (d & 31));
-            }
+            read_lists<D, kThreads>(a, sq, kvh, row0, n_rows, keep);
             __syncthreads();
         }
         // dims that lane (col, g) holds at contraction step s
         auto dim_of = [&](int s) { return MX ? (D / 4) * g + 8 * s : 32 * s + 8 * g; };
-        uint4 qf[R][KS];
-        int lim[R];                                        // last key the lane's row sees
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int rr = 16 * r + col, rho = row0 + rr;
-            const bool on = rr < n_rows;
-            const int tok = on ? rho / grp : 0, hd = on ? kvh * grp + rho % grp : 0;
-            lim[r] = !on ? -1 : a.causal ? sq.len - sq.n + tok : sq.len - 1;
+        const bool on = col < n_rows;
+        const int rho = row0 + col, tok = on ? rho / grp : 0;
+        uint4 qf[KS];
+        {
+            const int hd = on ? kvh * grp + rho % grp : 0;
             const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                uint4 w = make_uint4(0, 0, 0, 0);
-                if (on) w = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
-                if constexpr (IDX) {
-                    const uint32_t m = keep[rr][dim_of(s) >> 5] >> (dim_of(s) & 31);
-                    w.x &= (m & 1 ? 0xffffu : 0u) | (m & 2 ? 0xffff0000u : 0u);
-                    w.y &= (m & 4 ? 0xffffu : 0u) | (m & 8 ? 0xffff0000u : 0u);
-                    w.z &= (m & 16 ? 0xffffu : 0u) | (m & 32 ? 0xffff0000u : 0u);
-                    w.w &= (m & 64 ? 0xffffu : 0u) | (m & 128 ? 0xffff0000u : 0u);
-                }
-                qf[r][s] = w;
+                qf[s] = make_uint4(0, 0, 0, 0);
+                if (on) qf[s] = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
+                if constexpr (IDX) qf[s] = keep8(qf[s], keep[col][dim_of(s) >> 5] >> (dim_of(s) & 31));
             }
         }
-        // keys seen by every row / by no row past it
-        const int first_tok = row0 / grp, last_tok = (row0 + n_rows - 1) / grp;
-        const int lo_lim = a.causal ? sq.len - sq.n + first_tok : sq.len - 1;
-        const int hi_lim = a.causal ? sq.len - sq.n + last_tok : sq.len - 1;
-        const int c_stop = min(c1, hi_lim < 0 ? 0 : hi_lim / TK + 1);
+        // last key of the lane's row; the first limit and the last of the unit's rows
+        const int lim = !on ? -1 : a.causal ? sq.len - sq.n + tok : sq.len - 1;
+        const int tok_a = row0 / grp, tok_b = (row0 + n_rows - 1) / grp;
+        const int lo_lim = a.causal ? sq.len - sq.n + tok_a : sq.len - 1;
+        const int hi_lim = a.causal ? sq.len - sq.n + tok_b : sq.len - 1;
+        const int c_stop = min(w.c1, hi_lim < 0 ? 0 : hi_lim / TK + 1);
 
-        f32x4_t o[R][DM];
-        float m_run[R], l_run[R];
+        f32x4_t o[DM];
+        float m_run = -__builtin_inff(), l_run = 0.f, least = 0.f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            m_run[r] = -__builtin_inff();
-            l_run[r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < DM; ++i) o[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
+        for (int i = 0; i < DM; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         bool bad = sq.bad;
 
         // ---- the wave's chunks c0 + wave, + 4, ...; lane l holds the pages of the
         // l-th of them (two where a page has 16 keys)
-        const int32_t *trow = a.table + b * a.table_ld;
+        const int32_t *trow = a.table + w.b * a.table_ld;
         int pid_a = 0, pid_b = 0;
-        struct Chunk {
-            uint4 k[2][MX ? 1 : KS];
-            uint32_t ks[2];
-            uint4 v[MX ? 1 : 8];                           // bf16: DM elements of 8 value rows
-            uint32_t vc[8];                                // MX: DM codes of 8 value rows
-            uint4 vs[MX ? 2 : 1];
-        };
         auto fetch_pages = [&](int c) __attribute__((always_inline)) {
-            const int key = (c + kWaves * lane) * TK;      // this lane's chunk
-            const bool on = c + kWaves * lane < c_stop;
-            const int p0 = on ? key >> lg : 0, p1 = on && key + 16 < sq.len ? (key + 16) >> lg : p0;
-            pid_a = on ? trow[p0] : 0;
-            pid_b = on ? trow[p1] : 0;
+            const bool in = c + kWaves * lane < c_stop;
+            const int key = in ? (c + kWaves * lane) * TK : 0;
+            const int p0 = key >> lg, p1 = in && key + 16 < sq.len ? (key + 16) >> lg : p0;
+            pid_a = in ? trow[p0] : 0;
+            pid_b = in ? trow[p1] : 0;
             const bool oka = pid_a >= 0 && pid_a < a.kv.n_pages, okb = pid_b >= 0 && pid_b < a.kv.n_pages;
             if (__ballot(!oka || !okb)) bad = true;
             if (!oka) pid_a = 0;
             if (!okb) pid_b = 0;
         };
-        // rows of the chunk at keys 8 (col / 4) + 4 tb + col % 4 (K), 8 g + kk (V)
-        auto load = [&](Chunk &ck, int c, int nth) __attribute__((always_inline)) {
+        // keys 8 (col / 4) + 4 tb + col % 4 of the chunk (K), 8 g + kk (V): the
+        // lane's first row, among the second 16 keys for `second` lanes
+        auto row_at = [&](const uint8_t *base, int64_t page_bytes, int row_bytes, int c, int nth, bool second,
+                          int row) __attribute__((always_inline)) {
             const int64_t pa = __builtin_amdgcn_readlane(pid_a, nth), pb = __builtin_amdgcn_readlane(pid_b, nth);
-            const int key = c * TK, oa = key & (ps - 1), ob = (key + 16) & (ps - 1);
+            const int key = c * TK, oa = key & (ps - 1), ob = ((key + 16) & (ps - 1)) - 16;
             const int64_t hrow = static_cast<int64_t>(kvh) << lg;
-            const int krow = 8 * (col >> 2) + (col & 3), vrow = 8 * g;
-            const bool k2 = col >= 8, v2 = g >= 2;
-            const int64_t ra = hrow + oa, rb = hrow + ob - 16;
-            const uint8_t *kp = (k2 ? a.kv.k + pb * a.kv.k_page + rb * ROWB : a.kv.k + pa * a.kv.k_page + ra * ROWB) + krow * ROWB;
-            const uint8_t *vp = (v2 ? a.kv.v + pb * a.kv.v_page + rb * ROWB : a.kv.v + pa * a.kv.v_page + ra * ROWB) + vrow * ROWB;
+            const uint8_t *ra = base + pa * page_bytes + (hrow + oa) * row_bytes;
+            const uint8_t *rb = base + pb * page_bytes + (hrow + ob) * row_bytes;
+            return (second ? rb : ra) + row * row_bytes;
+        };
+        uint4 kraw[2][MX ? 1 : KS], vraw[MX ? 1 : 8], vsraw[MX ? 2 : 1];
+        uint32_t ksraw[2], vcraw[8];
+        auto load_k = [&](int c, int nth) __attribute__((always_inline)) {
+            const int krow = 8 * (col >> 2) + (col & 3);
+            const uint8_t *kp = row_at(a.kv.k, a.kv.k_page, ROWB, c, nth, col >= 8, krow);
             if constexpr (!MX) {
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                     for (int s = 0; s < KS; ++s)
-                        ck.k[tb][s] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 64 * s + 16 * g);
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    if constexpr (D == 128) {
-                        ck.v[kk] = *reinterpret_cast<const uint4 *>(vp + kk * ROWB + 16 * col);
-                    } else {
-                        const uint2 w = *reinterpret_cast<const uint2 *>(vp + kk * ROWB + 8 * col);
-                        ck.v[kk] = make_uint4(w.x, w.y, 0, 0);
-                    }
-                }
+                        kraw[tb][s] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 64 * s + 16 * g);
             } else {
-                const uint8_t *ksp = (k2 ? a.kv.ks + pb * a.kv.ks_page + rb * SROWB : a.kv.ks + pa * a.kv.ks_page + ra * SROWB) + krow * SROWB;
-                const uint8_t *vsp = (v2 ? a.kv.vs + pb * a.kv.vs_page + rb * SROWB : a.kv.vs + pa * a.kv.vs_page + ra * SROWB) + vrow * SROWB;
+                const uint8_t *sp = row_at(a.kv.ks, a.kv.ks_page, SROWB, c, nth, col >= 8, krow);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     if constexpr (D == 128) {
-                        ck.k[tb][0] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 16 * g);
-                        ck.ks[tb] = ksp[tb * 4 * SROWB + g];
+                        kraw[tb][0] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 16 * g);
+                        ksraw[tb] = sp[tb * 4 * SROWB + g];
                     } else {
-                        const uint2 w = *reinterpret_cast<const uint2 *>(kp + tb * 4 * ROWB + 8 * g);
-                        ck.k[tb][0] = make_uint4(w.x, w.y, 0, 0);
-                        ck.ks[tb] = ksp[tb * 4 * SROWB + (g >> 1)];
+                        const uint2 x = *reinterpret_cast<const uint2 *>(kp + tb * 4 * ROWB + 8 * g);
+                        kraw[tb][0] = make_uint4(x.x, x.y, 0, 0);
+                        ksraw[tb] = sp[tb * 4 * SROWB + (g >> 1)];
                     }
                 }
+            }
+        };
+        auto load_v = [&](int c, int nth) __attribute__((always_inline)) {
+            const uint8_t *vp = row_at(a.kv.v, a.kv.v_page, ROWB, c, nth, g >= 2, 8 * g);
+            if constexpr (!MX) {
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
-                    if constexpr (D == 128) ck.vc[kk] = *reinterpret_cast<const uint32_t *>(vp + kk * ROWB + 4 * col);
-                    else ck.vc[kk] = *reinterpret_cast<const uint16_t *>(vp + kk * ROWB + 2 * col);
+                    if constexpr (D == 128) {
+                        vraw[kk] = *reinterpret_cast<const uint4 *>(vp + kk * ROWB + 16 * col);
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(vp + kk * ROWB + 8 * col);
+                        vraw[kk] = make_uint4(x.x, x.y, 0, 0);
+                    }
                 }
-                ck.vs[0] = reinterpret_cast<const uint4 *>(vsp)[0];
-                if constexpr (D == 128) ck.vs[1] = reinterpret_cast<const uint4 *>(vsp)[1];
+            } else {
+                const uint8_t *sp = row_at(a.kv.vs, a.kv.vs_page, SROWB, c, nth, g >= 2, 8 * g);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    if constexpr (D == 128) vcraw[kk] = *reinterpret_cast<const uint32_t *>(vp + kk * ROWB + 4 * col);
+                    else vcraw[kk] = *reinterpret_cast<const uint16_t *>(vp + kk * ROWB + 2 * col);
+                }
+                vsraw[0] = reinterpret_cast<const uint4 *>(sp)[0];
+                if constexpr (D == 128) vsraw[MX ? 1 : 0] = reinterpret_cast<const uint4 *>(sp)[1];
             }
         };
 
-        auto compute = [&](const Chunk &ck, int c) __attribute__((always_inline)) {
+        // scores of chunk c, then the next chunk's keys are asked for
+        auto chunk = [&](int c, int nth, bool next) __attribute__((always_inline)) {
             const int key = c * TK;
             const bool edge = key + TK - 1 > lo_lim;       // wave-uniform: some row does not see every key
-            // ---- key fragments, and the value rows as pairs of dims
-            uint4 kf[2][KS];
-            uint32_t vr[8][DM / 2];
-            if constexpr (!MX) {
+            f32x4_t sc[2];
+            {
+                uint4 kf[2][KS];
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    const uint32_t cw[4] = {kraw[tb][0].x, kraw[tb][0].y, kraw[tb][0].z, kraw[tb][0].w};
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        if constexpr (MX) kf[tb][s] = unpack_mx8(cw[s], __uint_as_float(ksraw[tb] << 23));
+                        else kf[tb][s] = kraw[tb][s];
+                    }
+                }
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    sc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) sc[tb] = mfma(kf[tb][s], qf[s], sc[tb]);
+                }
+                if constexpr (IDX) {
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) least = fminf(least, sc[tb][i]);
+                }
+            }
+            if (next) load_k(c + kWaves, nth + 1);
+            // ---- weights
+            float p[2][4], mx = -__builtin_inff();
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[tb][i] = sc[tb][i] * a.c;
+            if (edge) {
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) kf[tb][s] = ck.k[tb][s];
+                    for (int i = 0; i < 4; ++i)
+                        if (key + 8 * g + 4 * tb + i > lim) p[tb][i] = -__builtin_inff();
+            }
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tb][i]);
+            mx = across_rows(mx, fmax2);
+            if (__ballot(mx > m_run + kTau)) {
+                const float m_new = fmaxf(m_run, mx);
+                const float al = m_new == -__builtin_inff() ? 1.f : exp_two(m_run - m_new);
+                l_run *= al;
+#pragma unroll
+                for (int i = 0; i < DM; ++i) o[i] *= al;
+                m_run = m_new;
+            }
+            // a row with nothing kept yet has only masked (-inf) scores here
+            const float m_use = m_run == -__builtin_inff() ? 0.f : m_run;
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[tb][i] = exp_two(p[tb][i] - m_use);
+                    l_run += p[tb][i];
+                }
+            const uint4 pf = make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
+                                        pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3]));
+            // ---- O^T += V^T P^T: dim DM * col + i of the value rows at MFMA i
+            uint32_t vr[8][DM / 2];
+            if constexpr (!MX) {
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
-                    const uint32_t w[4] = {ck.v[kk].x, ck.v[kk].y, ck.v[kk].z, ck.v[kk].w};
+                    const uint32_t x[4] = {vraw[kk].x, vraw[kk].y, vraw[kk].z, vraw[kk].w};
 #pragma unroll
-                    for (int p = 0; p < DM / 2; ++p) vr[kk][p] = w[p];
+                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = x[q];
                 }
             } else {
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    const float sc = __uint_as_float(ck.ks[tb] << 23);
-                    const uint32_t w[4] = {ck.k[tb][0].x, ck.k[tb][0].y, ck.k[tb][0].z, ck.k[tb][0].w};
-#pragma unroll
-                    for (int s = 0; s < KS; ++s)
-                        kf[tb][s] = make_uint4(unpack_mx<0>(w[s], sc), unpack_mx<1>(w[s], sc), unpack_mx<2>(w[s], sc),
-                                               unpack_mx<3>(w[s], sc));
-                }
-                const uint32_t sw[8] = {ck.vs[0].x, ck.vs[0].y, ck.vs[0].z, ck.vs[0].w,
-                                        ck.vs[MX ? 1 : 0].x, ck.vs[MX ? 1 : 0].y, ck.vs[MX ? 1 : 0].z, ck.vs[MX ? 1 : 0].w};
+                const uint32_t sw[8] = {vsraw[0].x, vsraw[0].y, vsraw[0].z, vsraw[0].w,
+                                        vsraw[MX ? 1 : 0].x, vsraw[MX ? 1 : 0].y, vsraw[MX ? 1 : 0].z, vsraw[MX ? 1 : 0].w};
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
                     // D = 128: four scale bytes per row; D = 64: two
                     const uint32_t sb = D == 128 ? (sw[kk] >> (8 * (col >> 2))) & 0xffu
                                                  : (sw[kk >> 1] >> (16 * (kk & 1) + 8 * (col >> 3))) & 0xffu;
-                    const float sc = __uint_as_float(sb << 23);
-                    vr[kk][0] = unpack_mx<0>(ck.vc[kk], sc);
-                    vr[kk][1] = unpack_mx<1>(ck.vc[kk], sc);
+                    const uint4 x = unpack_mx8(vcraw[kk], __uint_as_float(sb << 23));
+                    vr[kk][0] = x.x;
+                    vr[kk][1] = x.y;
                     if constexpr (D == 128) {
-                        vr[kk][2] = unpack_mx<2>(ck.vc[kk], sc);
-                        vr[kk][3] = unpack_mx<3>(ck.vc[kk], sc);
+                        vr[kk][2] = x.z;
+                        vr[kk][3] = x.w;
                     }
                 }
             }
-            // ---- scores of the row tiles and their weights
-            uint4 pf[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                f32x4_t sc[2];
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    sc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) sc[tb] = mfma(kf[tb][s], qf[r][s], sc[tb]);
-                }
-                if constexpr (IDX) {
-                    // an infinite or NaN key value in a dim that a row drops must not
-                    // reach it: then each row multiplies keys cleared by its own set
-                    bool fin = true;
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) fin = fin && __builtin_fabsf(sc[tb][i]) < __builtin_inff();
-                    if (__ballot(!fin)) {
-                        for (int cc = 0; cc < 16; ++cc) {
-#pragma unroll
-                            for (int tb = 0; tb < 2; ++tb) {
-                                f32x4_t t = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                                for (int s = 0; s < KS; ++s) {
-                                    const uint32_t m = keep[16 * r + cc][dim_of(s) >> 5] >> (dim_of(s) & 31);
-                                    uint4 w = kf[tb][s];
-                                    w.x &= (m & 1 ? 0xffffu : 0u) | (m & 2 ? 0xffff0000u : 0u);
-                                    w.y &= (m & 4 ? 0xffffu : 0u) | (m & 8 ? 0xffff0000u : 0u);
-                                    w.z &= (m & 16 ? 0xffffu : 0u) | (m & 32 ? 0xffff0000u : 0u);
-                                    w.w &= (m & 64 ? 0xffffu : 0u) | (m & 128 ? 0xffff0000u : 0u);
-                                    t = mfma(w, qf[r][s], t);
-                                }
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) sc[tb][i] = col == cc ? t[i] : sc[tb][i];
-                            }
-                        }
-                    }
-                }
-                float p[2][4], mx = -__builtin_inff();
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[tb][i] = sc[tb][i] * a.c;
-                        if (edge && key + 8 * g + 4 * tb + i > lim[r]) p[tb][i] = -__builtin_inff();
-                        mx = fmaxf(mx, p[tb][i]);
-                    }
-                mx = across_rows(mx, [](float u, float v) { return fmaxf(u, v); });
-                if (__ballot(mx > m_run[r] + kTau)) {
-                    const float m_new = fmaxf(m_run[r], mx);
-                    const float al = m_new == -__builtin_inff() ? 1.f : exp_two(m_run[r] - m_new);
-                    l_run[r] *= al;
-#pragma unroll
-                    for (int i = 0; i < DM; ++i) o[r][i] *= al;
-                    m_run[r] = m_new;
-                }
-                const float m_use = m_run[r] == -__builtin_inff() ? 0.f : m_run[r];
-                float ls = 0.f;
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[tb][i] = exp_two(p[tb][i] - m_use);
-                        ls += p[tb][i];
-                    }
-                l_run[r] += ls;
-                pf[r] = make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
-                                   pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3]));
-            }
-            // ---- O^T += V^T P^T: dim DM * col + i of the value rows at MFMA i
             auto value_frag = [&](const uint32_t(&v)[8][DM / 2], int i) __attribute__((always_inline)) {
                 const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-                uint4 w;
-                w.x = __builtin_amdgcn_perm(v[1][i >> 1], v[0][i >> 1], sel);
-                w.y = __builtin_amdgcn_perm(v[3][i >> 1], v[2][i >> 1], sel);
-                w.z = __builtin_amdgcn_perm(v[5][i >> 1], v[4][i >> 1], sel);
-                w.w = __builtin_amdgcn_perm(v[7][i >> 1], v[6][i >> 1], sel);
-                return w;
+                return make_uint4(__builtin_amdgcn_perm(v[1][i >> 1], v[0][i >> 1], sel),
+                                  __builtin_amdgcn_perm(v[3][i >> 1], v[2][i >> 1], sel),
+                                  __builtin_amdgcn_perm(v[5][i >> 1], v[4][i >> 1], sel),
+                                  __builtin_amdgcn_perm(v[7][i >> 1], v[6][i >> 1], sel));
             };
-            if (!edge) {
+            if (edge) {                                    // nothing of what lies past the last key seen
+                const uint32_t m = (1u << min(max(hi_lim + 1 - key - 8 * g, 0), 8)) - 1;
 #pragma unroll
-                for (int i = 0; i < DM; ++i) {
-                    const uint4 w = value_frag(vr, i);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) o[r][i] = mfma(w, pf[r], o[r][i]);
-                }
+                for (int i = 0; i < DM; ++i) o[i] = mfma(keep8(value_frag(vr, i), m), pf, o[i]);
             } else {
-                // A weight of zero does not silence an infinite or NaN value, so the
-                // rows of each token multiply values cleared past what it sees
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int ra = row0 + 16 * r, rb = min(ra + 15, row0 + n_rows - 1);
-                    if (ra > rb) continue;
-                    const int t0 = a.causal ? ra / grp : 0, t1 = a.causal ? rb / grp : 0;
-                    for (int tok = t0; tok <= t1; ++tok) {
-                        const int last = a.causal ? sq.len - sq.n + tok : sq.len - 1;
-                        uint32_t vm[8][DM / 2];
+                for (int i = 0; i < DM; ++i) o[i] = mfma(value_frag(vr, i), pf, o[i]);
+            }
+            if (next) load_v(c + kWaves, nth + 1);
+        };
+        for (int c = w.c0 + wave; c < c_stop;) {           // up to 64 chunks per fetch of page numbers
+            fetch_pages(c);
+            const int n = min(64, (c_stop - c + kWaves - 1) / kWaves);
+            load_k(c, 0);
+            load_v(c, 0);
+            for (int i = 0; i < n; ++i) chunk(c + kWaves * i, i, i + 1 < n);
+            c += kWaves * n;
+        }
+
+        // ---- the four waves join
+        const bool complete = w.complete();
+        const int part = w.part();
+        const float l = across_rows(l_run, add2);
+        bool odd = !(l < __builtin_inff()) || (IDX && least == -__builtin_inff());
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)
+        for (int i = 0; i < DM; ++i)
 #pragma unroll
-                            for (int p = 0; p < DM / 2; ++p) vm[kk][p] = key + 8 * g + kk <= last ? vr[kk][p] : 0u;
-                        const bool mine = lim[r] == last;
+            for (int e = 0; e < 4; ++e) odd = odd || !(__builtin_fabsf(o[i][e]) < __builtin_inff());
+        const bool redo = __ballot(on && odd) != 0;
+        __syncthreads();
+        if (lane == 0) state[wave] = bad ? 1 : redo ? 2 : 0;
+        if (g == 0) {
+            ml[wave][col][0] = m_run;
+            ml[wave][col][1] = l;
+        }
 #pragma unroll
-                        for (int i = 0; i < DM; ++i) {
-                            const f32x4_t t = mfma(value_frag(vm, i), pf[r], o[r][i]);
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[r][i][e] = mine ? t[e] : o[r][i][e];
-                        }
-                    }
+            for (int i = 0; i < DM; i += 4)
+                *reinterpret_cast<float4 *>(&oj[wave][col][DM * (4 * g + e) + i]) =
+                    make_float4(o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]);
+        __syncthreads();
+        const int all = state[0] | state[1] | state[2] | state[3];
+        // row r of the unit: N dims from d on
+        auto put = [&](int r, float m, float ls, int d, const auto &acc) __attribute__((always_inline)) {
+            constexpr int N = sizeof(acc) / sizeof(float);
+            if (complete) {
+                const int q = row0 + r;
+                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + q / grp) * a.o.st + (kvh * grp + q % grp) * a.o.sh + d;
+                uint32_t x[N / 2];
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) x[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+                if constexpr (N == 8) *reinterpret_cast<uint4 *>(op) = make_uint4(x[0], x[1], x[2], x[3]);
+                else if constexpr (N == 4) *reinterpret_cast<uint2 *>(op) = make_uint2(x[0], x[1]);
+                else *reinterpret_cast<uint32_t *>(op) = x[0];
+            } else {
+                const int64_t prow = (2 * static_cast<int64_t>(wg) + part) * ROWS + r;
+                if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * prow) = make_float2(m, ls);
+#pragma unroll
+                for (int i = 0; i < N; i += N >= 4 ? 4 : 2) {
+                    float *po = a.part_o + prow * D + d + i;
+                    if constexpr (N >= 4) *reinterpret_cast<float4 *>(po) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+                    else *reinterpret_cast<float2 *>(po) = make_float2(acc[0], acc[1]);
                 }
             }
         };
-
-        {
-            Chunk ca, cb;
-            int c = c0 + wave;
-            while (c < c_stop) {                           // up to 64 chunks per fetch of page numbers
-                fetch_pages(c);
-                const int n = min(64, (c_stop - c + kWaves - 1) / kWaves);
-                load(ca, c, 0);
-                for (int i = 0; i < n; i += 2) {
-                    if (i + 1 < n) load(cb, c + kWaves * (i + 1), i + 1);
-                    compute(ca, c + kWaves * i);
-                    if (i + 1 < n) {
-                        if (i + 2 < n) load(ca, c + kWaves * (i + 2), i + 2);
-                        compute(cb, c + kWaves * (i + 1));
-                    }
-                }
-                c += kWaves * n;
-            }
-        }
-
-        // ---- the four waves join, 16 rows at a time
-        const bool whole = ubegin >= x_begin && u_end <= x_end;
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (ubegin >= x_begin ? 1 : 0);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float l = across_rows(l_run[r], [](float u, float v) { return u + v; });
-            __syncthreads();
-            if (g == 0) {
-                ml[wave][col][0] = m_run[r];
-                ml[wave][col][1] = bad ? __builtin_nanf("") : l;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < DM; i += 4)
-                    *reinterpret_cast<float4 *>(&oj[wave][col][DM * (4 * g + e) + i]) =
-                        make_float4(o[r][i][e], o[r][i + 1][e], o[r][i + 2][e], o[r][i + 3][e]);
-            __syncthreads();
+        if (all == 2) {
+            careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, kWaves, w.c0 * TK, w.c1 * TK, keep,
+                                     [&](int r, float m, float ls, int d, float x, float y) {
+                                         const float acc[2] = {x, y};
+                                         put(r, m, ls, d, acc);
+                                     });
+        } else {
             const int rr = tid >> 4, d0 = (tid & 15) * DM;
-            if (16 * r + rr < n_rows) {
+            if (rr < n_rows) {
                 float m = -__builtin_inff(), ls = 0.f, acc[DM];
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w][rr][0]);
+                for (int v = 0; v < kWaves; ++v) m = fmaxf(m, ml[v][rr][0]);
 #pragma unroll
                 for (int i = 0; i < DM; ++i) acc[i] = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const float mw = ml[w][rr][0], al = mw == -__builtin_inff() ? 0.f : exp_two(mw - m);
-                    const float lw = ml[w][rr][1];
-                    ls += lw == lw ? lw * al : lw;
+                for (int v = 0; v < kWaves; ++v) {
+                    const float mw = ml[v][rr][0], al = mw == -__builtin_inff() ? 0.f : exp_two(mw - m);
+                    ls += ml[v][rr][1] * al;
 #pragma unroll
-                    for (int i = 0; i < DM; ++i) acc[i] += al == 0.f ? 0.f : al * oj[w][rr][d0 + i];
+                    for (int i = 0; i < DM; ++i) acc[i] += al * oj[v][rr][d0 + i];
                 }
-                if (whole) {
-                    const int rho = row0 + 16 * r + rr;
-                    const float inv = ls == 0.f ? 0.f : 1.f / ls;
-                    uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + rho / grp) * a.o.st +
-                                   (kvh * grp + rho % grp) * a.o.sh + d0;
-                    uint32_t w[DM / 2];
-#pragma unroll
-                    for (int i = 0; i < DM / 2; ++i) w[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-                    if constexpr (D == 128) *reinterpret_cast<uint4 *>(op) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2 *>(op) = make_uint2(w[0], w[1]);
-                } else {
-                    const int64_t prow = slot * (16 * R) + 16 * r + rr;
-                    if ((tid & 15) == 0) {
-                        a.part_ml[2 * prow] = m;
-                        a.part_ml[2 * prow + 1] = ls;
-                    }
-#pragma unroll
-                    for (int i = 0; i < DM; i += 4)
-                        *reinterpret_cast<float4 *>(a.part_o + prow * D + d0 + i) =
-                            make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-                }
+                put(rr, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
             }
         }
-        x = f + static_cast<int64_t>(unit) * sq.chunks + c1;
+        if (!complete) {
+            if (tid == 0) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + part] = piece_of(w, n_rows);
+            held |= 1 << part;
+        }
+        w.advance();
+        more = w.x < w.end;
     }
+    if (tid < 2 && !(held >> tid & 1)) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + tid].n = 0;
 }
 
-// Joins the pieces of the cut unit that workgroup blockIdx.x ends inside of or
-// continues: the unit's pieces are those of workgroups i0 .. i1, and workgroup
-// i0 + q of them takes its rows q, q + (i1 - i0 + 1), ...
-template <int D, int R>
-__global__ __launch_bounds__(pg::kThreads) void paged_merge_kernel(PagedArgs a) {
+// ------------------------------------------------------------ many rows
+namespace rowsk {
+constexpr int TK = 64, NS = 4;            // keys per tile, ring slots
+constexpr int kGroups = 256;              // workgroups: one per CU
+constexpr int kMinRun = 4;                // tiles
+}  // namespace rowsk
+
+// NW waves of 32 query rows over a ring of 64-key tiles in LDS, each filled two
+// steps (bf16, by LDS DMA) or one step (4-bit, through registers, as bf16) ahead:
+// S^T = K Q^T with v_mfma_f32_32x32x16 (a lane holds 16 keys of one row), online softmax in log2
+// units, O^T += V^T P^T with V^T by the transposing LDS read.  Step i multiplies
+// the keys of tile i and the values of tile i - 1; the two halves of the
+// workgroup take the softmax at opposite ends of a step, so that one's
+// exponentials meet the other's matrix instructions.
+template <int D, bool MX, int NW, bool IDX>
+__global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
     using namespace pg;
-    constexpr int LD = D / 4, PW = kThreads / LD;          // lanes per row, pieces taken at once
+    using namespace rowsk;
+    constexpr int ROWS = 32 * NW, NT = 64 * NW;
+    constexpr int KS = D / 16, DB = D / 32;               // contraction steps of S^T, 32-dim blocks of O^T
+    constexpr int RB = D * 2, KB = TK * RB;               // bytes per staged row, of the keys of a slot
+    constexpr int CH = RB / 16;                           // 16-byte chunks per row
+    __shared__ __attribute__((aligned(1024))) char slot0[2 * KB], slot1[2 * KB], slot2[2 * KB], slot3[2 * KB];
+    __shared__ uint32_t keep[IDX ? ROWS : 1][D / 32];
+    __shared__ int state;                                 // bit 0: a page or length out of range, bit 1: to be redone
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lr = lane & 31, lh = lane >> 5;
+    const int H = a.q.n, grp = H / a.kv.Hkv;
+    const int lg = a.kv.lg_page, ps = 1 << lg;
+    const int wg = line_index(a.nw);
+    // scale: a negative one is taken into the queries; zero as the smallest normal
+    // float, which leaves the weights of finite scores exactly 1 and of masked ones 0
+    const float c = fmaxf(__builtin_fabsf(a.c), 1.17549435e-38f);
+    const uint32_t flip = a.c < 0.f ? 0x80008000u : 0u;
+
+    // chunk p of staged row r sits at p ^ swizzle(r): rows that are read together at
+    // one chunk fall on distinct banks
+    auto kswz = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
+    auto vswz = [](int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
+    // K fragment (A of S^T): key row 32 tb + lr, chunk 2 ks + lh
+    int kaddr[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kaddr[ks] = lr * RB + 16 * ((2 * ks + lh) ^ kswz(lr));
+    // V^T fragment (A of O^T): 16-lane group gr reads keys 16 st + 4 (gr / 2) + s16 / 4 (and
+    // + 8) of dims 32 db + 16 (gr % 2) + 4 (s16 % 4) .. + 3 (transposing read)
+    int vaddr[DB];
+    {
+        const int gr = lane >> 4, s16 = lane & 15, vv = s16 >> 2, qq = s16 & 3, r = 4 * (gr >> 1) + vv;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            vaddr[db] = KB + r * RB + 16 * ((4 * db + 2 * (gr & 1) + (qq >> 1)) ^ vswz(r)) + 8 * (qq & 1);
+    }
+
+    int held = 0;                                          // which of the two pieces there are
+    Walk<TK, ROWS> w;
+    bool more = w.init(a, wg, kMinRun);
+    while (more) {
+        if (!w.locate(a)) {
+            more = w.x < w.end;
+            continue;
+        }
+        const Seq sq = w.s;
+        const int kvh = w.kvh, row0 = w.tile * ROWS, n_rows = min(ROWS, sq.n * grp - row0);
+        const int hi_lim = a.causal ? sq.len - sq.n + (row0 + n_rows - 1) / grp : sq.len - 1;
+        const int kend = max(hi_lim + 1, 0);               // keys that some row sees
+        const int c_end = kend == 0 ? w.c0 : w.c1;
+        const int n_tiles = c_end - w.c0;
+        if (tid == 0) state = sq.bad;
+
+        // ---- the wave's rows
+        const int rr = wave * 32 + lr, rho = row0 + rr;
+        const bool on = rr < n_rows;
+        const int tok = on ? rho / grp : 0;
+        const int hd = on ? kvh * grp + rho % grp : 0;
+        const int lim = !on ? -1 : a.causal ? sq.len - sq.n + tok : sq.len - 1;
+        const int wa = row0 + wave * 32, wb = min(wa + 31, row0 + n_rows - 1);      // the wave's rows (none: wb < wa)
+        const int tok_a = wa / grp, tok_b = max(wb, wa) / grp;
+        const int lim_lo = a.causal ? sq.len - sq.n + tok_a : sq.len - 1;      // every row of the wave sees these
+        const int lim_hi = wb < wa ? -1 : a.causal ? sq.len - sq.n + tok_b : sq.len - 1;
+
+        if constexpr (IDX) {
+            for (int i = tid; i < ROWS * (D / 32); i += NT) (&keep[0][0])[i] = 0;
+            __syncthreads();
+            read_lists<D, NT>(a, sq, kvh, row0, n_rows, keep);
+            __syncthreads();
+        }
+        uint4 qf[KS];
+        {
+            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                qf[ks] = make_uint4(0, 0, 0, 0);
+                if (on) qf[ks] = *reinterpret_cast<const uint4 *>(qp + 16 * ks + 8 * lh);
+                if constexpr (IDX) qf[ks] = keep8(qf[ks], keep[rr][ks >> 1] >> (16 * (ks & 1) + 8 * lh));
+                qf[ks].x ^= flip; qf[ks].y ^= flip; qf[ks].z ^= flip; qf[ks].w ^= flip;
+            }
+        }
+
+        // ---- staging
+        const int32_t *trow = a.table + w.b * a.table_ld;
+        bool bad = false;
+        auto page_at = [&](int key, bool in) __attribute__((always_inline)) {
+            int pid = in ? trow[key >> lg] : 0;
+            const bool ok = pid >= 0 && pid < a.kv.n_pages;
+            if (__ballot(!ok)) bad = true;
+            return ok ? pid : 0;
+        };
+        const int64_t hrow = static_cast<int64_t>(kvh) << lg;
+        // bf16: the wave stages RPW rows of keys and of values, NP pages' worth; lane l
+        // holds the pages of tile pbase + l
+        constexpr int RPW = TK / NW, NP = RPW > 16 ? RPW / 16 : 1, PR = RPW / NP;    // rows per page piece
+        constexpr int RPI = 1024 / RB, PER_K = RPW / RPI, PER = 2 * PER_K;           // rows, DMA instructions
+        int pid[NP], pbase = 0;
+        auto fetch = [&](int kt) __attribute__((always_inline)) {
+            pbase = kt;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int key = (kt + lane) * TK + wave * RPW + 16 * p;
+                pid[p] = page_at(key, kt + lane < c_end && key < kend);
+            }
+        };
+        auto dma = [&](char *slot, int kt) __attribute__((always_inline)) {
+            if (kt - pbase >= 64) fetch(kt);
+            const int r = lane / CH, ch = lane % CH;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int key = kt * TK + wave * RPW + 16 * p;
+                const int rows = kt < c_end ? max(0, min(PR, kend - key)) : 0;
+                const int64_t page = __builtin_amdgcn_readlane(pid[p], (kt - pbase) & 63);
+                const int64_t at = (hrow + (key & (ps - 1))) * RB;
+                const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+                    a.kv.k + page * a.kv.k_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
+                const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+                    a.kv.v + page * a.kv.v_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
+#pragma unroll
+                for (int u = 0; u < PER_K / NP; ++u) {
+                    const int row = wave * RPW + 16 * p + u * RPI;      // first row of the instruction in the tile
+                    lds_load16(kr, slot + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ kswz(row + r))));
+                    lds_load16(vr, slot + KB + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ vswz(row + r))));
+                }
+            }
+        };
+        // 4-bit: a thread takes groups of 32 dims (16 bytes of codes, a scale byte);
+        // lane l holds the page of key block l % 4 (16 keys) of tile pbase + l / 4
+        constexpr int GPR = D / 32, UNITS = 2 * TK * GPR, UPT = UNITS > NT ? UNITS / NT : 1;
+        uint4 cr[UPT];
+        uint32_t csr[UPT];
+        int pcur = 0, pnext = 0;
+        auto mx_pages = [&](int kt) __attribute__((always_inline)) {
+            const int key = (kt + (lane >> 2)) * TK + 16 * (lane & 3);
+            return page_at(key, kt + (lane >> 2) < c_end && key < kend);
+        };
+        auto mx_load = [&](int kt) __attribute__((always_inline)) {
+            if (kt - pbase >= 16) {
+                pcur = pnext;
+                pbase += 16;
+                pnext = mx_pages(pbase + 16);
+            }
+#pragma unroll
+            for (int u = 0; u < UPT; ++u) {
+                const int id = tid + NT * u, kid = id % (TK * GPR), r = kid / GPR, gi = kid % GPR;
+                const bool val = id >= TK * GPR;
+                const int key = kt * TK + r;
+                const int64_t page = __shfl(pcur, (4 * (kt - pbase) + (r >> 4)) & 63, 64);
+                cr[u] = make_uint4(0, 0, 0, 0);
+                csr[u] = 0;
+                if (id < UNITS && kt < c_end && key < kend) {
+                    const int64_t row = hrow + (key & (ps - 1));
+                    const uint8_t *cp = (val ? a.kv.v + page * a.kv.v_page : a.kv.k + page * a.kv.k_page) + row * (D / 2);
+                    const uint8_t *sp = (val ? a.kv.vs + page * a.kv.vs_page : a.kv.ks + page * a.kv.ks_page) + row * GPR;
+                    cr[u] = reinterpret_cast<const uint4 *>(cp)[gi];
+                    csr[u] = sp[gi];
+                }
+            }
+        };
+        auto mx_store = [&](char *slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < UPT; ++u) {
+                const int id = tid + NT * u, kid = id % (TK * GPR), r = kid / GPR, gi = kid % GPR;
+                if (id >= UNITS) continue;
+                char *row = slot + (id >= TK * GPR ? KB : 0) + r * RB;
+                const int swz = id >= TK * GPR ? vswz(r) : kswz(r);
+                const uint32_t cw[4] = {cr[u].x, cr[u].y, cr[u].z, cr[u].w};
+                const float sc = __uint_as_float(csr[u] << 23);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<uint4 *>(row + 16 * ((4 * gi + j) ^ swz)) = unpack_mx8(cw[j], sc);
+            }
+        };
+
+        // ---- one tile's work
+        f32x16_t o[DB];
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+        float m_run = -__builtin_inff(), l_run = 0.f, least = 0.f;
+        f32x16_t s[2];
+        uint4 pf[TK / 16];
+        // s[tb][v] is key kt * TK + 32 tb + 8 (v / 4) + 4 lh + v % 4 of row lr
+        auto qk = [&](const char *slot) __attribute__((always_inline)) {
+            uint4 kf[KS][2];                               // all fragments first, so the MFMAs wait once
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) kf[ks][tb] = *reinterpret_cast<const uint4 *>(slot + kaddr[ks] + 32 * tb * RB);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[tb][v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) s[tb] = mfma(kf[ks][tb], qf[ks], s[tb]);
+            if constexpr (IDX) {
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) least = fminf(least, s[tb][v]);
+            }
+        };
+        auto softmax = [&](int kt) __attribute__((always_inline)) {
+            const int t0 = kt * TK;
+            if (t0 + TK - 1 > lim_lo) {                    // the tile crosses some row's limit
+                const int rel = lim - t0 - 4 * lh;
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (32 * tb + 8 * (v >> 2) + (v & 3) > rel) s[tb][v] = -__builtin_inff();
+            }
+            float m4[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) m4[v & 3] = fmaxf(m4[v & 3], s[tb][v]);
+            const float mx = across_halves(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fmax2);
+            const float mt = mx == -__builtin_inff() ? mx : mx * c;
+            const bool need = mt > m_run + kTau;
+            if (__ballot(need)) {
+                const float al = need ? exp_two(m_run - mt) : 1.f;
+                l_run *= al;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[db][v] *= al;
+                m_run = need ? mt : m_run;
+            }
+            const float mu = m_run == -__builtin_inff() ? 0.f : m_run;
+            float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float p = exp_two(__builtin_fmaf(s[tb][v], c, -mu));
+                    s[tb][v] = p;
+                    l4[v & 3] += p;
+                }
+            l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            // weights of keys 16 st + 8 (e / 4) + 4 lh + e % 4: the order of the V^T fragments
+#pragma unroll
+            for (int st = 0; st < TK / 16; ++st) {
+                const int tb = st >> 1, v0 = 8 * (st & 1);
+                pf[st] = make_uint4(pack_bf16x2(s[tb][v0], s[tb][v0 + 1]), pack_bf16x2(s[tb][v0 + 2], s[tb][v0 + 3]),
+                                    pack_bf16x2(s[tb][v0 + 4], s[tb][v0 + 5]), pack_bf16x2(s[tb][v0 + 6], s[tb][v0 + 7]));
+            }
+        };
+        auto pv = [&](const char *slot) __attribute__((always_inline)) {
+            uint4 vf[TK / 16][DB];                         // all fragments first, so the MFMAs wait once
+#pragma unroll
+            for (int st = 0; st < TK / 16; ++st)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const char *p = slot + vaddr[db] + 16 * st * RB;
+                    const s16x4_t lo = lds_read_tr16(p);
+                    const s16x4_t hi = lds_read_tr16(p + 8 * RB);
+                    vf[st][db] = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int st = 0; st < TK / 16; ++st)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) o[db] = mfma(vf[st][db], pf[st], o[db]);
+        };
+
+        // ---- the ring: tile c0 + i lives in slot i % 4
+        const int t0 = w.c0;
+        if constexpr (!MX) {
+            fetch(t0);
+            dma(slot0, t0);
+            dma(slot1, t0 + 1);
+            wait_vmcnt_le<PER>();
+        } else {
+            pbase = t0;
+            pcur = mx_pages(t0);
+            pnext = mx_pages(t0 + 16);
+            mx_load(t0);
+            mx_store(slot0);
+            mx_load(t0 + 1);
+        }
+        lds_barrier();
+        auto slot_at = [&](auto S) -> char * {
+            constexpr int sl = decltype(S)::value;
+            if constexpr (sl == 0) return slot0;
+            else if constexpr (sl == 1) return slot1;
+            else if constexpr (sl == 2) return slot2;
+            else return slot3;
+        };
+        const bool late = wave >= NW / 2;
+        auto active = [&](int i) { return i >= 0 && i < n_tiles && (t0 + i) * TK <= lim_hi; };
+        auto step = [&](auto S, int i) __attribute__((always_inline)) {
+            constexpr int sl = decltype(S)::value;
+            if constexpr (!MX) {
+                dma(slot_at(std::integral_constant<int, (sl + 2) % NS>{}), t0 + i + 2);
+            } else {
+                mx_store(slot_at(std::integral_constant<int, (sl + 1) % NS>{}));
+                mx_load(t0 + i + 2);
+            }
+            const bool prev = active(i - 1), cur = active(i);
+            if (late && prev) softmax(t0 + i - 1);
+            if (prev) pv(slot_at(std::integral_constant<int, (sl + 3) % NS>{}));
+            if (cur) qk(slot_at(S));
+            if (!late && cur) softmax(t0 + i);
+            if constexpr (!MX) wait_vmcnt_le<PER>();
+            lds_barrier();
+        };
+        for (int i = 0; i <= n_tiles; i += NS) {
+            step(std::integral_constant<int, 0>{}, i);
+            if (i + 1 <= n_tiles) step(std::integral_constant<int, 1>{}, i + 1);
+            if (i + 2 <= n_tiles) step(std::integral_constant<int, 2>{}, i + 2);
+            if (i + 3 <= n_tiles) step(std::integral_constant<int, 3>{}, i + 3);
+        }
+        wait_vmcnt_le<0>();                                // the trailing loads
+
+        // ---- the unit's rows out
+        const bool complete = w.complete();
+        const int part = w.part();
+        const float l = across_halves(l_run, add2);
+        bool odd = !(l < __builtin_inff()) || (IDX && least == -__builtin_inff());
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) odd = odd || !(__builtin_fabsf(o[db][v]) < __builtin_inff());
+        const int mine = (bad ? 1 : 0) | (__ballot(on && odd) ? 2 : 0);
+        if (mine && lane == 0) atomicOr(&state, mine);
+        __syncthreads();
+        const int all = state;
+        if (all == 2) {
+            careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, NW, w.c0 * TK, w.c1 * TK, keep,
+                                     [&](int r, float m, float ls, int d, float x, float y) {
+                if (complete) {
+                    const int q = row0 + r;
+                    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                    *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o.p) + (sq.q0 + q / grp) * a.o.st +
+                                                  (kvh * grp + q % grp) * a.o.sh + d) = pack_bf16x2(x * inv, y * inv);
+                } else {
+                    const int64_t prow = (2 * static_cast<int64_t>(wg) + part) * ROWS + r;
+                    if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * prow) = make_float2(m, ls);
+                    *reinterpret_cast<float2 *>(a.part_o + prow * D + d) = make_float2(x, y);
+                }
+            });
+        } else if (on) {
+            const float ls = all & 1 ? __builtin_nanf("") : l;
+            if (complete) {
+                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + tok) * a.o.st + hd * a.o.sh + 4 * lh;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<uint2 *>(op + 32 * db + 8 * q) =
+                            make_uint2(pack_bf16x2(o[db][4 * q] * inv, o[db][4 * q + 1] * inv),
+                                       pack_bf16x2(o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv));
+            } else {
+                const int64_t prow = (2 * static_cast<int64_t>(wg) + part) * ROWS + rr;
+                if (lh == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * prow) = make_float2(m_run, ls);
+                float *po = a.part_o + prow * D + 4 * lh;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<float4 *>(po + 32 * db + 8 * q) =
+                            make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
+            }
+        }
+        if (!complete) {
+            if (tid == 0) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + part] = piece_of(w, n_rows);
+            held |= 1 << part;
+        }
+        w.advance();
+        more = w.x < w.end;
+        // the ring and the state are free for the next unit, no store is on its way
+        wait_vmcnt_le<0>();
+        __syncthreads();
+    }
+    if (tid < 2 && !(held >> tid & 1)) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + tid].n = 0;
+}
+
+// Joins the pieces of the cut units: workgroup i looks at its own two, and of a
+// unit cut over workgroups first .. first + n - 1 takes the rows i - first, + n, ...
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+    using namespace pg;
+    constexpr int LD = D / 4, PW = 256 / LD;               // lanes per row, groups of lanes
+    constexpr int kFew = 8;                                // pieces that one group adds by itself
     __shared__ float4 acc_s[PW][LD];
     __shared__ float2 ml_s[PW];
-    const int H = a.q.n, grp = H / a.kv.Hkv, tid = threadIdx.x;
-    const int64_t total = uniform64(total_work(a, grp, 16 * R));
-    const int64_t run = run_length(total, a.nw);
-    // the unit that a workgroup's first chunk lies in, or the one that its run
-    // ends inside of: the latter also covers the former of the next workgroup,
-    // so a unit that continues is looked at from its first chunk here
+    const int tid = threadIdx.x, pw = tid / LD, l = tid % LD;
+    const int H = a.q.n, grp = H / a.kv.Hkv, wg = static_cast<int>(blockIdx.x);
     for (int part = 0; part < 2; ++part) {
-        const int64_t x = blockIdx.x * run, x_end = min(total, x + run);
-        if (x >= x_end) return;
-        const int64_t at = part == 0 ? x : x_end - 1;
-        int64_t f = 0;
-        const int b = __builtin_amdgcn_readfirstlane(find_seq(a, grp, 16 * R, at, &f));
-        f = uniform64(f);
-        const Seq sq = seq_of(a, b, grp, 16 * R);
-        const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>((at - f) / sq.chunks));
-        const int64_t u0 = f + static_cast<int64_t>(unit) * sq.chunks, u1 = u0 + sq.chunks;
-        if (part == 0 && u0 >= x) continue;                // not a continued unit
-        if (part == 1 && (u0 < x || u1 <= x_end)) continue;    // seen as part 0, or whole
-        const int i0 = static_cast<int>(u0 / run), i1 = static_cast<int>((u1 - 1) / run), n = i1 - i0 + 1;
-        const int kvh = unit / sq.tiles, row0 = unit % sq.tiles * 16 * R;
-        const int n_rows = min(16 * R, sq.n * grp - row0);
-        for (int r = static_cast<int>(blockIdx.x) - i0; r < n_rows; r += n) {
-            const int pw = tid / LD, l = tid % LD;
-            float m = -__builtin_inff(), ls = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int p = pw; p < n; p += PW) {
-                // a piece is its workgroup's first one (continued) unless the unit starts there
-                const int64_t slot = 2 * static_cast<int64_t>(i0 + p) + (u0 >= (i0 + p) * run ? 1 : 0);
-                const int64_t row = slot * (16 * R) + r;
-                const float mp = a.part_ml[2 * row], lp = a.part_ml[2 * row + 1];
+        const PieceOf pc = reinterpret_cast<const PieceOf *>(a.pieces)[2 * wg + part];
+        if (pc.n == 0) continue;
+        // (m, ls, o) += the pieces p0, p0 + step, ... of row r
+        auto add = [&](int r, int p0, int step, float &m, float &ls, float4 &o) __attribute__((always_inline)) {
+            m = -__builtin_inff();
+            ls = 0.f;
+            o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int p = p0; p < pc.n; p += step) {
+                // the unit's first piece is its workgroup's last one, the others begin a run
+                const int64_t row = (2 * static_cast<int64_t>(pc.first + p) + (p == 0 ? 1 : 0)) * ROWS + r;
+                const float2 x = *reinterpret_cast<const float2 *>(a.part_ml + 2 * row);
                 const float4 v = *reinterpret_cast<const float4 *>(a.part_o + row * D + 4 * l);
-                const float mn = fmaxf(m, mp);
+                const float mn = fmaxf(m, x.x);
                 const float a0 = m == -__builtin_inff() ? 0.f : exp_two(m - mn);
-                const float a1 = mp == -__builtin_inff() ? 0.f : exp_two(mp - mn);
-                ls = ls * (ls == ls ? a0 : 1.f) + (lp == lp ? lp * a1 : lp);
+                const float a1 = x.x == -__builtin_inff() ? 0.f : exp_two(x.x - mn);
+                ls = (ls == ls ? ls * a0 : ls) + (x.y == x.y ? x.y * a1 : x.y);
                 o.x = (a0 == 0.f ? 0.f : o.x * a0) + (a1 == 0.f ? 0.f : v.x * a1);
                 o.y = (a0 == 0.f ? 0.f : o.y * a0) + (a1 == 0.f ? 0.f : v.y * a1);
                 o.z = (a0 == 0.f ? 0.f : o.z * a0) + (a1 == 0.f ? 0.f : v.z * a1);
                 o.w = (a0 == 0.f ? 0.f : o.w * a0) + (a1 == 0.f ? 0.f : v.w * a1);
                 m = mn;
             }
+        };
+        auto write = [&](int r, float ls, const float4 o) __attribute__((always_inline)) {
+            const float inv = ls == 0.f ? 0.f : 1.f / ls;
+            const int rho = pc.row0 + r;
+            uint16_t *op = static_cast<uint16_t *>(a.o.p) + (pc.q0 + rho / grp) * a.o.st + (pc.kvh * grp + rho % grp) * a.o.sh + 4 * l;
+            *reinterpret_cast<uint2 *>(op) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        };
+        float m, ls;
+        float4 o;
+        if (pc.n <= kFew) {                                // rows to the groups of lanes in turn
+            for (int r = wg - pc.first + pc.n * pw; r < pc.rows; r += pc.n * PW) {
+                add(r, 0, 1, m, ls, o);
+                write(r, ls, o);
+            }
+            continue;
+        }
+        for (int r = wg - pc.first; r < pc.rows; r += pc.n) {
+            add(r, pw, PW, m, ls, o);
             __syncthreads();
             acc_s[pw][l] = o;
             if (l == 0) ml_s[pw] = make_float2(m, ls);
@@ -616,11 +1229,7 @@ __global__ __launch_bounds__(pg::kThreads) void paged_merge_kernel(PagedArgs a) 
                     t.z += al == 0.f ? 0.f : v.z * al;
                     t.w += al == 0.f ? 0.f : v.w * al;
                 }
-                const float inv = lt == 0.f ? 0.f : 1.f / lt;
-                const int rho = row0 + r;
-                uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + rho / grp) * a.o.st +
-                               (kvh * grp + rho % grp) * a.o.sh + 4 * l;
-                *reinterpret_cast<uint2 *>(op) = make_uint2(pack_bf16x2(t.x * inv, t.y * inv), pack_bf16x2(t.z * inv, t.w * inv));
+                write(r, lt, t);
             }
         }
     }
@@ -628,43 +1237,63 @@ __global__ __launch_bounds__(pg::kThreads) void paged_merge_kernel(PagedArgs a) 
 
 namespace {
 
-// 16-row tiles per wave: as many as an average sequence's query rows fill
-int row_tiles(int64_t T, int64_t B, int64_t grp) {
+// Query rows per workgroup: as many as an average sequence has
+int unit_rows(int64_t T, int64_t B, int64_t grp) {
     const int64_t rows = (T * grp + B - 1) / B;
-    return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
 }
+int workgroups(int rows) { return rows == 16 ? few::kGroups : rowsk::kGroups; }
 
-template <int D, bool MX, int R>
+template <int D, bool MX, int ROWS>
 hipError_t launch(const PagedArgs &a, hipStream_t stream) {
-    if (a.idx) paged_attn_kernel<D, MX, R, true><<<a.nw, pg::kThreads, 0, stream>>>(a);
-    else paged_attn_kernel<D, MX, R, false><<<a.nw, pg::kThreads, 0, stream>>>(a);
+    if constexpr (ROWS == 16) {
+        if (a.idx) paged_few_kernel<D, MX, true><<<a.nw, few::kThreads, 0, stream>>>(a);
+        else paged_few_kernel<D, MX, false><<<a.nw, few::kThreads, 0, stream>>>(a);
+    } else {
+        if (a.idx) paged_rows_kernel<D, MX, ROWS / 32, true><<<a.nw, 2 * ROWS, 0, stream>>>(a);
+        else paged_rows_kernel<D, MX, ROWS / 32, false><<<a.nw, 2 * ROWS, 0, stream>>>(a);
+    }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    paged_merge_kernel<D, R><<<a.nw, pg::kThreads, 0, stream>>>(a);
+    // a page table this narrow holds short units only: none is cut
+    const int64_t keys = static_cast<int64_t>(a.width) << a.kv.lg_page;
+    if (e != hipSuccess || keys <= pg::kShort * (ROWS == 16 ? few::TK : rowsk::TK)) return e;
+    paged_join_kernel<D, ROWS><<<a.nw, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int D, bool MX>
-hipError_t launch_rows(const PagedArgs &a, int R, hipStream_t stream) {
-    if (R == 1) return launch<D, MX, 1>(a, stream);
-    if (R == 2) return launch<D, MX, 2>(a, stream);
-    return launch<D, MX, 4>(a, stream);
+hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
+    if (rows == 16) return launch<D, MX, 16>(a, stream);
+    if (rows == 64) return launch<D, MX, 64>(a, stream);
+    if (rows == 128) return launch<D, MX, 128>(a, stream);
+    return launch<D, MX, 256>(a, stream);
 }
 
 }  // namespace
 
+// whether the line is shorter than 2^31 whatever the lengths (keys: what a page
+// table row can hold)
+bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys) {
+    const int rows = unit_rows(T, B, H / Hkv), tk = rows == 16 ? few::TK : rowsk::TK;
+    const int64_t units = T * H / rows + (T < B ? T : B) * Hkv;      // row tiles: full ones, a last one per sequence
+    return (units + 1) * (keys / tk + 3) < (int64_t(1) << 31) - 1024;
+}
+
+// two pieces per workgroup: what joins them, their maxima and sums, their outputs
 size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D) {
-    const int64_t rows = 2 * pg::kMaxGroups * 16 * row_tiles(T, B, H / Hkv);
-    return static_cast<size_t>(rows) * (D + 2) * sizeof(float);
+    const int rows = unit_rows(T, B, H / Hkv);
+    const size_t n = 2 * static_cast<size_t>(workgroups(rows));
+    return n * (sizeof(pg::PieceOf) + static_cast<size_t>(rows) * (D + 2) * sizeof(float));
 }
 
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream) {
-    const int R = row_tiles(a.T, a.B, a.q.n / a.kv.Hkv);
-    a.nw = pg::kMaxGroups;
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = a.part_o + static_cast<int64_t>(2 * pg::kMaxGroups * 16 * R) * D;
-    if (a.kv.mx) return D == 128 ? launch_rows<128, true>(a, R, stream) : launch_rows<64, true>(a, R, stream);
-    return D == 128 ? launch_rows<128, false>(a, R, stream) : launch_rows<64, false>(a, R, stream);
+    const int rows = unit_rows(a.T, a.B, a.q.n / a.kv.Hkv);
+    a.nw = workgroups(rows);
+    a.pieces = workspace;
+    a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * a.nw * sizeof(pg::PieceOf));
+    a.part_ml = a.part_o + static_cast<int64_t>(2 * a.nw) * rows * D;
+    if (a.kv.mx) return D == 128 ? launch_rows<128, true>(a, rows, stream) : launch_rows<64, true>(a, rows, stream);
+    return D == 128 ? launch_rows<128, false>(a, rows, stream) : launch_rows<64, false>(a, rows, stream);
 }
 
 }  // namespace rmm

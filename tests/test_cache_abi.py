@@ -164,6 +164,8 @@ def test_binding_refusals():
     Q = torch.zeros(1, 3, 4, 64, dtype=bf)
     with pytest.raises(ValueError, match="GPU"):
         rmm.rmm_qk_norm_rope(Q, Q.transpose(1, 2))
+    with pytest.raises(ValueError, match="positions"):
+        rmm._positions(object(), None, 3)
     with pytest.raises(ValueError):
         rmm.rmm_qk_norm_rope(Q, Q)
     with pytest.raises(ValueError):
