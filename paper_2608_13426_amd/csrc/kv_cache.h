@@ -54,7 +54,7 @@ struct PagedArgs {
     int causal;
     void *pieces;                          // what joins the pieces of cut units
     float *part_o, *part_ml;               // their outputs, their (max, sum)
-    int nw;                                // workgroups
+    int nw, whole;                         // workgroups; whether no unit is cut
 };
 bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys);
 size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D);

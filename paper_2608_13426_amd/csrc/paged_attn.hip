@@ -6,18 +6,20 @@
 // A query row is one (new token, query head of a kv head): the heads of a group
 // share every key read.  A unit is one (sequence, kv head, tile of query rows).
 //
-//   up to 16 rows (a decode step): paged_few_kernel, 16-row tiles.  The four waves
-//   of a workgroup take 32-key chunks in turn; keys and values go from memory to
-//   registers to the matrix cores without LDS.  Bound by reading the cache.
-//   more rows (drafted tokens, prompt chunks): paged_rows_kernel, 32 rows per wave,
-//   64-key tiles staged once per workgroup in an LDS ring.
+//   up to 64 rows (a decode step, a few drafted tokens): paged_few_kernel, 16, 32
+//   or 64 rows.  The four waves of a workgroup take 32-key chunks in turn; keys and
+//   values go from memory to registers to the matrix cores without LDS.  Bound by
+//   reading the cache.
+//   more rows (prompt chunks): paged_rows_kernel, 32 rows per wave, 64-key tiles
+//   staged once per workgroup in an LDS ring.
 //
 // Lengths are known on the device only, and a batch may hold one long sequence
 // among short ones, so the work is cut there: the key blocks of all units lie on
 // one line, which is cut into equal runs, one per workgroup.  A unit inside one
 // run is written at once; the pieces of a cut one go to the workspace as (maximum,
-// sum, unnormalised output) and a second launch joins them in order.  Where every
-// unit is short (kShort blocks) the line is cut between units instead.
+// sum, unnormalised output) and a second launch joins them in order.  Where whole
+// units spread over the workgroups as well, but for less than what the pieces cost,
+// the line is cut between units instead.
 //
 // With the causal mask a unit ends at the last key that any of its rows sees.
 // Row tiles are laid on the line in pairs of one early and one late tile, which
@@ -35,7 +37,9 @@ namespace {
 
 namespace pg {
 constexpr float kTau = 8.f;               // lazy-rescale threshold, log2 units
-constexpr int kShort = 16;                // units of at most this many blocks are not cut
+// Units of at most kShort blocks, no more of them than workgroups, are never cut
+// (the host then leaves out the joining launch: 5 us of a 12 us call).
+constexpr int kShort = 16;
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
 template <typename F>
@@ -156,25 +160,30 @@ struct Plan {
     __device__ __forceinline__ int blocks(const Seq &s, int tile) const {
         return max((keys(s, last_token(s, tile)) + TK - 1) / TK, 1);
     }
-    __device__ __forceinline__ int weight(const Seq &s, int tile) const { return whole ? 1 : blocks(s, tile); }
     // length on the line of a pair of tiles (p, 2 np - 1 - p)
     __device__ __forceinline__ int pair(const Seq &s, int np) const {
-        if (whole) return 2;
         if (np == 1 || !causal) return blocks(s, 0) + blocks(s, 2 * np - 1);
         const int tok = static_cast<int>((static_cast<uint32_t>(np) * 2 * ROWS - 1) / static_cast<uint32_t>(grp));    // of a full last tile
         const int k = min(max(s.len - s.n + tok + 1, 1), s.len + ROWS);
         return blocks(s, 0) + (k + TK - 1) / TK + 2;
     }
+    __device__ __forceinline__ int units(const Seq &s) const { return tiles(s) * Hkv; }
     // a sequence's share of the line per kv head
     __device__ __forceinline__ int head_work(const Seq &s) const {
         const int t = tiles(s), np = t >> 1;
+        if (whole) return t;
         int w = np > 0 ? np * pair(s, np) : 0;
-        if (t & 1) w += weight(s, t - 1);
+        if (t & 1) w += blocks(s, t - 1);
         return w;
     }
     __device__ __forceinline__ int work(const Seq &s) const { return head_work(s) * Hkv; }
     __device__ __forceinline__ int longest(const Seq &s) const {
         return s.n > 0 ? blocks(s, tiles(s) - 1) : 0;
+    }
+    // of two units that are neighbours when none is cut
+    __device__ __forceinline__ int longest_pair(const Seq &s) const {
+        const int t = tiles(s);
+        return t > 1 ? blocks(s, 0) + blocks(s, t - 1) : 2 * longest(s);
     }
 };
 
@@ -182,6 +191,7 @@ struct Plan {
 template <int TK, int ROWS>
 struct Walk {
     Plan<TK, ROWS> pl;
+    int wg;                               // the workgroup's place among the runs
     int x, begin, end, run;               // position, the workgroup's run, run length
     int b, f;                             // the sequence at x, where it begins
     Seq s;
@@ -190,28 +200,50 @@ struct Walk {
     int u0, u1;                           // its place on the line
 
     // false: no work for this workgroup
-    __device__ __forceinline__ bool init(const PagedArgs &a, int wg, int min_run) {
+    // min_run: shortest run; cut_cost: what cutting units costs, in blocks
+    __device__ __forceinline__ bool init(const PagedArgs &a, int min_run, int cut_cost) {
         const int lane = threadIdx.x & 63;
         pl.grp = a.q.n / a.kv.Hkv;
         pl.causal = a.causal;
         pl.Hkv = a.kv.Hkv;
-        // whether all units are short, then the line's length: lane l looks at
-        // sequences l, l + 64, ...
+        pl.whole = false;
+        // the line's length in blocks and in units, the longest unit: lane l looks
+        // at sequences l, l + 64, ...
         Seq mine = {0, 0, 0, 0};
         if (lane < a.B) mine = pl.load(a, lane);
-        int most = pl.longest(mine);
-        for (int i = lane + 64; i < a.B; i += 64) most = max(most, pl.longest(pl.load(a, i)));
-        pl.whole = __ballot(most > kShort) == 0;
-        const int w0 = pl.work(mine), sum0 = prefix_sum(w0);
-        int rest = 0;
-        for (int i = lane + 64; i < a.B; i += 64) rest += pl.work(pl.load(a, i));
+        int most = pl.longest(mine), most2 = pl.longest_pair(mine);
+        int w0 = pl.work(mine), blocks = w0, units = pl.units(mine);
+        for (int i = lane + 64; i < a.B; i += 64) {
+            const Seq q = pl.load(a, i);
+            most = max(most, pl.longest(q));
+            most2 = max(most2, pl.longest_pair(q));
+            blocks += pl.work(q);
+            units += pl.units(q);
+        }
+        int sum0 = prefix_sum(blocks);
         int total = __builtin_amdgcn_readlane(sum0, 63);
-        if (a.B > 64) total += __builtin_amdgcn_readlane(prefix_sum(rest), 63);
+        if (a.whole) {
+            pl.whole = true;
+        } else {
+            const int nu = __builtin_amdgcn_readlane(prefix_sum(units), 63);
+            const int rounds = quot(nu + a.nw - 1, a.nw), room = quot(total, a.nw) + cut_cost;
+            pl.whole = __ballot((rounds >> 1) * most2 + (rounds & 1) * most > room) == 0;
+        }
+        if (pl.whole) {
+            w0 = pl.units(mine);
+            sum0 = prefix_sum(units);
+            total = __builtin_amdgcn_readlane(sum0, 63);
+        }
+        if (a.B > 64) sum0 = prefix_sum(w0);
         run = quot(total + a.nw - 1, a.nw);
         run = pl.whole ? max(run, 1) : (max(run, min_run) + 3) / 4 * 4;
-        const int64_t at = static_cast<int64_t>(wg) * run;
-        if (at >= total) return false;
-        begin = x = static_cast<int>(at);
+        // consecutive runs on one XCD (workgroups are dealt to the 8 XCDs in turn),
+        // where units that share keys share its L2, the XCDs evenly used
+        const int i0 = static_cast<int>(blockIdx.x), runs = quot(total + run - 1, run), per = (runs + 7) >> 3;
+        wg = i0;                          // idle workgroups keep the places behind the runs
+        if ((i0 >> 3) < per) wg = (i0 & 7) * per + (i0 >> 3);
+        if ((i0 >> 3) >= per || wg >= runs) return false;
+        begin = x = wg * run;
         end = min(total - x, run) + x;
         // the sequence at x
         int base = 0;
@@ -249,6 +281,14 @@ struct Walk {
         }
         kvh = quot(x - f, hw);
         const int y = x - f - kvh * hw;
+        if (pl.whole) {                   // one place per unit, late and early tiles in turn
+            tile = y & 1 ? y >> 1 : hw - 1 - (y >> 1);
+            u0 = x;
+            u1 = x + 1;
+            c0 = 0;
+            c1 = pl.blocks(s, tile);
+            return true;
+        }
         const int t = pl.tiles(s), np = t >> 1;
         const int pr = np > 0 ? pl.pair(s, np) : 0;
         int off;
@@ -256,10 +296,10 @@ struct Walk {
             const int p = quot(y, pr);
             off = y - p * pr;
             tile = p;
-            const int wa = pl.weight(s, p);
+            const int wa = pl.blocks(s, p);
             if (off >= wa) {
                 tile = 2 * np - 1 - p;
-                const int wb = pl.weight(s, tile);
+                const int wb = pl.blocks(s, tile);
                 if (off >= wa + wb) {     // the rest of the pair's length is empty
                     x += pr - off;
                     return false;
@@ -271,9 +311,9 @@ struct Walk {
             off = y - np * pr;
         }
         u0 = x - off;
-        u1 = u0 + pl.weight(s, tile);
-        c0 = pl.whole ? 0 : off;
-        c1 = pl.whole ? pl.blocks(s, tile) : min(end, u1) - u0;
+        u1 = u0 + pl.blocks(s, tile);
+        c0 = off;
+        c1 = min(end, u1) - u0;
         return true;
     }
     __device__ __forceinline__ void advance() { x = min(end, u1); }
@@ -384,13 +424,6 @@ __device__ __forceinline__ void read_lists(const PagedArgs &a, const Seq &sq, in
     }
 }
 
-// Consecutive runs of the line on one XCD (workgroups are dealt to the 8 XCDs
-// in turn), where units that share keys share its L2
-__device__ __forceinline__ int line_index(int nw) {
-    const int i = static_cast<int>(blockIdx.x);
-    return i % 8 * (nw / 8) + i / 8;
-}
-
 template <int N>
 __device__ __forceinline__ void wait_vmcnt_le() {
     static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -400,9 +433,10 @@ __device__ __forceinline__ void wait_vmcnt_le() {
 
 // ------------------------------------------------------------- few rows
 namespace few {
-constexpr int kWaves = 4, kThreads = 64 * kWaves, TK = 32, ROWS = 16;
+constexpr int kWaves = 4, kThreads = 64 * kWaves, TK = 32;
 constexpr int kGroups = 512;              // workgroups: two per CU
 constexpr int kMinRun = 8;                // chunks: two rounds of the four waves
+constexpr int kCutCost = 8;
 }  // namespace few
 
 }  // namespace
@@ -413,29 +447,33 @@ constexpr int kMinRun = 8;                // chunks: two rounds of the four wave
 // its lane group contributes to O^T = V^T P^T: the weights stay where they are.
 // The value rows, loaded as rows, are turned 8 x 8 in registers (v_perm).  4-bit
 // codes become bf16 with v_cvt_scalef32_pk_bf16_fp4 (exact, the scale included).
-// MX: 4-bit cache; IDX: scores over retained dims
-template <int D, bool MX, bool IDX>
+// R: 16-row tiles, which share each key and value fragment (their queries are then
+// kept in LDS); MX: 4-bit cache; IDX: scores over retained dims
+template <int D, bool MX, int R, bool IDX>
 __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a) {
     using namespace pg;
     using namespace few;
+    constexpr int ROWS = 16 * R;
     constexpr int KS = D / 32, DM = D / 16;               // contraction steps of S^T, MFMA rows of O^T
     constexpr int ROWB = MX ? D / 2 : D * 2, SROWB = D / 32;    // bytes per cached row, scale bytes per row
     constexpr int OLD = D + 4;                            // row stride of the joining buffer, floats
+    constexpr int NBUF = MX && R == 1 ? 2 : 1;            // chunks held
     __shared__ __attribute__((aligned(16))) float oj[kWaves][16][OLD];
     __shared__ float ml[kWaves][16][2];
     __shared__ int state[kWaves];                         // bit 0: a page or length out of range, bit 1: to be redone
-    __shared__ uint32_t keep[IDX ? 16 : 1][KS];
+    __shared__ uint32_t keep[IDX ? ROWS : 1][KS];
+    __shared__ uint4 qs[R > 1 ? R : 1][KS][R > 1 ? 64 : 1];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int H = a.q.n, grp = H / a.kv.Hkv;
     const int lg = a.kv.lg_page, ps = 1 << lg;
-    const int wg = line_index(a.nw);
 
     int held = 0;                                          // which of the two pieces there are
     Walk<TK, ROWS> w;
-    bool more = w.init(a, wg, kMinRun);
+    bool more = w.init(a, kMinRun, kCutCost);
+    const int wg = w.wg;
     while (more) {
         if (!w.locate(a)) {
             more = w.x < w.end;
@@ -446,37 +484,50 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 
         // ---- the unit's query rows
         if constexpr (IDX) {
-            for (int i = tid; i < 16 * KS; i += kThreads) (&keep[0][0])[i] = 0;
+            for (int i = tid; i < ROWS * KS; i += kThreads) (&keep[0][0])[i] = 0;
             __syncthreads();
             read_lists<D, kThreads>(a, sq, kvh, row0, n_rows, keep);
             __syncthreads();
         }
         // dims that lane (col, g) holds at contraction step s
         auto dim_of = [&](int s) { return MX ? (D / 4) * g + 8 * s : 32 * s + 8 * g; };
-        const bool on = col < n_rows;
-        const int rho = row0 + col, tok = on ? rho / grp : 0;
-        uint4 qf[KS];
-        {
-            const int hd = on ? kvh * grp + rho % grp : 0;
-            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
+        auto query = [&](int r, int s) __attribute__((always_inline)) {
+            const int rr = 16 * r + col;
+            if (rr >= n_rows) return make_uint4(0, 0, 0, 0);
+            const int rho = row0 + rr, tok = rho / grp;
+            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + (kvh * grp + rho - tok * grp) * a.q.sh;
+            uint4 x = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
+            if constexpr (IDX) x = keep8(x, keep[rr][dim_of(s) >> 5] >> (dim_of(s) & 31));
+            return x;
+        };
+        uint4 qf[R > 1 ? 1 : KS];
+        if constexpr (R == 1) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                qf[s] = make_uint4(0, 0, 0, 0);
-                if (on) qf[s] = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
-                if constexpr (IDX) qf[s] = keep8(qf[s], keep[col][dim_of(s) >> 5] >> (dim_of(s) & 31));
-            }
+            for (int s = 0; s < KS; ++s) qf[s] = query(0, s);
+        } else {
+            for (int i = wave; i < R * KS; i += kWaves) qs[i / KS][i % KS][lane] = query(i / KS, i % KS);
+            __syncthreads();
         }
-        // last key of the lane's row; the first limit and the last of the unit's rows
-        const int lim = !on ? -1 : a.causal ? sq.len - sq.n + tok : sq.len - 1;
-        const int tok_a = row0 / grp, tok_b = (row0 + n_rows - 1) / grp;
-        const int lo_lim = a.causal ? sq.len - sq.n + tok_a : sq.len - 1;
-        const int hi_lim = a.causal ? sq.len - sq.n + tok_b : sq.len - 1;
+        // last key of the lane's rows; the first limit and the last of the unit's rows
+        int lim[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int rr = 16 * r + col;
+            lim[r] = rr >= n_rows ? -1 : a.causal ? sq.len - sq.n + (row0 + rr) / grp : sq.len - 1;
+        }
+        const int lo_lim = a.causal ? sq.len - sq.n + quot(row0, grp) : sq.len - 1;
+        const int hi_lim = a.causal ? sq.len - sq.n + quot(row0 + n_rows - 1, grp) : sq.len - 1;
         const int c_stop = min(w.c1, hi_lim < 0 ? 0 : hi_lim / TK + 1);
 
-        f32x4_t o[DM];
-        float m_run = -__builtin_inff(), l_run = 0.f, least = 0.f;
+        f32x4_t o[R][DM];
+        float m_run[R], l_run[R], least = 0.f;
 #pragma unroll
-        for (int i = 0; i < DM; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < R; ++r) {
+            m_run[r] = -__builtin_inff();
+            l_run[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DM; ++i) o[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
         bool bad = sq.bad;
 
         // ---- the wave's chunks c0 + wave, + 4, ...; lane l holds the pages of the
@@ -505,9 +556,11 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             const uint8_t *rb = base + pb * page_bytes + (hrow + ob) * row_bytes;
             return (second ? rb : ra) + row * row_bytes;
         };
-        uint4 kraw[2][MX ? 1 : KS], vraw[MX ? 1 : 8], vsraw[MX ? 2 : 1];
-        uint32_t ksraw[2], vcraw[8];
-        auto load_k = [&](int c, int nth) __attribute__((always_inline)) {
+        struct Raw {
+            uint4 k[2][MX ? 1 : KS], v[MX ? 1 : 8], vs[MX ? 2 : 1];
+            uint32_t ks[2], vc[8];
+        };
+        auto load_k = [&](Raw &x, int c, int nth) __attribute__((always_inline)) {
             const int krow = 8 * (col >> 2) + (col & 3);
             const uint8_t *kp = row_at(a.kv.k, a.kv.k_page, ROWB, c, nth, col >= 8, krow);
             if constexpr (!MX) {
@@ -515,189 +568,205 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                     for (int s = 0; s < KS; ++s)
-                        kraw[tb][s] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 64 * s + 16 * g);
+                        x.k[tb][s] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 64 * s + 16 * g);
             } else {
                 const uint8_t *sp = row_at(a.kv.ks, a.kv.ks_page, SROWB, c, nth, col >= 8, krow);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     if constexpr (D == 128) {
-                        kraw[tb][0] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 16 * g);
-                        ksraw[tb] = sp[tb * 4 * SROWB + g];
+                        x.k[tb][0] = *reinterpret_cast<const uint4 *>(kp + tb * 4 * ROWB + 16 * g);
+                        x.ks[tb] = sp[tb * 4 * SROWB + g];
                     } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(kp + tb * 4 * ROWB + 8 * g);
-                        kraw[tb][0] = make_uint4(x.x, x.y, 0, 0);
-                        ksraw[tb] = sp[tb * 4 * SROWB + (g >> 1)];
+                        const uint2 y = *reinterpret_cast<const uint2 *>(kp + tb * 4 * ROWB + 8 * g);
+                        x.k[tb][0] = make_uint4(y.x, y.y, 0, 0);
+                        x.ks[tb] = sp[tb * 4 * SROWB + (g >> 1)];
                     }
                 }
             }
         };
-        auto load_v = [&](int c, int nth) __attribute__((always_inline)) {
+        auto load_v = [&](Raw &x, int c, int nth) __attribute__((always_inline)) {
             const uint8_t *vp = row_at(a.kv.v, a.kv.v_page, ROWB, c, nth, g >= 2, 8 * g);
             if constexpr (!MX) {
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
                     if constexpr (D == 128) {
-                        vraw[kk] = *reinterpret_cast<const uint4 *>(vp + kk * ROWB + 16 * col);
+                        x.v[kk] = *reinterpret_cast<const uint4 *>(vp + kk * ROWB + 16 * col);
                     } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(vp + kk * ROWB + 8 * col);
-                        vraw[kk] = make_uint4(x.x, x.y, 0, 0);
+                        const uint2 y = *reinterpret_cast<const uint2 *>(vp + kk * ROWB + 8 * col);
+                        x.v[kk] = make_uint4(y.x, y.y, 0, 0);
                     }
                 }
             } else {
                 const uint8_t *sp = row_at(a.kv.vs, a.kv.vs_page, SROWB, c, nth, g >= 2, 8 * g);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
-                    if constexpr (D == 128) vcraw[kk] = *reinterpret_cast<const uint32_t *>(vp + kk * ROWB + 4 * col);
-                    else vcraw[kk] = *reinterpret_cast<const uint16_t *>(vp + kk * ROWB + 2 * col);
+                    if constexpr (D == 128) x.vc[kk] = *reinterpret_cast<const uint32_t *>(vp + kk * ROWB + 4 * col);
+                    else x.vc[kk] = *reinterpret_cast<const uint16_t *>(vp + kk * ROWB + 2 * col);
                 }
-                vsraw[0] = reinterpret_cast<const uint4 *>(sp)[0];
-                if constexpr (D == 128) vsraw[MX ? 1 : 0] = reinterpret_cast<const uint4 *>(sp)[1];
+                x.vs[0] = reinterpret_cast<const uint4 *>(sp)[0];
+                if constexpr (D == 128) x.vs[MX ? 1 : 0] = reinterpret_cast<const uint4 *>(sp)[1];
             }
         };
 
-        // scores of chunk c, then the next chunk's keys are asked for
-        auto chunk = [&](int c, int nth, bool next) __attribute__((always_inline)) {
+        // chunk c, held in x; the keys and then the values of the chunk that takes its
+        // place are asked for as soon as its own are used up
+        auto chunk = [&](Raw &x, int c, int nth, bool next) __attribute__((always_inline)) {
             const int key = c * TK;
             const bool edge = key + TK - 1 > lo_lim;       // wave-uniform: some row does not see every key
-            f32x4_t sc[2];
-            {
-                uint4 kf[2][KS];
+            uint4 kf[2][KS];
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    const uint32_t cw[4] = {kraw[tb][0].x, kraw[tb][0].y, kraw[tb][0].z, kraw[tb][0].w};
+            for (int tb = 0; tb < 2; ++tb) {
+                const uint32_t cw[4] = {x.k[tb][0].x, x.k[tb][0].y, x.k[tb][0].z, x.k[tb][0].w};
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        if constexpr (MX) kf[tb][s] = unpack_mx8(cw[s], __uint_as_float(ksraw[tb] << 23));
-                        else kf[tb][s] = kraw[tb][s];
-                    }
+                for (int s = 0; s < KS; ++s) {
+                    if constexpr (MX) kf[tb][s] = unpack_mx8(cw[s], __uint_as_float(x.ks[tb] << 23));
+                    else kf[tb][s] = x.k[tb][s];
                 }
+            }
+            uint4 pf[R];
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    sc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < R; ++r) {
+                f32x4_t sc[2];
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) sc[tb] = mfma(kf[tb][s], qf[s], sc[tb]);
+                for (int tb = 0; tb < 2; ++tb) sc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    uint4 q;
+                    if constexpr (R == 1) q = qf[s];
+                    else q = qs[r][s][lane];
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) sc[tb] = mfma(kf[tb][s], q, sc[tb]);
                 }
+                // the next keys as soon as these are used up
+                if (r == R - 1 && next) load_k(x, c + kWaves * NBUF, nth + NBUF);
                 if constexpr (IDX) {
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) least = fminf(least, sc[tb][i]);
                 }
-            }
-            if (next) load_k(c + kWaves, nth + 1);
-            // ---- weights
-            float p[2][4], mx = -__builtin_inff();
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[tb][i] = sc[tb][i] * a.c;
-            if (edge) {
+                // ---- weights
+                float p[2][4], mx = -__builtin_inff();
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key + 8 * g + 4 * tb + i > lim) p[tb][i] = -__builtin_inff();
-            }
+                    for (int i = 0; i < 4; ++i) p[tb][i] = sc[tb][i] * a.c;
+                if (edge) {
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
+                    for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tb][i]);
-            mx = across_rows(mx, fmax2);
-            if (__ballot(mx > m_run + kTau)) {
-                const float m_new = fmaxf(m_run, mx);
-                const float al = m_new == -__builtin_inff() ? 1.f : exp_two(m_run - m_new);
-                l_run *= al;
-#pragma unroll
-                for (int i = 0; i < DM; ++i) o[i] *= al;
-                m_run = m_new;
-            }
-            // a row with nothing kept yet has only masked (-inf) scores here
-            const float m_use = m_run == -__builtin_inff() ? 0.f : m_run;
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[tb][i] = exp_two(p[tb][i] - m_use);
-                    l_run += p[tb][i];
+                        for (int i = 0; i < 4; ++i)
+                            if (key + 8 * g + 4 * tb + i > lim[r]) p[tb][i] = -__builtin_inff();
                 }
-            const uint4 pf = make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
-                                        pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3]));
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tb][i]);
+                mx = across_rows(mx, fmax2);
+                if (__ballot(mx > m_run[r] + kTau)) {
+                    const float m_new = fmaxf(m_run[r], mx);
+                    const float al = m_new == -__builtin_inff() ? 1.f : exp_two(m_run[r] - m_new);
+                    l_run[r] *= al;
+#pragma unroll
+                    for (int i = 0; i < DM; ++i) o[r][i] *= al;
+                    m_run[r] = m_new;
+                }
+                // a row with nothing kept yet has only masked (-inf) scores here
+                const float m_use = m_run[r] == -__builtin_inff() ? 0.f : m_run[r];
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[tb][i] = exp_two(p[tb][i] - m_use);
+                        l_run[r] += p[tb][i];
+                    }
+                pf[r] = make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
+                                   pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3]));
+                // one row tile after the other: their scores together do not fit the registers
+                if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
+            }
             // ---- O^T += V^T P^T: dim DM * col + i of the value rows at MFMA i
             uint32_t vr[8][DM / 2];
             if constexpr (!MX) {
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
-                    const uint32_t x[4] = {vraw[kk].x, vraw[kk].y, vraw[kk].z, vraw[kk].w};
+                    const uint32_t y[4] = {x.v[kk].x, x.v[kk].y, x.v[kk].z, x.v[kk].w};
 #pragma unroll
-                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = x[q];
+                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = y[q];
                 }
             } else {
-                const uint32_t sw[8] = {vsraw[0].x, vsraw[0].y, vsraw[0].z, vsraw[0].w,
-                                        vsraw[MX ? 1 : 0].x, vsraw[MX ? 1 : 0].y, vsraw[MX ? 1 : 0].z, vsraw[MX ? 1 : 0].w};
+                const uint4 s2 = x.vs[MX ? 1 : 0];
+                const uint32_t sw[8] = {x.vs[0].x, x.vs[0].y, x.vs[0].z, x.vs[0].w, s2.x, s2.y, s2.z, s2.w};
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
                     // D = 128: four scale bytes per row; D = 64: two
                     const uint32_t sb = D == 128 ? (sw[kk] >> (8 * (col >> 2))) & 0xffu
                                                  : (sw[kk >> 1] >> (16 * (kk & 1) + 8 * (col >> 3))) & 0xffu;
-                    const uint4 x = unpack_mx8(vcraw[kk], __uint_as_float(sb << 23));
-                    vr[kk][0] = x.x;
-                    vr[kk][1] = x.y;
+                    const uint4 y = unpack_mx8(x.vc[kk], __uint_as_float(sb << 23));
+                    vr[kk][0] = y.x;
+                    vr[kk][1] = y.y;
                     if constexpr (D == 128) {
-                        vr[kk][2] = x.z;
-                        vr[kk][3] = x.w;
+                        vr[kk][2] = y.z;
+                        vr[kk][3] = y.w;
                     }
                 }
             }
-            auto value_frag = [&](const uint32_t(&v)[8][DM / 2], int i) __attribute__((always_inline)) {
-                const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-                return make_uint4(__builtin_amdgcn_perm(v[1][i >> 1], v[0][i >> 1], sel),
-                                  __builtin_amdgcn_perm(v[3][i >> 1], v[2][i >> 1], sel),
-                                  __builtin_amdgcn_perm(v[5][i >> 1], v[4][i >> 1], sel),
-                                  __builtin_amdgcn_perm(v[7][i >> 1], v[6][i >> 1], sel));
-            };
-            if (edge) {                                    // nothing of what lies past the last key seen
-                const uint32_t m = (1u << min(max(hi_lim + 1 - key - 8 * g, 0), 8)) - 1;
+            // a weight of zero does not silence what lies past the last key that some row sees
+            if (key + TK - 1 > hi_lim) {
 #pragma unroll
-                for (int i = 0; i < DM; ++i) o[i] = mfma(keep8(value_frag(vr, i), m), pf, o[i]);
-            } else {
+                for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-                for (int i = 0; i < DM; ++i) o[i] = mfma(value_frag(vr, i), pf, o[i]);
+                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = key + 8 * g + kk <= hi_lim ? vr[kk][q] : 0u;
+                asm volatile("" ::: "memory");             // a branch of its own: rarely taken
             }
-            if (next) load_v(c + kWaves, nth + 1);
+#pragma unroll
+            for (int i = 0; i < DM; ++i) {
+                const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
+                const uint4 f = make_uint4(__builtin_amdgcn_perm(vr[1][i >> 1], vr[0][i >> 1], sel),
+                                           __builtin_amdgcn_perm(vr[3][i >> 1], vr[2][i >> 1], sel),
+                                           __builtin_amdgcn_perm(vr[5][i >> 1], vr[4][i >> 1], sel),
+                                           __builtin_amdgcn_perm(vr[7][i >> 1], vr[6][i >> 1], sel));
+#pragma unroll
+                for (int r = 0; r < R; ++r) o[r][i] = mfma(f, pf[r], o[r][i]);
+            }
+            if (next) load_v(x, c + kWaves * NBUF, nth + NBUF);
         };
+        Raw raw[NBUF];
         for (int c = w.c0 + wave; c < c_stop;) {           // up to 64 chunks per fetch of page numbers
             fetch_pages(c);
             const int n = min(64, (c_stop - c + kWaves - 1) / kWaves);
-            load_k(c, 0);
-            load_v(c, 0);
-            for (int i = 0; i < n; ++i) chunk(c + kWaves * i, i, i + 1 < n);
+            load_k(raw[0], c, 0);
+            load_v(raw[0], c, 0);
+            if constexpr (NBUF == 2) {
+                if (n > 1) {
+                    load_k(raw[NBUF - 1], c + kWaves, 1);
+                    load_v(raw[NBUF - 1], c + kWaves, 1);
+                }
+            }
+            for (int i = 0; i < n; i += NBUF) {
+                chunk(raw[0], c + kWaves * i, i, i + NBUF < n);
+                if constexpr (NBUF == 2) {
+                    if (i + 1 < n) chunk(raw[NBUF - 1], c + kWaves * (i + 1), i + 1, i + 3 < n);
+                }
+            }
             c += kWaves * n;
         }
 
-        // ---- the four waves join
+        // ---- the four waves join, 16 rows at a time
         const bool complete = w.complete();
         const int part = w.part();
-        const float l = across_rows(l_run, add2);
-        bool odd = !(l < __builtin_inff()) || (IDX && least == -__builtin_inff());
+        bool odd = IDX && least == -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < DM; ++i)
+        for (int r = 0; r < R; ++r) {
+            l_run[r] = across_rows(l_run[r], add2);
+            bool fin = l_run[r] < __builtin_inff();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd = odd || !(__builtin_fabsf(o[i][e]) < __builtin_inff());
-        const bool redo = __ballot(on && odd) != 0;
-        __syncthreads();
-        if (lane == 0) state[wave] = bad ? 1 : redo ? 2 : 0;
-        if (g == 0) {
-            ml[wave][col][0] = m_run;
-            ml[wave][col][1] = l;
+            for (int i = 0; i < DM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) fin = fin && __builtin_fabsf(o[r][i][e]) < __builtin_inff();
+            odd = odd || (!fin && 16 * r + col < n_rows);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < DM; i += 4)
-                *reinterpret_cast<float4 *>(&oj[wave][col][DM * (4 * g + e) + i]) =
-                    make_float4(o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]);
-        __syncthreads();
-        const int all = state[0] | state[1] | state[2] | state[3];
+        const int mine = (bad ? 1 : 0) | (__ballot(odd) ? 2 : 0);
         // row r of the unit: N dims from d on
         auto put = [&](int r, float m, float ls, int d, const auto &acc) __attribute__((always_inline)) {
             constexpr int N = sizeof(acc) / sizeof(float);
@@ -705,12 +774,12 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                 const int q = row0 + r;
                 const float inv = ls == 0.f ? 0.f : 1.f / ls;
                 uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + q / grp) * a.o.st + (kvh * grp + q % grp) * a.o.sh + d;
-                uint32_t x[N / 2];
+                uint32_t y[N / 2];
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) x[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-                if constexpr (N == 8) *reinterpret_cast<uint4 *>(op) = make_uint4(x[0], x[1], x[2], x[3]);
-                else if constexpr (N == 4) *reinterpret_cast<uint2 *>(op) = make_uint2(x[0], x[1]);
-                else *reinterpret_cast<uint32_t *>(op) = x[0];
+                for (int i = 0; i < N / 2; ++i) y[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+                if constexpr (N == 8) *reinterpret_cast<uint4 *>(op) = make_uint4(y[0], y[1], y[2], y[3]);
+                else if constexpr (N == 4) *reinterpret_cast<uint2 *>(op) = make_uint2(y[0], y[1]);
+                else *reinterpret_cast<uint32_t *>(op) = y[0];
             } else {
                 const int64_t prow = (2 * static_cast<int64_t>(wg) + part) * ROWS + r;
                 if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * prow) = make_float2(m, ls);
@@ -722,15 +791,25 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                 }
             }
         };
-        if (all == 2) {
-            careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, kWaves, w.c0 * TK, w.c1 * TK, keep,
-                                     [&](int r, float m, float ls, int d, float x, float y) {
-                                         const float acc[2] = {x, y};
-                                         put(r, m, ls, d, acc);
-                                     });
-        } else {
+        int all = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            __syncthreads();
+            if (r == 0 && lane == 0) state[wave] = mine;
+            if (g == 0) {
+                ml[wave][col][0] = m_run[r];
+                ml[wave][col][1] = l_run[r];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < DM; i += 4)
+                    *reinterpret_cast<float4 *>(&oj[wave][col][DM * (4 * g + e) + i]) =
+                        make_float4(o[r][i][e], o[r][i + 1][e], o[r][i + 2][e], o[r][i + 3][e]);
+            __syncthreads();
+            if (r == 0) all = state[0] | state[1] | state[2] | state[3];
             const int rr = tid >> 4, d0 = (tid & 15) * DM;
-            if (rr < n_rows) {
+            if (all != 2 && 16 * r + rr < n_rows) {
                 float m = -__builtin_inff(), ls = 0.f, acc[DM];
 #pragma unroll
                 for (int v = 0; v < kWaves; ++v) m = fmaxf(m, ml[v][rr][0]);
@@ -743,38 +822,45 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 #pragma unroll
                     for (int i = 0; i < DM; ++i) acc[i] += al * oj[v][rr][d0 + i];
                 }
-                put(rr, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
+                put(16 * r + rr, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
             }
         }
+        if (all == 2)
+            careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, kWaves, w.c0 * TK, w.c1 * TK, keep,
+                                     [&](int r, float m, float ls, int d, float y, float z) {
+                                         const float acc[2] = {y, z};
+                                         put(r, m, ls, d, acc);
+                                     });
         if (!complete) {
             if (tid == 0) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + part] = piece_of(w, n_rows);
             held |= 1 << part;
         }
         w.advance();
         more = w.x < w.end;
+        if constexpr (IDX || R > 1) __syncthreads();       // the lists and queries are free for the next unit
     }
     if (tid < 2 && !(held >> tid & 1)) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + tid].n = 0;
 }
 
 // ------------------------------------------------------------ many rows
 namespace rowsk {
-constexpr int TK = 64, NS = 4;            // keys per tile, ring slots
+constexpr int NW = 8, NT = 64 * NW;       // waves of 32 query rows
+constexpr int ROWS = 32 * NW, TK = 64, NS = 4;    // rows per unit, keys per tile, ring slots
 constexpr int kGroups = 256;              // workgroups: one per CU
-constexpr int kMinRun = 4;                // tiles
+constexpr int kMinRun = 4, kCutCost = 16; // tiles
 }  // namespace rowsk
 
-// NW waves of 32 query rows over a ring of 64-key tiles in LDS, each filled two
+// Eight waves of 32 query rows over a ring of 64-key tiles in LDS, each filled two
 // steps (bf16, by LDS DMA) or one step (4-bit, through registers, as bf16) ahead:
 // S^T = K Q^T with v_mfma_f32_32x32x16 (a lane holds 16 keys of one row), online softmax in log2
 // units, O^T += V^T P^T with V^T by the transposing LDS read.  Step i multiplies
 // the keys of tile i and the values of tile i - 1; the two halves of the
 // workgroup take the softmax at opposite ends of a step, so that one's
 // exponentials meet the other's matrix instructions.
-template <int D, bool MX, int NW, bool IDX>
-__global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
+template <int D, bool MX, bool IDX>
+__global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     using namespace pg;
     using namespace rowsk;
-    constexpr int ROWS = 32 * NW, NT = 64 * NW;
     constexpr int KS = D / 16, DB = D / 32;               // contraction steps of S^T, 32-dim blocks of O^T
     constexpr int RB = D * 2, KB = TK * RB;               // bytes per staged row, of the keys of a slot
     constexpr int CH = RB / 16;                           // 16-byte chunks per row
@@ -787,7 +873,6 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
     const int lr = lane & 31, lh = lane >> 5;
     const int H = a.q.n, grp = H / a.kv.Hkv;
     const int lg = a.kv.lg_page, ps = 1 << lg;
-    const int wg = line_index(a.nw);
     // scale: a negative one is taken into the queries; zero as the smallest normal
     // float, which leaves the weights of finite scores exactly 1 and of masked ones 0
     const float c = fmaxf(__builtin_fabsf(a.c), 1.17549435e-38f);
@@ -813,7 +898,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
 
     int held = 0;                                          // which of the two pieces there are
     Walk<TK, ROWS> w;
-    bool more = w.init(a, wg, kMinRun);
+    bool more = w.init(a, kMinRun, kCutCost);
+    const int wg = w.wg;
     while (more) {
         if (!w.locate(a)) {
             more = w.x < w.end;
@@ -821,7 +907,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
         }
         const Seq sq = w.s;
         const int kvh = w.kvh, row0 = w.tile * ROWS, n_rows = min(ROWS, sq.n * grp - row0);
-        const int hi_lim = a.causal ? sq.len - sq.n + (row0 + n_rows - 1) / grp : sq.len - 1;
+        const int hi_lim = a.causal ? sq.len - sq.n + quot(row0 + n_rows - 1, grp) : sq.len - 1;
         const int kend = max(hi_lim + 1, 0);               // keys that some row sees
         const int c_end = kend == 0 ? w.c0 : w.c1;
         const int n_tiles = c_end - w.c0;
@@ -834,7 +920,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
         const int hd = on ? kvh * grp + rho % grp : 0;
         const int lim = !on ? -1 : a.causal ? sq.len - sq.n + tok : sq.len - 1;
         const int wa = row0 + wave * 32, wb = min(wa + 31, row0 + n_rows - 1);      // the wave's rows (none: wb < wa)
-        const int tok_a = wa / grp, tok_b = max(wb, wa) / grp;
+        const int tok_a = quot(wa, grp), tok_b = quot(max(wb, wa), grp);
         const int lim_lo = a.causal ? sq.len - sq.n + tok_a : sq.len - 1;      // every row of the wave sees these
         const int lim_hi = wb < wa ? -1 : a.causal ? sq.len - sq.n + tok_b : sq.len - 1;
 
@@ -866,45 +952,41 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
             return ok ? pid : 0;
         };
         const int64_t hrow = static_cast<int64_t>(kvh) << lg;
-        // bf16: the wave stages RPW rows of keys and of values, NP pages' worth; lane l
-        // holds the pages of tile pbase + l
-        constexpr int RPW = TK / NW, NP = RPW > 16 ? RPW / 16 : 1, PR = RPW / NP;    // rows per page piece
-        constexpr int RPI = 1024 / RB, PER_K = RPW / RPI, PER = 2 * PER_K;           // rows, DMA instructions
-        int pid[NP], pbase = 0;
+        // bf16: the wave stages 8 rows of keys and of values, which lie in one page;
+        // lane l holds the page of tile pbase + l
+        constexpr int RPW = TK / NW, RPI = 1024 / RB, PER = 2 * (RPW / RPI);     // rows per wave, per DMA instruction
+        int pid = 0, pbase = 0;
         auto fetch = [&](int kt) __attribute__((always_inline)) {
             pbase = kt;
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const int key = (kt + lane) * TK + wave * RPW + 16 * p;
-                pid[p] = page_at(key, kt + lane < c_end && key < kend);
-            }
+            const int key = (kt + lane) * TK + wave * RPW;
+            pid = page_at(key, kt + lane < c_end && key < kend);
         };
         auto dma = [&](char *slot, int kt) __attribute__((always_inline)) {
             if (kt - pbase >= 64) fetch(kt);
             const int r = lane / CH, ch = lane % CH;
+            const int key = kt * TK + wave * RPW;
+            // rows past the last key that some row sees are staged as zeros
+            const int rows = kt < c_end ? max(0, min(RPW, kend - key)) : 0;
+            const int64_t page = __builtin_amdgcn_readlane(pid, (kt - pbase) & 63);
+            const int64_t at = (hrow + (key & (ps - 1))) * RB;
+            const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+                a.kv.k + page * a.kv.k_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
+            const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+                a.kv.v + page * a.kv.v_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const int key = kt * TK + wave * RPW + 16 * p;
-                const int rows = kt < c_end ? max(0, min(PR, kend - key)) : 0;
-                const int64_t page = __builtin_amdgcn_readlane(pid[p], (kt - pbase) & 63);
-                const int64_t at = (hrow + (key & (ps - 1))) * RB;
-                const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
-                    a.kv.k + page * a.kv.k_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
-                const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
-                    a.kv.v + page * a.kv.v_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
-#pragma unroll
-                for (int u = 0; u < PER_K / NP; ++u) {
-                    const int row = wave * RPW + 16 * p + u * RPI;      // first row of the instruction in the tile
-                    lds_load16(kr, slot + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ kswz(row + r))));
-                    lds_load16(vr, slot + KB + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ vswz(row + r))));
-                }
+            for (int u = 0; u < RPW / RPI; ++u) {
+                const int row = wave * RPW + u * RPI;      // first row of the instruction in the tile
+                lds_load16(kr, slot + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ kswz(row + r))));
+                lds_load16(vr, slot + KB + row * RB, static_cast<uint32_t>((u * RPI + r) * RB + 16 * (ch ^ vswz(row + r))));
             }
         };
         // 4-bit: a thread takes groups of 32 dims (16 bytes of codes, a scale byte);
         // lane l holds the page of key block l % 4 (16 keys) of tile pbase + l / 4
-        constexpr int GPR = D / 32, UNITS = 2 * TK * GPR, UPT = UNITS > NT ? UNITS / NT : 1;
-        uint4 cr[UPT];
-        uint32_t csr[UPT];
+        constexpr int GPR = D / 32, UNITS = TK * GPR;      // groups per row, per tile of keys (of values)
+        const int mid = tid % UNITS, mrow = mid / GPR, mgrp = mid % GPR;
+        const bool mval = tid >= UNITS, mon = tid < 2 * UNITS;
+        uint4 codes = make_uint4(0, 0, 0, 0);
+        uint32_t scale = 0;
         int pcur = 0, pnext = 0;
         auto mx_pages = [&](int kt) __attribute__((always_inline)) {
             const int key = (kt + (lane >> 2)) * TK + 16 * (lane & 3);
@@ -916,36 +998,27 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
                 pbase += 16;
                 pnext = mx_pages(pbase + 16);
             }
-#pragma unroll
-            for (int u = 0; u < UPT; ++u) {
-                const int id = tid + NT * u, kid = id % (TK * GPR), r = kid / GPR, gi = kid % GPR;
-                const bool val = id >= TK * GPR;
-                const int key = kt * TK + r;
-                const int64_t page = __shfl(pcur, (4 * (kt - pbase) + (r >> 4)) & 63, 64);
-                cr[u] = make_uint4(0, 0, 0, 0);
-                csr[u] = 0;
-                if (id < UNITS && kt < c_end && key < kend) {
-                    const int64_t row = hrow + (key & (ps - 1));
-                    const uint8_t *cp = (val ? a.kv.v + page * a.kv.v_page : a.kv.k + page * a.kv.k_page) + row * (D / 2);
-                    const uint8_t *sp = (val ? a.kv.vs + page * a.kv.vs_page : a.kv.ks + page * a.kv.ks_page) + row * GPR;
-                    cr[u] = reinterpret_cast<const uint4 *>(cp)[gi];
-                    csr[u] = sp[gi];
-                }
+            const int key = kt * TK + mrow;
+            const int64_t page = __shfl(pcur, (4 * (kt - pbase) + (mrow >> 4)) & 63, 64);
+            codes = make_uint4(0, 0, 0, 0);
+            scale = 0;
+            if (mon && kt < c_end && key < kend) {
+                const int64_t row = hrow + (key & (ps - 1));
+                const uint8_t *cp = (mval ? a.kv.v + page * a.kv.v_page : a.kv.k + page * a.kv.k_page) + row * (D / 2);
+                const uint8_t *sp = (mval ? a.kv.vs + page * a.kv.vs_page : a.kv.ks + page * a.kv.ks_page) + row * GPR;
+                codes = reinterpret_cast<const uint4 *>(cp)[mgrp];
+                scale = sp[mgrp];
             }
         };
         auto mx_store = [&](char *slot) __attribute__((always_inline)) {
+            if (!mon) return;
+            char *row = slot + (mval ? KB : 0) + mrow * RB;
+            const int swz = mval ? vswz(mrow) : kswz(mrow);
+            const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
+            const float sc = __uint_as_float(scale << 23);
 #pragma unroll
-            for (int u = 0; u < UPT; ++u) {
-                const int id = tid + NT * u, kid = id % (TK * GPR), r = kid / GPR, gi = kid % GPR;
-                if (id >= UNITS) continue;
-                char *row = slot + (id >= TK * GPR ? KB : 0) + r * RB;
-                const int swz = id >= TK * GPR ? vswz(r) : kswz(r);
-                const uint32_t cw[4] = {cr[u].x, cr[u].y, cr[u].z, cr[u].w};
-                const float sc = __uint_as_float(csr[u] << 23);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint4 *>(row + 16 * ((4 * gi + j) ^ swz)) = unpack_mx8(cw[j], sc);
-            }
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<uint4 *>(row + 16 * ((4 * mgrp + j) ^ swz)) = unpack_mx8(cw[j], sc);
         };
 
         // ---- one tile's work
@@ -1157,13 +1230,17 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_rows_kernel(PagedArgs a) {
     if (tid < 2 && !(held >> tid & 1)) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + tid].n = 0;
 }
 
+constexpr int joins(int rows) { return (rows + 31) / 32; }
+
 // Joins the pieces of the cut units: workgroup i looks at its own two, and of a
-// unit cut over workgroups first .. first + n - 1 takes the rows i - first, + n, ...
+// unit cut over workgroups first .. first + n - 1 takes the rows i - first, + n, ...,
+// of which the YS workgroups (i, y) take every YS-th (a 256-row unit has too many for one).
+// D / 4 lanes take a row's dims; RP rows are joined at once, each by SP of the
+// workgroup's groups of lanes (which take every SP-th piece)
 template <int D, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     using namespace pg;
-    constexpr int LD = D / 4, PW = 256 / LD;               // lanes per row, groups of lanes
-    constexpr int kFew = 8;                                // pieces that one group adds by itself
+    constexpr int LD = D / 4, PW = 256 / LD, YS = joins(ROWS);
     __shared__ float4 acc_s[PW][LD];
     __shared__ float2 ml_s[PW];
     const int tid = threadIdx.x, pw = tid / LD, l = tid % LD;
@@ -1171,65 +1248,64 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     for (int part = 0; part < 2; ++part) {
         const PieceOf pc = reinterpret_cast<const PieceOf *>(a.pieces)[2 * wg + part];
         if (pc.n == 0) continue;
-        // (m, ls, o) += the pieces p0, p0 + step, ... of row r
-        auto add = [&](int r, int p0, int step, float &m, float &ls, float4 &o) __attribute__((always_inline)) {
-            m = -__builtin_inff();
-            ls = 0.f;
-            o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int p = p0; p < pc.n; p += step) {
-                // the unit's first piece is its workgroup's last one, the others begin a run
-                const int64_t row = (2 * static_cast<int64_t>(pc.first + p) + (p == 0 ? 1 : 0)) * ROWS + r;
-                const float2 x = *reinterpret_cast<const float2 *>(a.part_ml + 2 * row);
-                const float4 v = *reinterpret_cast<const float4 *>(a.part_o + row * D + 4 * l);
-                const float mn = fmaxf(m, x.x);
+        // as many rows at once as this workgroup has
+        const int step = pc.n * YS, r0 = wg - pc.first + static_cast<int>(blockIdx.y) * pc.n;
+        const int mine = (pc.rows - r0 + step - 1) / step;
+        int RP = 1;
+        while (RP < PW && RP < mine) RP *= 2;
+        const int SP = PW / RP, ri = pw % RP, si = pw / RP;
+        for (int i0 = 0; i0 < mine; i0 += RP) {
+            const int r = r0 + (i0 + ri) * step;
+            float m = -__builtin_inff(), ls = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto add = [&](float mp, float lp, const float4 v) __attribute__((always_inline)) {
+                const float mn = fmaxf(m, mp);
                 const float a0 = m == -__builtin_inff() ? 0.f : exp_two(m - mn);
-                const float a1 = x.x == -__builtin_inff() ? 0.f : exp_two(x.x - mn);
-                ls = (ls == ls ? ls * a0 : ls) + (x.y == x.y ? x.y * a1 : x.y);
+                const float a1 = mp == -__builtin_inff() ? 0.f : exp_two(mp - mn);
+                // a NaN sum stays one whatever its maximum; what has no weight adds nothing
+                ls = (ls == ls ? ls * a0 : ls) + (lp == lp ? lp * a1 : lp);
                 o.x = (a0 == 0.f ? 0.f : o.x * a0) + (a1 == 0.f ? 0.f : v.x * a1);
                 o.y = (a0 == 0.f ? 0.f : o.y * a0) + (a1 == 0.f ? 0.f : v.y * a1);
                 o.z = (a0 == 0.f ? 0.f : o.z * a0) + (a1 == 0.f ? 0.f : v.z * a1);
                 o.w = (a0 == 0.f ? 0.f : o.w * a0) + (a1 == 0.f ? 0.f : v.w * a1);
                 m = mn;
-            }
-        };
-        auto write = [&](int r, float ls, const float4 o) __attribute__((always_inline)) {
-            const float inv = ls == 0.f ? 0.f : 1.f / ls;
-            const int rho = pc.row0 + r;
-            uint16_t *op = static_cast<uint16_t *>(a.o.p) + (pc.q0 + rho / grp) * a.o.st + (pc.kvh * grp + rho % grp) * a.o.sh + 4 * l;
-            *reinterpret_cast<uint2 *>(op) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-        };
-        float m, ls;
-        float4 o;
-        if (pc.n <= kFew) {                                // rows to the groups of lanes in turn
-            for (int r = wg - pc.first + pc.n * pw; r < pc.rows; r += pc.n * PW) {
-                add(r, 0, 1, m, ls, o);
-                write(r, ls, o);
-            }
-            continue;
-        }
-        for (int r = wg - pc.first; r < pc.rows; r += pc.n) {
-            add(r, pw, PW, m, ls, o);
-            __syncthreads();
-            acc_s[pw][l] = o;
-            if (l == 0) ml_s[pw] = make_float2(m, ls);
-            __syncthreads();
-            if (pw == 0) {
-#pragma unroll
-                for (int p = 1; p < PW; ++p) m = fmaxf(m, ml_s[p].x);
-                float lt = 0.f;
-                float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int p = 0; p < PW; ++p) {
-                    const float mp = ml_s[p].x, al = mp == -__builtin_inff() ? 0.f : exp_two(mp - m), lp = ml_s[p].y;
-                    lt += lp == lp ? lp * al : lp;
-                    const float4 v = acc_s[p][l];
-                    t.x += al == 0.f ? 0.f : v.x * al;
-                    t.y += al == 0.f ? 0.f : v.y * al;
-                    t.z += al == 0.f ? 0.f : v.z * al;
-                    t.w += al == 0.f ? 0.f : v.w * al;
+            };
+            if (r < pc.rows) {
+#pragma unroll 4
+                for (int p = si; p < pc.n; p += SP) {
+                    // the unit's first piece is its workgroup's last one, the others begin a run
+                    const int64_t row = (2 * static_cast<int64_t>(pc.first + p) + (p == 0 ? 1 : 0)) * ROWS + r;
+                    const float2 x = *reinterpret_cast<const float2 *>(a.part_ml + 2 * row);
+                    add(x.x, x.y, *reinterpret_cast<const float4 *>(a.part_o + row * D + 4 * l));
                 }
-                write(r, lt, t);
+            }
+            if (SP > 1) {
+                __syncthreads();
+                acc_s[pw][l] = o;
+                if (l == 0) ml_s[pw] = make_float2(m, ls);
+                __syncthreads();
+                if (si == 0) {
+                    for (int q = 1; q < SP; ++q) m = fmaxf(m, ml_s[ri + q * RP].x);
+                    ls = 0.f;
+                    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int q = 0; q < SP; ++q) {
+                        const float2 x = ml_s[ri + q * RP];
+                        const float4 v = acc_s[ri + q * RP][l];
+                        const float al = x.x == -__builtin_inff() ? 0.f : exp_two(x.x - m);
+                        ls += x.y == x.y ? x.y * al : x.y;
+                        o.x += al == 0.f ? 0.f : v.x * al;
+                        o.y += al == 0.f ? 0.f : v.y * al;
+                        o.z += al == 0.f ? 0.f : v.z * al;
+                        o.w += al == 0.f ? 0.f : v.w * al;
+                    }
+                }
+            }
+            if (si == 0 && r < pc.rows) {
+                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                const int rho = pc.row0 + r;
+                uint16_t *op = static_cast<uint16_t *>(a.o.p) + (pc.q0 + rho / grp) * a.o.st + (pc.kvh * grp + rho % grp) * a.o.sh + 4 * l;
+                *reinterpret_cast<uint2 *>(op) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
             }
         }
     }
@@ -1237,36 +1313,38 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
 
 namespace {
 
-// Query rows per workgroup: as many as an average sequence has
+// Query rows per unit, by the average sequence's
 int unit_rows(int64_t T, int64_t B, int64_t grp) {
     const int64_t rows = (T * grp + B - 1) / B;
-    return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    return rows <= 16 ? 16 : rows <= 128 ? 32 : rowsk::ROWS;
 }
-int workgroups(int rows) { return rows == 16 ? few::kGroups : rowsk::kGroups; }
+int workgroups(int rows) { return rows <= 32 ? few::kGroups : rowsk::kGroups; }
+int block_keys(int rows) { return rows <= 32 ? few::TK : rowsk::TK; }
+// units at most: full row tiles, and a last one per sequence
+int64_t most_units(int64_t T, int64_t B, int64_t H, int64_t Hkv, int rows) {
+    return T * H / rows + (T < B ? T : B) * Hkv;
+}
 
 template <int D, bool MX, int ROWS>
 hipError_t launch(const PagedArgs &a, hipStream_t stream) {
-    if constexpr (ROWS == 16) {
-        if (a.idx) paged_few_kernel<D, MX, true><<<a.nw, few::kThreads, 0, stream>>>(a);
-        else paged_few_kernel<D, MX, false><<<a.nw, few::kThreads, 0, stream>>>(a);
+    if constexpr (ROWS <= 32) {
+        if (a.idx) paged_few_kernel<D, MX, ROWS / 16, true><<<a.nw, few::kThreads, 0, stream>>>(a);
+        else paged_few_kernel<D, MX, ROWS / 16, false><<<a.nw, few::kThreads, 0, stream>>>(a);
     } else {
-        if (a.idx) paged_rows_kernel<D, MX, ROWS / 32, true><<<a.nw, 2 * ROWS, 0, stream>>>(a);
-        else paged_rows_kernel<D, MX, ROWS / 32, false><<<a.nw, 2 * ROWS, 0, stream>>>(a);
+        if (a.idx) paged_rows_kernel<D, MX, true><<<a.nw, rowsk::NT, 0, stream>>>(a);
+        else paged_rows_kernel<D, MX, false><<<a.nw, rowsk::NT, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
-    // a page table this narrow holds short units only: none is cut
-    const int64_t keys = static_cast<int64_t>(a.width) << a.kv.lg_page;
-    if (e != hipSuccess || keys <= pg::kShort * (ROWS == 16 ? few::TK : rowsk::TK)) return e;
-    paged_join_kernel<D, ROWS><<<a.nw, 256, 0, stream>>>(a);
+    if (e != hipSuccess || a.whole) return e;
+    paged_join_kernel<D, ROWS><<<dim3(a.nw, joins(ROWS)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int D, bool MX>
 hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
     if (rows == 16) return launch<D, MX, 16>(a, stream);
-    if (rows == 64) return launch<D, MX, 64>(a, stream);
-    if (rows == 128) return launch<D, MX, 128>(a, stream);
-    return launch<D, MX, 256>(a, stream);
+    if (rows == 32) return launch<D, MX, 32>(a, stream);
+    return launch<D, MX, rowsk::ROWS>(a, stream);
 }
 
 }  // namespace
@@ -1274,9 +1352,8 @@ hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
 // whether the line is shorter than 2^31 whatever the lengths (keys: what a page
 // table row can hold)
 bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys) {
-    const int rows = unit_rows(T, B, H / Hkv), tk = rows == 16 ? few::TK : rowsk::TK;
-    const int64_t units = T * H / rows + (T < B ? T : B) * Hkv;      // row tiles: full ones, a last one per sequence
-    return (units + 1) * (keys / tk + 3) < (int64_t(1) << 31) - 1024;
+    const int rows = unit_rows(T, B, H / Hkv);
+    return (most_units(T, B, H, Hkv, rows) + 1) * (keys / block_keys(rows) + 3) < (int64_t(1) << 31) - 1024;
 }
 
 // two pieces per workgroup: what joins them, their maxima and sums, their outputs
@@ -1289,6 +1366,8 @@ size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream) {
     const int rows = unit_rows(a.T, a.B, a.q.n / a.kv.Hkv);
     a.nw = workgroups(rows);
+    a.whole = (static_cast<int64_t>(a.width) << a.kv.lg_page) <= pg::kShort * block_keys(rows) &&
+              most_units(a.T, a.B, a.q.n, a.kv.Hkv, rows) <= a.nw;
     a.pieces = workspace;
     a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * a.nw * sizeof(pg::PieceOf));
     a.part_ml = a.part_o + static_cast<int64_t>(2 * a.nw) * rows * D;
