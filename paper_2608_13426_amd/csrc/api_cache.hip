@@ -123,7 +123,9 @@ rmm_status_t rmm_qk_norm_rope(rmm_dtype_t dtype, int64_t batch, int64_t L, int64
     }
     const hipError_t e = rmm::launch_rotate(a, dtype == RMM_BF16, static_cast<int>(D), stream);
     if (e != hipSuccess || need == 0) return from_hip(e);
-    return from_hip(rmm::launch_score_finalize(a.partials, batch, blocks, a.q.n * D, energy, stream));
+    // few partial sums per column are added by one thread, many by sixteen
+    if (blocks < 32 || batch > kMaxHeads) return from_hip(rmm::launch_score_finalize(a.partials, batch, blocks, a.q.n * D, energy, stream));
+    return from_hip(rmm::launch_score_finalize_grouped(a.partials, batch, blocks, a.q.n * D, energy, stream));
 }
 
 rmm_status_t rmm_kv_append(int64_t T, const rmm_heads_t *k, const rmm_heads_t *v, const int32_t *slots,

@@ -100,6 +100,20 @@ __device__ __forceinline__ Piece piece_of(int j, int rot, int interleaved) {
     return {2 * h + r, 2 * h + n / 2 + r, 0};
 }
 
+// 1 / sqrt(x) for x >= 0: the hardware's estimate and two Newton steps, within a
+// few float64 roundings (its fp32 rounding is the correct one but for about one
+// value in 2^27); 0 for infinity
+__device__ __forceinline__ double rsqrt64(double x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = fma(0.5 * r, fma(-x * r, r, 1.0), r);
+    return __builtin_isinf(x) ? 0.0 : r;
+#else
+    return x;
+#endif
+}
+
 __device__ __forceinline__ void turn(float &a, float &b, float c, float s) {
 #pragma clang fp contract(off)
     const float x = a * c - b * s, y = b * c + a * s;
@@ -170,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
             ss += dpp_f64<0xB1>(ss);
             ss += dpp_f64<0x4E>(ss);
             if constexpr (LPH == 8) ss += dpp_f64<0x141>(ss);
-            const float r = static_cast<float>(1.0 / sqrt(ss / D + static_cast<double>(a.eps)));
+            const float r = static_cast<float>(rsqrt64(ss / D + static_cast<double>(a.eps)));
             if (gam) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -292,12 +306,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
 
 // Cached tokens as bf16 rows: one thread per 8 elements
 template <int D>
-__global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const int32_t *__restrict__ slots, int64_t n8,
+__global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const int32_t *__restrict__ slots, uint32_t rows,
                                                              Heads k, Heads v) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= n8) return;
-    const int c = static_cast<int>(i % (D / 8)), hv = static_cast<int>(i / (D / 8) % (2 * kv.Hkv));
-    const int64_t t = i / (D / 8) / (2 * kv.Hkv);
+    constexpr int CH = D / 8;
+    const uint32_t i = blockIdx.x * (kThreads / CH) + threadIdx.x / CH;      // row: token, key or value head
+    if (i >= rows) return;
+    const uint32_t t = i / (2u * kv.Hkv);
+    const int c = threadIdx.x % CH, hv = static_cast<int>(i - t * (2u * kv.Hkv));
     const bool key = hv < kv.Hkv;
     const int head = key ? hv : hv - kv.Hkv, slot = slots[t];
     const int page = slot >> kv.lg_page, off = slot & ((1 << kv.lg_page) - 1);
@@ -327,20 +342,23 @@ __global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const i
 
 namespace {
 
-// Tokens per workgroup: few while there are too few workgroups to fill the
-// CUs, more where the sums of squares (one float64 row of columns per
-// workgroup) would be traffic of their own
-int rotate_tokens(int64_t T, int64_t heads, int D) {
+// Tokens per workgroup.  With energies each workgroup writes a float64 row of
+// columns and adds up its waves, so 256 workgroups at least, else as many tokens
+// as that leaves (us, kernel and final sum, for 256 / 512 / 1024 of them: 8192
+// tokens x 32 + 8 heads 32 + 4.8 / 32 + 4.7 / 34 + 4.7; 2 x 1001 x 16 + 8 with norms 12
+// + 4.4 / 14 + 5.7 / 14 + 5.7).  Without, 2048 (8192 tokens x 8 + 8 heads into a 4-bit
+// cache, 256 / 512 / 1024 / 2048: 25 / 16 / 14 / 12).
+int rotate_tokens(int64_t T, int64_t heads, int D, bool energy) {
     const int64_t groups = (heads + 1024 / D - 1) / (1024 / D);
     int tb = kWaves;
-    while (tb < 64 && T / (2 * tb) * groups >= 1024) tb *= 2;
+    while (tb < 64 && T / (2 * tb) * groups >= (energy ? 256 : 2048)) tb *= 2;
     return tb;
 }
 
 template <typename T, int D, int KV, bool ENERGY>
 hipError_t launch(const RotateArgs &a, hipStream_t stream) {
     const int nv = a.q.n + a.k.n + a.v.n, groups = (nv + 1024 / D - 1) / (1024 / D);
-    const int TB = rotate_tokens(a.T, ENERGY ? a.q.n : nv, D);
+    const int TB = rotate_tokens(a.T, ENERGY ? a.q.n : nv, D, ENERGY);
     const int64_t per = ENERGY ? a.L : a.T, blocks = (per + TB - 1) / TB, units = ENERGY ? a.T / a.L : 1;
     const dim3 grid(static_cast<uint32_t>(units * blocks), static_cast<uint32_t>(groups));
     if (a.gq || a.gk) rotate_kernel<T, D, KV, true, ENERGY><<<grid, kThreads, 0, stream>>>(a, TB, blocks);
@@ -351,7 +369,7 @@ hipError_t launch(const RotateArgs &a, hipStream_t stream) {
 }  // namespace
 
 int64_t rotate_blocks(int64_t batch, int64_t L, int64_t heads, int D) {
-    const int TB = rotate_tokens(batch * L, heads, D);
+    const int TB = rotate_tokens(batch * L, heads, D, true);
     return (L + TB - 1) / TB;
 }
 
@@ -373,10 +391,10 @@ hipError_t launch_kv_append(const RotateArgs &a, int D, hipStream_t stream) {
 
 hipError_t launch_kv_gather(const KvPages &kv, const int32_t *slots, int64_t T, const Heads &k, const Heads &v, int D,
                             hipStream_t stream) {
-    const int64_t n8 = T * 2 * kv.Hkv * (D / 8);
-    const dim3 grid(static_cast<uint32_t>((n8 + kThreads - 1) / kThreads));
-    if (D == 128) kv_gather_kernel<128><<<grid, kThreads, 0, stream>>>(kv, slots, n8, k, v);
-    else kv_gather_kernel<64><<<grid, kThreads, 0, stream>>>(kv, slots, n8, k, v);
+    const uint32_t rows = static_cast<uint32_t>(T * 2 * kv.Hkv), per = kThreads / (D / 8);
+    const uint32_t grid = rows / per + (rows % per != 0);
+    if (D == 128) kv_gather_kernel<128><<<grid, kThreads, 0, stream>>>(kv, slots, rows, k, v);
+    else kv_gather_kernel<64><<<grid, kThreads, 0, stream>>>(kv, slots, rows, k, v);
     return hipGetLastError();
 }
 
