@@ -6,8 +6,8 @@
 // A query row is one (new token, query head of a kv head): the heads of a group
 // share every key read.  A unit is one (sequence, kv head, tile of query rows).
 //
-//   up to 64 rows (a decode step, a few drafted tokens): paged_few_kernel, 16, 32
-//   or 64 rows.  The four waves of a workgroup take 32-key chunks in turn; keys and
+//   up to 128 rows (a decode step, drafted tokens): paged_few_kernel, units of 16
+//   to 128 rows.  The four waves of a workgroup take 32-key chunks in turn; keys and
 //   values go from memory to registers to the matrix cores without LDS.  Bound by
 //   reading the cache.
 //   more rows (prompt chunks): paged_rows_kernel, 32 rows per wave, 64-key tiles
@@ -106,6 +106,15 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // a / b of non-negative values
 __device__ __forceinline__ int quot(int a, int b) {
     return uniform(static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)));
+}
+// x or that of the lane that the DPP control CTRL names; every lane must be active
+template <int CTRL>
+__device__ __forceinline__ uint32_t or_row(uint32_t x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return x | static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xF, 0xF, false));
+#else
+    return x;
+#endif
 }
 // inclusive prefix sum over the wave's lanes
 __device__ __forceinline__ int prefix_sum(int x) {
@@ -410,16 +419,32 @@ __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, 
     }
 }
 
-// The retained dims of a unit's rows as bits (16 lanes per row); dims outside [0, D) are ignored
+// The retained dims of a unit's rows as bits; dims outside [0, D) are ignored.  16
+// lanes per row, each with up to D / 16 entries of its list, all asked for at once.
 template <int D, int NT>
 __device__ __forceinline__ void read_lists(const PagedArgs &a, const Seq &sq, int kvh, int row0, int n_rows, uint32_t (*keep)[D / 32]) {
-    const int H = a.q.n, grp = H / a.kv.Hkv;
-    for (int r = threadIdx.x >> 4; r < n_rows; r += NT / 16) {
-        const int q = row0 + r;
+    constexpr int E = D / 16, W = D / 32;
+    const int H = a.q.n, grp = H / a.kv.Hkv, u0 = threadIdx.x & 15;
+    for (int r = threadIdx.x >> 4; r < (n_rows + 3) / 4 * 4; r += NT / 16) {     // whole waves together
+        const int q = row0 + min(r, n_rows - 1);
         const int32_t *list = a.idx + (static_cast<int64_t>(sq.q0 + q / grp) * H + kvh * grp + q % grp) * a.k;
-        for (int u = threadIdx.x & 15; u < a.k; u += 16) {
-            const int d = list[u];
-            if (d >= 0 && d < D) atomicOr(&keep[r][d >> 5], 1u << (d & 31));
+        int d[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] = u0 + 16 * i < a.k ? list[u0 + 16 * i] : -1;
+        uint32_t w[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            w[j] = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) w[j] |= (d[i] >> 5) == j ? 1u << (d[i] & 31) : 0u;
+            w[j] = or_row<0xB1>(w[j]);                     // over the 16 lanes: l ^ 1, l ^ 2, mirrored in 8, in 16
+            w[j] = or_row<0x4E>(w[j]);
+            w[j] = or_row<0x141>(w[j]);
+            w[j] = or_row<0x140>(w[j]);
+        }
+        if (r < n_rows && u0 == 0) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) keep[r][j] = w[j];
         }
     }
 }
@@ -447,13 +472,15 @@ constexpr int kCutCost = 8;
 // its lane group contributes to O^T = V^T P^T: the weights stay where they are.
 // The value rows, loaded as rows, are turned 8 x 8 in registers (v_perm).  4-bit
 // codes become bf16 with v_cvt_scalef32_pk_bf16_fp4 (exact, the scale included).
-// R: 16-row tiles, which share each key and value fragment (their queries are then
-// kept in LDS); MX: 4-bit cache; IDX: scores over retained dims
-template <int D, bool MX, int R, bool IDX>
+// R: 16-row tiles per wave, which share each key and value fragment (their queries
+// are then kept in LDS); RG: groups of waves with rows of their own, which walk the
+// same chunks side by side, so that all but the first read them from a cache;
+// MX: 4-bit cache; IDX: scores over retained dims
+template <int D, bool MX, int R, int RG, bool IDX>
 __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a) {
     using namespace pg;
     using namespace few;
-    constexpr int ROWS = 16 * R;
+    constexpr int WROWS = 16 * R, ROWS = WROWS * RG, KG = kWaves / RG;       // rows per wave, per unit; chunk streams
     constexpr int KS = D / 32, DM = D / 16;               // contraction steps of S^T, MFMA rows of O^T
     constexpr int ROWB = MX ? D / 2 : D * 2, SROWB = D / 32;    // bytes per cached row, scale bytes per row
     constexpr int OLD = D + 4;                            // row stride of the joining buffer, floats
@@ -462,10 +489,11 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
     __shared__ float ml[kWaves][16][2];
     __shared__ int state[kWaves];                         // bit 0: a page or length out of range, bit 1: to be redone
     __shared__ uint32_t keep[IDX ? ROWS : 1][KS];
-    __shared__ uint4 qs[R > 1 ? R : 1][KS][R > 1 ? 64 : 1];
+    __shared__ uint4 qs[R > 1 ? R * RG : 1][KS][R > 1 ? 64 : 1];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rg = wave % RG, kg = wave / RG;
     const int col = lane & 15, g = lane >> 4;
     const int H = a.q.n, grp = H / a.kv.Hkv;
     const int lg = a.kv.lg_page, ps = 1 << lg;
@@ -482,61 +510,27 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
         const Seq sq = w.s;
         const int kvh = w.kvh, row0 = w.tile * ROWS, n_rows = min(ROWS, sq.n * grp - row0);
 
-        // ---- the unit's query rows
-        if constexpr (IDX) {
-            for (int i = tid; i < ROWS * KS; i += kThreads) (&keep[0][0])[i] = 0;
-            __syncthreads();
-            read_lists<D, kThreads>(a, sq, kvh, row0, n_rows, keep);
-            __syncthreads();
-        }
-        // dims that lane (col, g) holds at contraction step s
-        auto dim_of = [&](int s) { return MX ? (D / 4) * g + 8 * s : 32 * s + 8 * g; };
-        auto query = [&](int r, int s) __attribute__((always_inline)) {
-            const int rr = 16 * r + col;
-            if (rr >= n_rows) return make_uint4(0, 0, 0, 0);
-            const int rho = row0 + rr, tok = rho / grp;
-            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + (kvh * grp + rho - tok * grp) * a.q.sh;
-            uint4 x = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
-            if constexpr (IDX) x = keep8(x, keep[rr][dim_of(s) >> 5] >> (dim_of(s) & 31));
-            return x;
-        };
-        uint4 qf[R > 1 ? 1 : KS];
-        if constexpr (R == 1) {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s] = query(0, s);
-        } else {
-            for (int i = wave; i < R * KS; i += kWaves) qs[i / KS][i % KS][lane] = query(i / KS, i % KS);
-            __syncthreads();
-        }
         // last key of the lane's rows; the first limit and the last of the unit's rows
         int lim[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int rr = 16 * r + col;
+            const int rr = rg * WROWS + 16 * r + col;
             lim[r] = rr >= n_rows ? -1 : a.causal ? sq.len - sq.n + (row0 + rr) / grp : sq.len - 1;
         }
         const int lo_lim = a.causal ? sq.len - sq.n + quot(row0, grp) : sq.len - 1;
         const int hi_lim = a.causal ? sq.len - sq.n + quot(row0 + n_rows - 1, grp) : sq.len - 1;
-        const int c_stop = min(w.c1, hi_lim < 0 ? 0 : hi_lim / TK + 1);
+        // a wave without rows has no chunks
+        const int c_stop = rg * WROWS < n_rows ? min(w.c1, hi_lim < 0 ? 0 : hi_lim / TK + 1) : 0;
 
-        f32x4_t o[R][DM];
-        float m_run[R], l_run[R], least = 0.f;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            m_run[r] = -__builtin_inff();
-            l_run[r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < DM; ++i) o[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
         bool bad = sq.bad;
 
-        // ---- the wave's chunks c0 + wave, + 4, ...; lane l holds the pages of the
+        // ---- the wave's chunks c0 + kg, + KG, ...; lane l holds the pages of the
         // l-th of them (two where a page has 16 keys)
         const int32_t *trow = a.table + w.b * a.table_ld;
         int pid_a = 0, pid_b = 0;
         auto fetch_pages = [&](int c) __attribute__((always_inline)) {
-            const bool in = c + kWaves * lane < c_stop;
-            const int key = in ? (c + kWaves * lane) * TK : 0;
+            const bool in = c + KG * lane < c_stop;
+            const int key = in ? (c + KG * lane) * TK : 0;
             const int p0 = key >> lg, p1 = in && key + 16 < sq.len ? (key + 16) >> lg : p0;
             pid_a = in ? trow[p0] : 0;
             pid_b = in ? trow[p1] : 0;
@@ -608,6 +602,55 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             }
         };
 
+        // the first chunks are on their way while the lists and queries are read
+        Raw raw[NBUF];
+        int c = w.c0 + kg;
+        auto first = [&]() __attribute__((always_inline)) {    // up to 64 chunks per fetch of page numbers
+            fetch_pages(c);
+            load_k(raw[0], c, 0);
+            load_v(raw[0], c, 0);
+            if constexpr (NBUF == 2) {
+                if (c + KG < c_stop) {
+                    load_k(raw[NBUF - 1], c + KG, 1);
+                    load_v(raw[NBUF - 1], c + KG, 1);
+                }
+            }
+        };
+        if (c < c_stop) first();
+
+        // ---- the unit's query rows
+        if constexpr (IDX) {
+            read_lists<D, kThreads>(a, sq, kvh, row0, n_rows, keep);
+            lds_barrier();
+        }
+        // dims that lane (col, g) holds at contraction step s
+        auto dim_of = [&](int s) { return MX ? (D / 4) * g + 8 * s : 32 * s + 8 * g; };
+        auto query = [&](int r, int s) __attribute__((always_inline)) {
+            const int rr = 16 * r + col;
+            if (rr >= n_rows) return make_uint4(0, 0, 0, 0);
+            const int rho = row0 + rr, tok = rho / grp;
+            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + (kvh * grp + rho - tok * grp) * a.q.sh;
+            uint4 x = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
+            if constexpr (IDX) x = keep8(x, keep[rr][dim_of(s) >> 5] >> (dim_of(s) & 31));
+            return x;
+        };
+        uint4 qf[R > 1 ? 1 : KS];
+        if constexpr (R == 1) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[s] = query(0, s);
+        } else {
+            for (int i = wave; i < R * RG * KS; i += kWaves) qs[i / KS][i % KS][lane] = query(i / KS, i % KS);
+            lds_barrier();
+        }
+        f32x4_t o[R][DM];
+        float m_run[R], l_run[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m_run[r] = -__builtin_inff();
+            l_run[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DM; ++i) o[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
         // chunk c, held in x; the keys and then the values of the chunk that takes its
         // place are asked for as soon as its own are used up
         auto chunk = [&](Raw &x, int c, int nth, bool next) __attribute__((always_inline)) {
@@ -633,18 +676,12 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                 for (int s = 0; s < KS; ++s) {
                     uint4 q;
                     if constexpr (R == 1) q = qf[s];
-                    else q = qs[r][s][lane];
+                    else q = qs[rg * R + r][s][lane];
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb) sc[tb] = mfma(kf[tb][s], q, sc[tb]);
                 }
                 // the next keys as soon as these are used up
-                if (r == R - 1 && next) load_k(x, c + kWaves * NBUF, nth + NBUF);
-                if constexpr (IDX) {
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) least = fminf(least, sc[tb][i]);
-                }
+                if (r == R - 1 && next) load_k(x, c + KG * NBUF, nth + NBUF);
                 // ---- weights
                 float p[2][4], mx = -__builtin_inff();
 #pragma unroll
@@ -729,33 +766,26 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 #pragma unroll
                 for (int r = 0; r < R; ++r) o[r][i] = mfma(f, pf[r], o[r][i]);
             }
-            if (next) load_v(x, c + kWaves * NBUF, nth + NBUF);
+            if (next) load_v(x, c + KG * NBUF, nth + NBUF);
         };
-        Raw raw[NBUF];
-        for (int c = w.c0 + wave; c < c_stop;) {           // up to 64 chunks per fetch of page numbers
-            fetch_pages(c);
-            const int n = min(64, (c_stop - c + kWaves - 1) / kWaves);
-            load_k(raw[0], c, 0);
-            load_v(raw[0], c, 0);
-            if constexpr (NBUF == 2) {
-                if (n > 1) {
-                    load_k(raw[NBUF - 1], c + kWaves, 1);
-                    load_v(raw[NBUF - 1], c + kWaves, 1);
-                }
-            }
+        while (c < c_stop) {
+            const int n = min(64, (c_stop - c + KG - 1) / KG);
             for (int i = 0; i < n; i += NBUF) {
-                chunk(raw[0], c + kWaves * i, i, i + NBUF < n);
+                chunk(raw[0], c + KG * i, i, i + NBUF < n);
                 if constexpr (NBUF == 2) {
-                    if (i + 1 < n) chunk(raw[NBUF - 1], c + kWaves * (i + 1), i + 1, i + 3 < n);
+                    if (i + 1 < n) chunk(raw[NBUF - 1], c + KG * (i + 1), i + 1, i + 3 < n);
                 }
             }
-            c += kWaves * n;
+            c += KG * n;
+            if (c < c_stop) first();
         }
 
-        // ---- the four waves join, 16 rows at a time
+        // ---- the waves of a row group join, 16 rows at a time
         const bool complete = w.complete();
         const int part = w.part();
-        bool odd = IDX && least == -__builtin_inff();
+        // an infinite or NaN key or value that should not count has made these NaN (zero times
+        // it, in a score or a sum)
+        bool odd = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             l_run[r] = across_rows(l_run[r], add2);
@@ -764,7 +794,7 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             for (int i = 0; i < DM; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) fin = fin && __builtin_fabsf(o[r][i][e]) < __builtin_inff();
-            odd = odd || (!fin && 16 * r + col < n_rows);
+            odd = odd || (!fin && rg * WROWS + 16 * r + col < n_rows);
         }
         const int mine = (bad ? 1 : 0) | (__ballot(odd) ? 2 : 0);
         // row r of the unit: N dims from d on
@@ -809,20 +839,23 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             __syncthreads();
             if (r == 0) all = state[0] | state[1] | state[2] | state[3];
             const int rr = tid >> 4, d0 = (tid & 15) * DM;
-            if (all != 2 && 16 * r + rr < n_rows) {
+#pragma unroll
+            for (int q = 0; q < RG; ++q) {                 // row group q is held by the waves q, q + RG, ...
+                const int row = q * WROWS + 16 * r + rr;
+                if (all == 2 || row >= n_rows) continue;
                 float m = -__builtin_inff(), ls = 0.f, acc[DM];
 #pragma unroll
-                for (int v = 0; v < kWaves; ++v) m = fmaxf(m, ml[v][rr][0]);
+                for (int v = 0; v < KG; ++v) m = fmaxf(m, ml[q + RG * v][rr][0]);
 #pragma unroll
                 for (int i = 0; i < DM; ++i) acc[i] = 0.f;
 #pragma unroll
-                for (int v = 0; v < kWaves; ++v) {
-                    const float mw = ml[v][rr][0], al = mw == -__builtin_inff() ? 0.f : exp_two(mw - m);
-                    ls += ml[v][rr][1] * al;
+                for (int v = 0; v < KG; ++v) {
+                    const float mw = ml[q + RG * v][rr][0], al = mw == -__builtin_inff() ? 0.f : exp_two(mw - m);
+                    ls += ml[q + RG * v][rr][1] * al;
 #pragma unroll
-                    for (int i = 0; i < DM; ++i) acc[i] += al * oj[v][rr][d0 + i];
+                    for (int i = 0; i < DM; ++i) acc[i] += al * oj[q + RG * v][rr][d0 + i];
                 }
-                put(16 * r + rr, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
+                put(row, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
             }
         }
         if (all == 2)
@@ -882,18 +915,14 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     // one chunk fall on distinct banks
     auto kswz = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
     auto vswz = [](int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
-    // K fragment (A of S^T): key row 32 tb + lr, chunk 2 ks + lh
-    int kaddr[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kaddr[ks] = lr * RB + 16 * ((2 * ks + lh) ^ kswz(lr));
+    // K fragment (A of S^T): key row 32 tb + lr, chunk 2 ks + lh: kaddr ^ 32 ks
+    const int kaddr = lr * RB + 16 * (lh ^ kswz(lr));
     // V^T fragment (A of O^T): 16-lane group gr reads keys 16 st + 4 (gr / 2) + s16 / 4 (and
-    // + 8) of dims 32 db + 16 (gr % 2) + 4 (s16 % 4) .. + 3 (transposing read)
-    int vaddr[DB];
+    // + 8) of dims 32 db + 16 (gr % 2) + 4 (s16 % 4) .. + 3 (transposing read): vaddr ^ 64 db
+    int vaddr;
     {
         const int gr = lane >> 4, s16 = lane & 15, vv = s16 >> 2, qq = s16 & 3, r = 4 * (gr >> 1) + vv;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-            vaddr[db] = KB + r * RB + 16 * ((4 * db + 2 * (gr & 1) + (qq >> 1)) ^ vswz(r)) + 8 * (qq & 1);
+        vaddr = r * RB + 16 * ((2 * (gr & 1) + (qq >> 1)) ^ vswz(r)) + 8 * (qq & 1);
     }
 
     int held = 0;                                          // which of the two pieces there are
@@ -923,24 +952,6 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         const int tok_a = quot(wa, grp), tok_b = quot(max(wb, wa), grp);
         const int lim_lo = a.causal ? sq.len - sq.n + tok_a : sq.len - 1;      // every row of the wave sees these
         const int lim_hi = wb < wa ? -1 : a.causal ? sq.len - sq.n + tok_b : sq.len - 1;
-
-        if constexpr (IDX) {
-            for (int i = tid; i < ROWS * (D / 32); i += NT) (&keep[0][0])[i] = 0;
-            __syncthreads();
-            read_lists<D, NT>(a, sq, kvh, row0, n_rows, keep);
-            __syncthreads();
-        }
-        uint4 qf[KS];
-        {
-            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                qf[ks] = make_uint4(0, 0, 0, 0);
-                if (on) qf[ks] = *reinterpret_cast<const uint4 *>(qp + 16 * ks + 8 * lh);
-                if constexpr (IDX) qf[ks] = keep8(qf[ks], keep[rr][ks >> 1] >> (16 * (ks & 1) + 8 * lh));
-                qf[ks].x ^= flip; qf[ks].y ^= flip; qf[ks].z ^= flip; qf[ks].w ^= flip;
-            }
-        }
 
         // ---- staging
         const int32_t *trow = a.table + w.b * a.table_ld;
@@ -1021,13 +1032,42 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                 *reinterpret_cast<uint4 *>(row + 16 * ((4 * mgrp + j) ^ swz)) = unpack_mx8(cw[j], sc);
         };
 
+        // the first tiles are on their way while the lists and queries are read
+        const int t0 = w.c0;
+        if constexpr (!MX) {
+            fetch(t0);
+            dma(slot0, t0);
+            dma(slot1, t0 + 1);
+        } else {
+            pbase = t0;
+            pcur = mx_pages(t0);
+            pnext = mx_pages(t0 + 16);
+            mx_load(t0);
+        }
+
+        if constexpr (IDX) {
+            read_lists<D, NT>(a, sq, kvh, row0, n_rows, keep);
+            lds_barrier();
+        }
+        uint4 qf[KS];
+        {
+            const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                qf[ks] = make_uint4(0, 0, 0, 0);
+                if (on) qf[ks] = *reinterpret_cast<const uint4 *>(qp + 16 * ks + 8 * lh);
+                if constexpr (IDX) qf[ks] = keep8(qf[ks], keep[rr][ks >> 1] >> (16 * (ks & 1) + 8 * lh));
+                qf[ks].x ^= flip; qf[ks].y ^= flip; qf[ks].z ^= flip; qf[ks].w ^= flip;
+            }
+        }
+
         // ---- one tile's work
         f32x16_t o[DB];
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-        float m_run = -__builtin_inff(), l_run = 0.f, least = 0.f;
+        float m_run = -__builtin_inff(), l_run = 0.f;
         f32x16_t s[2];
         uint4 pf[TK / 16];
         // s[tb][v] is key kt * TK + 32 tb + 8 (v / 4) + 4 lh + v % 4 of row lr
@@ -1036,7 +1076,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) kf[ks][tb] = *reinterpret_cast<const uint4 *>(slot + kaddr[ks] + 32 * tb * RB);
+                for (int tb = 0; tb < 2; ++tb) kf[ks][tb] = *reinterpret_cast<const uint4 *>(slot + (kaddr ^ (32 * ks)) + 32 * tb * RB);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
@@ -1046,12 +1086,6 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) s[tb] = mfma(kf[ks][tb], qf[ks], s[tb]);
-            if constexpr (IDX) {
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) least = fminf(least, s[tb][v]);
-            }
         };
         auto softmax = [&](int kt) __attribute__((always_inline)) {
             const int t0 = kt * TK;
@@ -1105,7 +1139,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             for (int st = 0; st < TK / 16; ++st)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    const char *p = slot + vaddr[db] + 16 * st * RB;
+                    const char *p = slot + KB + (vaddr ^ (64 * db)) + 16 * st * RB;
                     const s16x4_t lo = lds_read_tr16(p);
                     const s16x4_t hi = lds_read_tr16(p + 8 * RB);
                     vf[st][db] = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -1118,17 +1152,9 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         };
 
         // ---- the ring: tile c0 + i lives in slot i % 4
-        const int t0 = w.c0;
         if constexpr (!MX) {
-            fetch(t0);
-            dma(slot0, t0);
-            dma(slot1, t0 + 1);
             wait_vmcnt_le<PER>();
         } else {
-            pbase = t0;
-            pcur = mx_pages(t0);
-            pnext = mx_pages(t0 + 16);
-            mx_load(t0);
             mx_store(slot0);
             mx_load(t0 + 1);
         }
@@ -1170,7 +1196,9 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         const bool complete = w.complete();
         const int part = w.part();
         const float l = across_halves(l_run, add2);
-        bool odd = !(l < __builtin_inff()) || (IDX && least == -__builtin_inff());
+        // an infinite or NaN key or value that should not count has made these NaN (zero times
+        // it, in a score or a sum)
+        bool odd = !(l < __builtin_inff());
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -1316,10 +1344,10 @@ namespace {
 // Query rows per unit, by the average sequence's
 int unit_rows(int64_t T, int64_t B, int64_t grp) {
     const int64_t rows = (T * grp + B - 1) / B;
-    return rows <= 16 ? 16 : rows <= 128 ? 32 : rowsk::ROWS;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 64 : rowsk::ROWS;
 }
-int workgroups(int rows) { return rows <= 32 ? few::kGroups : rowsk::kGroups; }
-int block_keys(int rows) { return rows <= 32 ? few::TK : rowsk::TK; }
+int workgroups(int rows) { return rows <= 64 ? few::kGroups : rowsk::kGroups; }
+int block_keys(int rows) { return rows <= 64 ? few::TK : rowsk::TK; }
 // units at most: full row tiles, and a last one per sequence
 int64_t most_units(int64_t T, int64_t B, int64_t H, int64_t Hkv, int rows) {
     return T * H / rows + (T < B ? T : B) * Hkv;
@@ -1327,9 +1355,10 @@ int64_t most_units(int64_t T, int64_t B, int64_t H, int64_t Hkv, int rows) {
 
 template <int D, bool MX, int ROWS>
 hipError_t launch(const PagedArgs &a, hipStream_t stream) {
-    if constexpr (ROWS <= 32) {
-        if (a.idx) paged_few_kernel<D, MX, ROWS / 16, true><<<a.nw, few::kThreads, 0, stream>>>(a);
-        else paged_few_kernel<D, MX, ROWS / 16, false><<<a.nw, few::kThreads, 0, stream>>>(a);
+    if constexpr (ROWS <= 64) {
+        constexpr int R = ROWS == 16 ? 1 : 2, RG = ROWS / (16 * R);
+        if (a.idx) paged_few_kernel<D, MX, R, RG, true><<<a.nw, few::kThreads, 0, stream>>>(a);
+        else paged_few_kernel<D, MX, R, RG, false><<<a.nw, few::kThreads, 0, stream>>>(a);
     } else {
         if (a.idx) paged_rows_kernel<D, MX, true><<<a.nw, rowsk::NT, 0, stream>>>(a);
         else paged_rows_kernel<D, MX, false><<<a.nw, rowsk::NT, 0, stream>>>(a);
@@ -1344,6 +1373,7 @@ template <int D, bool MX>
 hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
     if (rows == 16) return launch<D, MX, 16>(a, stream);
     if (rows == 32) return launch<D, MX, 32>(a, stream);
+    if (rows == 64) return launch<D, MX, 64>(a, stream);
     return launch<D, MX, rowsk::ROWS>(a, stream);
 }
 
