@@ -111,7 +111,21 @@ __device__ __forceinline__ uint4 keep8(uint4 w, uint32_t m) {
     return w;
 }
 
+// x, in a form that keeps what depends on it inside the branch it is used in (a
+// rarely taken one would be turned into selects that every pass pays for)
+__device__ __forceinline__ int in_branch(int x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(x));
+#endif
+    return x;
+}
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(static_cast<uint64_t>(x) >> 32));
+    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
 // a / b of non-negative values
 __device__ __forceinline__ int quot(int a, int b) {
     return uniform(static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)));
@@ -697,11 +711,12 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[tb][i] = sc[tb][i] * a.c;
                 if (edge) {
+                    const int rel = in_branch(lim[r] - key - 8 * g);
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (key + 8 * g + 4 * tb + i > lim[r]) p[tb][i] = -__builtin_inff();
+                            if (4 * tb + i > rel) p[tb][i] = -__builtin_inff();
                 }
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
@@ -758,11 +773,11 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             }
             // a weight of zero does not silence what lies past the last key that some row sees
             if (key + TK - 1 > hi_lim) {
+                const int rel = in_branch(hi_lim - key - 8 * g);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = key + 8 * g + kk <= hi_lim ? vr[kk][q] : 0u;
-                asm volatile("" ::: "memory");             // a branch of its own: rarely taken
+                    for (int q = 0; q < DM / 2; ++q) vr[kk][q] = kk <= rel ? vr[kk][q] : 0u;
             }
 #pragma unroll
             for (int i = 0; i < DM; ++i) {
@@ -985,13 +1000,15 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             const int r = lane / CH, ch = lane % CH;
             const int key = kt * TK + wave * RPW;
             // rows past the last key that some row sees are staged as zeros
-            const int rows = kt < c_end ? max(0, min(RPW, kend - key)) : 0;
+            const int rows = uniform(kt < c_end ? max(0, min(RPW, kend - key)) : 0);
             const int64_t page = __builtin_amdgcn_readlane(pid, (kt - pbase) & 63);
             const int64_t at = (hrow + (key & (ps - 1))) * RB;
+            // (scalar by construction; said so, since a descriptor that may differ between lanes
+            // is loaded from in a loop over its values)
             const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
-                a.kv.k + page * a.kv.k_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
+                a.kv.k + uniform(page * a.kv.k_page + at), 0, static_cast<uint32_t>(rows * RB), 0x00020000);
             const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
-                a.kv.v + page * a.kv.v_page + at, 0, static_cast<uint32_t>(rows * RB), 0x00020000);
+                a.kv.v + uniform(page * a.kv.v_page + at), 0, static_cast<uint32_t>(rows * RB), 0x00020000);
 #pragma unroll
             for (int u = 0; u < RPW / RPI; ++u) {
                 const int row = wave * RPW + u * RPI;      // first row of the instruction in the tile
@@ -1098,7 +1115,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         auto softmax = [&](int kt) __attribute__((always_inline)) {
             const int t0 = kt * TK;
             if (t0 + TK - 1 > lim_lo) {                    // the tile crosses some row's limit
-                const int rel = lim - t0 - 4 * lh;
+                const int rel = in_branch(lim - t0 - 4 * lh);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
