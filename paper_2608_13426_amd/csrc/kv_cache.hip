@@ -35,6 +35,10 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 
 // ---- 8 elements of a head
+template <typename T>
+struct alignas(16) Raw8 {
+    T x[8];
+};
 __device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
     const uint4 q = *reinterpret_cast<const uint4 *>(p);
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -161,17 +165,55 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
     __shared__ __attribute__((aligned(16))) uint32_t amax_of[KV == 2 ? kThreads * 2 : 4];
 
     // tokens of this workgroup: block `blk` of the batch entry (without
-    // energies the whole call is one entry of T tokens)
+    // energies the whole call is one entry of T tokens), at most 64
     const int64_t unit = static_cast<int64_t>(blockIdx.x) / blocks, blk = static_cast<int64_t>(blockIdx.x) % blocks;
-    const int64_t per = ENERGY ? a.L : a.T;
-    const int64_t t_end = min(per, (blk + 1) * TB);
-    for (int64_t tt = blk * TB + wave; tt < t_end; tt += kWaves) {
-        const int64_t t = unit * per + tt;                 // wave-uniform
-        const int64_t b = ENERGY ? unit : static_cast<int64_t>(static_cast<uint32_t>(t) / static_cast<uint32_t>(a.L));
-        const int64_t l = t - b * a.L;
+    const int64_t per = ENERGY ? a.L : a.T, t0 = unit * per + blk * TB;
+    const int n = static_cast<int>(min(static_cast<int64_t>(TB), per - blk * TB));
+    // lane i holds the position and slot of token i
+    int pos_of = 0, slot_of = -1;
+    if (lane < n) {
+        if (a.rot) pos_of = a.pos[t0 + lane];
+        if constexpr (KV != 0) slot_of = a.slots[t0 + lane];
+    }
+    auto place = [&](int i, int64_t &b, int64_t &l) __attribute__((always_inline)) {
+        const int64_t t = t0 + i;
+        b = ENERGY ? unit : static_cast<int64_t>(static_cast<uint32_t>(t) / static_cast<uint32_t>(a.L));
+        l = t - b * a.L;
+    };
+    // a token's values, and the cos and sin that the lane's pairs take: of its first
+    // piece's eight pairs, or (adjacent pairs) of both pieces' four
+    struct Token {
+        Raw8<T> r1, r2;
+        float4 c1, c2, s1, s2;
+    };
+    const int ca = a.interleaved ? 4 * pc.c1 : 8 * pc.c1, cb = a.interleaved ? 4 * pc.c2 : 8 * pc.c1 + 4;
+    const bool turn1 = kind < 2 && a.rot && (a.interleaved ? 8 * pc.c1 < a.rot : pc.on);
+    const bool turn2 = kind < 2 && a.rot && (a.interleaved ? 8 * pc.c2 < a.rot : pc.on);
+    auto load = [&](Token &k, int i) __attribute__((always_inline)) {
+        int64_t b, l;
+        place(i, b, l);
+        const T *x = in + b * isb + l * ist;
+        k.r1 = *reinterpret_cast<const Raw8<T> *>(x + 8 * pc.c1);
+        k.r2 = *reinterpret_cast<const Raw8<T> *>(x + 8 * pc.c2);
+        if (a.rot) {
+            const int p = __builtin_amdgcn_readlane(pos_of, i);
+            const int64_t row = static_cast<int64_t>(p >= 0 && p < a.n_pos ? p : 0) * (a.rot / 2);
+            if (turn1) {
+                k.c1 = *reinterpret_cast<const float4 *>(a.cs + row + ca);
+                k.s1 = *reinterpret_cast<const float4 *>(a.sn + row + ca);
+            }
+            if (turn2) {
+                k.c2 = *reinterpret_cast<const float4 *>(a.cs + row + cb);
+                k.s2 = *reinterpret_cast<const float4 *>(a.sn + row + cb);
+            }
+        }
+    };
+    auto token = [&](const Token &k, int i) __attribute__((always_inline)) {
+        int64_t b, l;
+        place(i, b, l);
         float x1[8], x2[8];
-        load8(in + b * isb + l * ist + 8 * pc.c1, x1);
-        load8(in + b * isb + l * ist + 8 * pc.c2, x2);
+        load8(k.r1.x, x1);
+        load8(k.r2.x, x2);
         if constexpr (NORM) {
 #pragma clang fp contract(off)
             double ss = 0.0;
@@ -195,33 +237,19 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
         }
         if (a.rot) {
             // a position outside the tables gives NaN
-            const int p = a.pos[t];
-            const bool ok = p >= 0 && p < a.n_pos;
-            const int64_t row = static_cast<int64_t>(ok ? p : 0) * (a.rot / 2);
-            const float *cs = a.cs + row, *sn = a.sn + row;
-            const float bad = ok ? 1.f : __builtin_nanf("");
-            if (kind < 2) {
-                if (a.interleaved) {
+            const int p = __builtin_amdgcn_readlane(pos_of, i);
+            const float bad = p >= 0 && p < a.n_pos ? 1.f : __builtin_nanf("");
+            const float c[8] = {k.c1.x, k.c1.y, k.c1.z, k.c1.w, k.c2.x, k.c2.y, k.c2.z, k.c2.w};
+            const float s[8] = {k.s1.x, k.s1.y, k.s1.z, k.s1.w, k.s2.x, k.s2.y, k.s2.z, k.s2.w};
+            if (a.interleaved) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float(&x)[8] = h ? x2 : x1;
-                        const int c = h ? pc.c2 : pc.c1;
-                        if (8 * c < a.rot) {
-                            const float4 cc = *reinterpret_cast<const float4 *>(cs + 4 * c);
-                            const float4 ss = *reinterpret_cast<const float4 *>(sn + 4 * c);
-                            turn(x[0], x[1], cc.x * bad, ss.x * bad);
-                            turn(x[2], x[3], cc.y * bad, ss.y * bad);
-                            turn(x[4], x[5], cc.z * bad, ss.z * bad);
-                            turn(x[6], x[7], cc.w * bad, ss.w * bad);
-                        }
-                    }
-                } else if (pc.on) {
-                    float cc[8], ss[8];
-                    load8(cs + 8 * pc.c1, cc);
-                    load8(sn + 8 * pc.c1, ss);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) turn(x1[i], x2[i], cc[i] * bad, ss[i] * bad);
+                for (int j = 0; j < 4; ++j) {
+                    if (turn1) turn(x1[2 * j], x1[2 * j + 1], c[j] * bad, s[j] * bad);
+                    if (turn2) turn(x2[2 * j], x2[2 * j + 1], c[4 + j] * bad, s[4 + j] * bad);
                 }
+            } else if (turn1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) turn(x1[j], x2[j], c[j] * bad, s[j] * bad);
             }
         }
         if (act && direct) {
@@ -240,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
             }
         }
         if constexpr (KV != 0) {
-            const int slot = a.slots[t];
+            const int slot = __builtin_amdgcn_readlane(slot_of, i);
             const int page = slot >> a.kv.lg_page, off = slot & ((1 << a.kv.lg_page) - 1);
             const bool held = slot >= 0 && page < a.kv.n_pages && (kind == 1 || kind == 2);
             const int64_t row = (static_cast<int64_t>(head) << a.kv.lg_page) + off;
@@ -286,6 +314,14 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
                 }
             }
         }
+    };
+    // the next token is on its way while one is worked on
+    Token cur, next;
+    if (wave < n) load(cur, wave);
+    for (int i = wave; i < n; i += kWaves) {               // wave-uniform
+        if (i + kWaves < n) load(next, i + kWaves);
+        token(cur, i);
+        cur = next;
     }
 
     if constexpr (ENERGY) {
