@@ -379,11 +379,11 @@ __global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const i
 namespace {
 
 // Tokens per workgroup.  With energies each workgroup writes a float64 row of
-// columns and adds up its waves, so 256 workgroups at least, else as many tokens
-// as that leaves (us, kernel and final sum, for 256 / 512 / 1024 of them: 8192
-// tokens x 32 + 8 heads 32 + 4.8 / 32 + 4.7 / 34 + 4.7; 2 x 1001 x 16 + 8 with norms 12
-// + 4.4 / 14 + 5.7 / 14 + 5.7).  Without, 2048 (8192 tokens x 8 + 8 heads into a 4-bit
-// cache, 256 / 512 / 1024 / 2048: 25 / 16 / 14 / 12).
+// columns and adds up its waves: 256 workgroups at least, else as many tokens as
+// that leaves (kernel + final sum, us, for 256 / 512 / 1024: 8192 tokens x 32 + 8 heads
+// 41 + 5 / 42 + 5 / 42 + 5; 2 x 1001 x 32 + 8 15 + 4 / 17 + 4 / 20 + 6; the same x 16 + 8
+// with norms 13 + 4 / 15 + 6 / 15 + 6).  Without, 2048 (512 / 1024 / 2048 / 4096: 8192 x 32 +
+// 8 heads 41 / 45 / 40 / 43, 6000 tokens appended with their queries 40 / 37 / 36 / 39).
 int rotate_tokens(int64_t T, int64_t heads, int D, bool energy) {
     const int64_t groups = (heads + 1024 / D - 1) / (1024 / D);
     int tb = kWaves;
