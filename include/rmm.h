@@ -863,9 +863,9 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  *             multiple of the cache's Hkv, o's head count not H, k outside
  *             [1, D], a misaligned workspace; UNSUPPORTED for a cache or
  *             strides that break the rules above, max_pages * page_size > 2^30,
- *             T*H >= 2^31, or so many tokens against so long a table that
- *             their key blocks number 2^31 (T*H * max_pages*page_size below 2^39 is always
- *             taken); WORKSPACE_TOO_SMALL.
+ *             T*H >= 2^31, or where the key blocks to be walked could number
+ *             2^30 (at most (T*H/16 + min(T, B)*Hkv) * (max_pages*page_size/32 + 5));
+ *             WORKSPACE_TOO_SMALL.
  */
 size_t rmm_paged_attention_workspace_size(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D);
 rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_cache_t *cache,

@@ -990,7 +990,7 @@ def _heads(t: torch.Tensor, shape, dtype, name: str, what: str, batched: bool = 
     """rmm_heads_t of [T, heads, D] (batched: [batch, L, heads, D], or with
     head_first [batch, heads, L, D]), checked; strides of axes of one entry are
     never used."""
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must be {what}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")

@@ -153,7 +153,7 @@ __device__ __forceinline__ int prefix_sum(int x) {
 }
 
 // ---- the line.  TK keys per block, ROWS query rows per unit.  The host keeps its
-// length below 2^31 (line_fits).
+// length below 2^30 (paged_line_fits).
 struct Seq {
     int q0, n, len;                       // first token, new tokens, keys
     int bad;                              // longer than its row of the page table
@@ -1405,11 +1405,12 @@ hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
 
 }  // namespace
 
-// whether the line is shorter than 2^31 whatever the lengths (keys: what a page
-// table row can hold)
+// whether the line is shorter than 2^30 whatever the lengths (keys: what a page
+// table row can hold; a unit's share of its pair's length is at most four blocks
+// more than the keys')
 bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys) {
     const int rows = unit_rows(T, B, H / Hkv);
-    return (most_units(T, B, H, Hkv, rows) + 1) * (keys / block_keys(rows) + 3) < (int64_t(1) << 31) - 1024;
+    return (most_units(T, B, H, Hkv, rows) + 1) * (keys / block_keys(rows) + 5) < (int64_t(1) << 30);
 }
 
 // two pieces per workgroup: what joins them, their maxima and sums, their outputs

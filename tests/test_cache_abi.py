@@ -126,6 +126,9 @@ def test_attention_refusals():
     assert call(q=heads(6), o=heads(6)) == INVALID and call(o=heads(4)) == INVALID
     assert call(idx=P, k=0) == INVALID and call(idx=P, k=129) == INVALID
     assert call(width=2 ** 27, ld=2 ** 27) == UNSUPPORTED and call(T=2 ** 29, qs=P) == UNSUPPORTED
+    # 2^15 sequences of one token, 8 heads on 4 kv heads: 2^17 units of up to 2^13 blocks
+    assert call(T=2 ** 15, B=2 ** 15, width=2 ** 14, ld=2 ** 14) == UNSUPPORTED
+    assert call(T=2 ** 15, B=2 ** 15, width=2 ** 12, ld=2 ** 12, ws=None) == WS_SMALL
     assert call(table=ctypes.c_void_p(A + 2)) == UNSUPPORTED
     assert call(ws=None) == WS_SMALL and call(n=need - 1) == WS_SMALL
     assert call(ws=ctypes.c_void_p(A + 16)) == INVALID
