@@ -56,7 +56,7 @@ struct PagedArgs {
     float *part_o, *part_ml;               // their outputs, their (max, sum)
     int nw, whole;                         // workgroups; whether no unit is cut
 };
-bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys);
+bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, bool mx, int D, int64_t keys);
 size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D);
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream);
 

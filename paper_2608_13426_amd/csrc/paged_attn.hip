@@ -6,12 +6,14 @@
 // A query row is one (new token, query head of a kv head): the heads of a group
 // share every key read.  A unit is one (sequence, kv head, tile of query rows).
 //
-//   up to 128 rows (a decode step, drafted tokens): paged_few_kernel, units of 16
-//   to 128 rows.  The four waves of a workgroup take 32-key chunks in turn; keys and
-//   values go from memory to registers to the matrix cores without LDS.  Bound by
-//   reading the cache.
-//   more rows (prompt chunks): paged_rows_kernel, 32 rows per wave, 64-key tiles
-//   staged once per workgroup in an LDS ring.
+//   few rows (a decode step, drafted tokens): paged_few_kernel, units of 16 to 64
+//   rows.  The four waves of a workgroup take 32-key chunks in turn; keys and values
+//   go from memory to registers to the matrix cores without LDS.  Bound by reading
+//   the cache.
+//   more rows (prompt chunks): paged_rows_kernel, units of 256 rows, 32 per wave,
+//   over 64-key tiles staged once per workgroup in an LDS ring.  Bound by the matrix
+//   cores and the exponentials beside them.
+// unit_rows says which, with what both measured.
 //
 // Lengths are known on the device only, and a batch may hold one long sequence
 // among short ones, so the work is cut there: the key blocks of all units lie on
@@ -38,7 +40,9 @@ namespace {
 namespace pg {
 constexpr float kTau = 8.f;               // lazy-rescale threshold, log2 units
 // Units of at most kShort blocks, no more of them than workgroups, are never cut
-// (the host then leaves out the joining launch: 5 us of a 12 us call).
+// (the host then leaves out the joining launch).  One token, 32 heads of 128 on 8:
+// 500 keys uncut 11.3 us, cut 9.9 + 3.9 and a launch; 1000 keys uncut 16.4, cut
+// 10.0 + 3.9, which is even with the launch and leaves the card to others.
 constexpr int kShort = 16;
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
@@ -481,8 +485,15 @@ __device__ __forceinline__ void wait_vmcnt_le() {
 // ------------------------------------------------------------- few rows
 namespace few {
 constexpr int kWaves = 4, kThreads = 64 * kWaves, TK = 32;
-constexpr int kGroups = 512;              // workgroups: two per CU
-constexpr int kMinRun = 8;                // chunks: two rounds of the four waves
+// Workgroups: two per CU, what the registers allow at once.  More wait their turn:
+// 64 sequences of up to 1000 keys 43 us with 512, 54 with 768, 51 with 1024.
+constexpr int kGroups = 512;
+// Chunks in a run at least: two rounds of the four waves.  Half of it is 1 us
+// faster at 1000 keys (9.1 for 10.0) and 3 slower at 8192 in the joining launch
+// (7.4 for 4.8); twice is slower at both (12.5; 14.8 for 13.0).
+constexpr int kMinRun = 8;
+// What a cut unit costs, in chunks: 64 sequences of up to 1000 keys 43 us, 47 with
+// 4, 43 with 16 (a unit's halves then end later than whole units elsewhere).
 constexpr int kCutCost = 8;
 }  // namespace few
 
@@ -494,6 +505,10 @@ constexpr int kCutCost = 8;
 // its lane group contributes to O^T = V^T P^T: the weights stay where they are.
 // The value rows, loaded as rows, are turned 8 x 8 in registers (v_perm).  4-bit
 // codes become bf16 with v_cvt_scalef32_pk_bf16_fp4 (exact, the scale included).
+// Bound by reading the cache, 16 bytes per lane and load, a wave's next chunk on
+// its way while one is used.  32 heads of 128 on 8, one token per sequence: 16
+// sequences of up to 8000 keys (318 MB) 65 us, 4.9 TB/s, and 6 joining; two of
+// 131000 in 4 bits (285 MB) 62 us, 4.6 TB/s, and 6; one of 200 8.6 us, all latency.
 // R: 16-row tiles per wave, which share each key and value fragment (their queries
 // are then kept in LDS); RG: groups of waves with rows of their own, which walk the
 // same chunks side by side, so that all but the first read them from a cache;
@@ -903,7 +918,10 @@ namespace rowsk {
 constexpr int NW = 8, NT = 64 * NW;       // waves of 32 query rows
 constexpr int ROWS = 32 * NW, TK = 64, NS = 4;    // rows per unit, keys per tile, ring slots
 constexpr int kGroups = 256;              // workgroups: one per CU
-constexpr int kMinRun = 4, kCutCost = 16; // tiles
+// In tiles.  Cutting costs a unit's 256 rows of partial sums written and read: a
+// prompt of 4096 tokens, 32 heads, takes 166 + 5 us uncut and 192 + 42 cut.  Three
+// sequences of 700 tokens behind up to 3300: cut 102 + 20, uncut (cost 32) 123 + 5.
+constexpr int kMinRun = 4, kCutCost = 16;
 }  // namespace rowsk
 
 // Eight waves of 32 query rows over a ring of 64-key tiles in LDS, each filled two
@@ -913,6 +931,10 @@ constexpr int kMinRun = 4, kCutCost = 16; // tiles
 // the keys of tile i and the values of tile i - 1; the two halves of the
 // workgroup take the softmax at opposite ends of a step, so that one's
 // exponentials meet the other's matrix instructions.
+// Two prompts' chunks of 1024 tokens behind 7000 cached ones, 32 heads of 128 on 8
+// (239 GFLOP): 240 to 280 us, 850 to 990 TFLOP/s of the 1103 that a large product
+// reaches, and 5 joining; from a 4-bit cache 342, since the tiles then pass through
+// registers.  At 256 registers per lane a larger tile of either kind spills.
 template <int D, bool MX, bool IDX>
 __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     using namespace pg;
@@ -1290,7 +1312,9 @@ constexpr int joins(int rows) { return (rows + 31) / 32; }
 // unit cut over workgroups first .. first + n - 1 takes the rows i - first, + n, ...,
 // of which the YS workgroups (i, y) take every YS-th (a 256-row unit has too many for one).
 // D / 4 lanes take a row's dims; RP rows are joined at once, each by SP of the
-// workgroup's groups of lanes (which take every SP-th piece)
+// workgroup's groups of lanes (which take every SP-th piece).
+// Bound by latency (descriptors, then maxima and sums, then outputs): 4 us where
+// nothing was cut, 6 for 16 sequences of one token, up to 20 for 256-row units all cut.
 template <int D, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     using namespace pg;
@@ -1367,10 +1391,25 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
 
 namespace {
 
-// Query rows per unit, by the average sequence's
-int unit_rows(int64_t T, int64_t B, int64_t grp) {
+// Query rows per unit, by the average sequence's.  A unit reads its keys once, so
+// small ones repeat reads (partly from a cache) and large ones spend matrix work and
+// registers on rows that are not there.  Measured (us, heads of 128, 8 sequences of
+// up to 9000 keys unless said, without the joining launch):
+//   bf16    16 rows: 16 per unit 37, 32: 38;   24 rows: 42, 41;   40 rows: 64, 46
+//   bf16    32 rows: 32 per unit 40, 256: 44;  64 rows: 49, 46;  128 rows: 72, 51
+//           64 sequences: 24 rows 80, 93;  40 rows 122, 98;  128 rows 210, 116
+//   4-bit   64 sequences: 24 rows, 16 per unit 59, 32: 50, 64: 60;  40 rows: 82, 81, 72
+//   4-bit   64 per unit against 256: 128 rows 54, 72;  256 rows 57, 74;  32 sequences
+//           of 256 rows 192, 179;  512 rows 100, 104.  Heads of 64: 40 rows 28, 30;
+//           64 rows 91, 121;  128 rows 42, 34
+// With a bf16 cache units of 64 rows were no better than 32 or 256 anywhere (40 rows
+// 47, 128 rows 66, 64 sequences of 40 rows 95): there is none.  A 4-bit cache keeps
+// them, since a 256-row unit turns every key into bf16 through registers into LDS.
+int unit_rows(int64_t T, int64_t B, int64_t grp, bool mx, int D) {
     const int64_t rows = (T * grp + B - 1) / B;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 64 : rowsk::ROWS;
+    if (rows <= 16) return 16;
+    if (rows <= 32) return 32;
+    return mx && rows <= (D == 128 ? 256 : 64) ? 64 : rowsk::ROWS;
 }
 int workgroups(int rows) { return rows <= 64 ? few::kGroups : rowsk::kGroups; }
 int block_keys(int rows) { return rows <= 64 ? few::TK : rowsk::TK; }
@@ -1399,7 +1438,9 @@ template <int D, bool MX>
 hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
     if (rows == 16) return launch<D, MX, 16>(a, stream);
     if (rows == 32) return launch<D, MX, 32>(a, stream);
-    if (rows == 64) return launch<D, MX, 64>(a, stream);
+    if constexpr (MX) {
+        if (rows == 64) return launch<D, MX, 64>(a, stream);
+    }
     return launch<D, MX, rowsk::ROWS>(a, stream);
 }
 
@@ -1408,20 +1449,25 @@ hipError_t launch_rows(const PagedArgs &a, int rows, hipStream_t stream) {
 // whether the line is shorter than 2^30 whatever the lengths (keys: what a page
 // table row can hold; a unit's share of its pair's length is at most four blocks
 // more than the keys')
-bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t keys) {
-    const int rows = unit_rows(T, B, H / Hkv);
+bool paged_line_fits(int64_t T, int64_t B, int64_t H, int64_t Hkv, bool mx, int D, int64_t keys) {
+    const int rows = unit_rows(T, B, H / Hkv, mx, D);
     return (most_units(T, B, H, Hkv, rows) + 1) * (keys / block_keys(rows) + 5) < (int64_t(1) << 30);
 }
 
 // two pieces per workgroup: what joins them, their maxima and sums, their outputs
+// (the same size for both types of cache)
 size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D) {
-    const int rows = unit_rows(T, B, H / Hkv);
-    const size_t n = 2 * static_cast<size_t>(workgroups(rows));
-    return n * (sizeof(pg::PieceOf) + static_cast<size_t>(rows) * (D + 2) * sizeof(float));
+    size_t bytes = 0;
+    for (bool mx : {false, true}) {
+        const int rows = unit_rows(T, B, H / Hkv, mx, D);
+        const size_t n = 2 * static_cast<size_t>(workgroups(rows));
+        bytes = std::max(bytes, n * (sizeof(pg::PieceOf) + static_cast<size_t>(rows) * (D + 2) * sizeof(float)));
+    }
+    return bytes;
 }
 
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream) {
-    const int rows = unit_rows(a.T, a.B, a.q.n / a.kv.Hkv);
+    const int rows = unit_rows(a.T, a.B, a.q.n / a.kv.Hkv, a.kv.mx, D);
     a.nw = workgroups(rows);
     a.whole = (static_cast<int64_t>(a.width) << a.kv.lg_page) <= pg::kShort * block_keys(rows) &&
               most_units(a.T, a.B, a.q.n, a.kv.Hkv, rows) <= a.nw;

@@ -83,10 +83,10 @@ def _check(O, cache, table, lens, news, Q, scale, causal, idx):
     ([600, 300], [200, 129], 4, 1, 64, 64, True, None, None),          # prompt chunks: 256-row tiles
     ([2500], [2500], 2, 1, 64, 32, True, None, None),                  # a whole prompt: 20 tiles in pairs, cut
     ([1300, 40], [1300, 1], 2, 1, 128, 16, True, None, None),          # 11 tiles: one without a partner
-    ([700, 20], [33, 90], 4, 2, 128, 16, True, 0.5, None),             # 128-row tiles; more new tokens than keys
+    ([700, 20], [33, 90], 4, 2, 128, 16, True, 0.5, None),             # more new tokens than keys, full and partial row tiles
     ([1500, 2100, 64], [70, 60, 1], 4, 4, 64, 64, False, None, None),
     ([300, 5], [80, 70], 6, 1, 128, 128, True, 0.25, -0.2),            # 256-row tiles with lists
-    ([2200], [40], 1, 1, 128, 256, True, None, None),                  # 64-row tiles over many workgroups
+    ([2200], [40], 1, 1, 128, 256, True, None, None),                  # 40 rows over many workgroups
 ])
 def test_attention(lens, news, H, Hkv, D, page, causal, r, scale, mx):
     dev = require_gpu()
