@@ -68,6 +68,21 @@ def test_rotate(batch, L, H, Hkv, D, rot, inter, norm, dtype):
     assert torch.allclose(e, e2, rtol=2 * (L + 1) * 2.0 ** -53, atol=0)
 
 
+def test_energies_of_many_sequences():
+    """More sequences than a grid's second axis holds, each over two workgroups' tokens."""
+    dev = require_gpu()
+    batch, L, D = 65537, 65, 64
+    Q = _randn(_gen(dev, 9), dev, batch, L, 1, D).bfloat16()
+    Qo = torch.empty(batch, 1, L, D, dtype=Q.dtype, device=dev)
+    cos, sin = rmm.rope_tables(128, D, device=dev)
+    pos = torch.arange(L, dtype=torch.int32, device=dev).repeat(batch)
+    e = torch.empty(batch * D, dtype=torch.float64, device=dev)
+    rmm.rmm_qk_norm_rope(Q, Qo, pos, rmm.Rope(cos, sin), energy=e)
+    want, err = cr.rotate(cr.np64(Q[-2:]).reshape(2 * L, 1, D), None, pos[:2 * L].cpu().numpy(), cr.np64(cos), cr.np64(sin), False)
+    _check(cr.np64(Qo[-2:]).reshape(want.shape), want, err, Q.dtype)
+    check_energies(e.cpu().numpy(), (Qo.double() ** 2).sum(2).reshape(-1).cpu().numpy(), L)
+
+
 def test_rotate_positions_and_nonfinite():
     """Positions outside the tables give NaN heads; a NaN or infinite value stays in its pair (or, normed, head)."""
     dev = require_gpu()
