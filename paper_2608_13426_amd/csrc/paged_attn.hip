@@ -446,31 +446,41 @@ __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, 
 }
 
 // The retained dims of a unit's rows as bits; dims outside [0, D) are ignored.  16
-// lanes per row, each with up to D / 16 entries of its list, all asked for at once.
-template <int D, int NT>
+// lanes per row, each with up to D / 16 entries of its list, up to four rows' lists
+// per lane asked for at once (whole waves together).
+template <int D, int NT, int ROWS>
 __device__ __forceinline__ void read_lists(const PagedArgs &a, const Seq &sq, int kvh, int row0, int n_rows, uint32_t (*keep)[D / 32]) {
-    constexpr int E = D / 16, W = D / 32;
-    const int H = a.q.n, grp = H / a.kv.Hkv, u0 = threadIdx.x & 15;
-    for (int r = threadIdx.x >> 4; r < (n_rows + 3) / 4 * 4; r += NT / 16) {     // whole waves together
-        const int q = row0 + min(r, n_rows - 1);
-        const int32_t *list = a.idx + (static_cast<int64_t>(sq.q0 + q / grp) * H + kvh * grp + q % grp) * a.k;
-        int d[E];
+    constexpr int E = D / 16, W = D / 32, STEP = NT / 16;
+    constexpr int M = ROWS <= STEP ? 1 : ROWS <= 2 * STEP ? 2 : 4;
+    const int H = a.q.n, grp = H / a.kv.Hkv, u0 = threadIdx.x & 15, n4 = (n_rows + 3) / 4 * 4;
+    for (int r = threadIdx.x >> 4; r < n4; r += M * STEP) {
+        int d[M][E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) d[i] = u0 + 16 * i < a.k ? list[u0 + 16 * i] : -1;
-        uint32_t w[W];
+        for (int m = 0; m < M; ++m) {
+            if (r + m * STEP >= n4) break;
+            const int q = row0 + min(r + m * STEP, n_rows - 1);
+            const int32_t *list = a.idx + (static_cast<int64_t>(sq.q0 + q / grp) * H + kvh * grp + q % grp) * a.k;
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            w[j] = 0;
-#pragma unroll
-            for (int i = 0; i < E; ++i) w[j] |= (d[i] >> 5) == j ? 1u << (d[i] & 31) : 0u;
-            w[j] = or_row<0xB1>(w[j]);                     // over the 16 lanes: l ^ 1, l ^ 2, mirrored in 8, in 16
-            w[j] = or_row<0x4E>(w[j]);
-            w[j] = or_row<0x141>(w[j]);
-            w[j] = or_row<0x140>(w[j]);
+            for (int i = 0; i < E; ++i) d[m][i] = u0 + 16 * i < a.k ? list[u0 + 16 * i] : -1;
         }
-        if (r < n_rows && u0 == 0) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) keep[r][j] = w[j];
+        for (int m = 0; m < M; ++m) {
+            if (r + m * STEP >= n4) break;
+            uint32_t w[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                w[j] = 0;
+#pragma unroll
+                for (int i = 0; i < E; ++i) w[j] |= (d[m][i] >> 5) == j ? 1u << (d[m][i] & 31) : 0u;
+                w[j] = or_row<0xB1>(w[j]);                 // over the 16 lanes: l ^ 1, l ^ 2, mirrored in 8, in 16
+                w[j] = or_row<0x4E>(w[j]);
+                w[j] = or_row<0x141>(w[j]);
+                w[j] = or_row<0x140>(w[j]);
+            }
+            if (r + m * STEP < n_rows && u0 == 0) {
+#pragma unroll
+                for (int j = 0; j < W; ++j) keep[r + m * STEP][j] = w[j];
+            }
         }
     }
 }
@@ -656,10 +666,6 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
         if (c < c_stop) first();
 
         // ---- the unit's query rows
-        if constexpr (IDX) {
-            read_lists<D, kThreads>(a, sq, kvh, row0, n_rows, keep);
-            lds_barrier();
-        }
         // dims that lane (col, g) holds at contraction step s
         auto dim_of = [&](int s) { return MX ? (D / 4) * g + 8 * s : 32 * s + 8 * g; };
         auto query = [&](int r, int s) __attribute__((always_inline)) {
@@ -667,18 +673,30 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             if (rr >= n_rows) return make_uint4(0, 0, 0, 0);
             const int rho = row0 + rr, tok = rho / grp;
             const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + (kvh * grp + rho - tok * grp) * a.q.sh;
-            uint4 x = *reinterpret_cast<const uint4 *>(qp + dim_of(s));
-            if constexpr (IDX) x = keep8(x, keep[rr][dim_of(s) >> 5] >> (dim_of(s) & 31));
+            return *reinterpret_cast<const uint4 *>(qp + dim_of(s));
+        };
+        auto kept = [&](int r, int s, uint4 x) __attribute__((always_inline)) {
+            if constexpr (IDX) return keep8(x, keep[16 * r + col][dim_of(s) >> 5] >> (dim_of(s) & 31));
             return x;
         };
-        uint4 qf[R > 1 ? 1 : KS];
-        if constexpr (R == 1) {
+        // the queries that this wave reads: all of its rows' (R = 1), or its share of the unit's
+        constexpr int NQ = R > 1 ? R * RG * KS / kWaves : KS;
+        uint4 qf[NQ];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s] = query(0, s);
-        } else {
-            for (int i = wave; i < R * RG * KS; i += kWaves) qs[i / KS][i % KS][lane] = query(i / KS, i % KS);
+        for (int i = 0; i < NQ; ++i) qf[i] = R > 1 ? query((wave + kWaves * i) / KS, (wave + kWaves * i) % KS) : query(0, i);
+        if constexpr (IDX) {
+            read_lists<D, kThreads, ROWS>(a, sq, kvh, row0, n_rows, keep);
             lds_barrier();
         }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            if constexpr (R == 1) qf[i] = kept(0, i, qf[i]);
+            else {
+                const int r = (wave + kWaves * i) / KS, s = (wave + kWaves * i) % KS;
+                qs[r][s][lane] = kept(r, s, qf[i]);
+            }
+        }
+        if constexpr (R > 1) lds_barrier();
         f32x4_t o[R][DM];
         float m_run[R], l_run[R];
 #pragma unroll
@@ -1092,10 +1110,6 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             mx_load(t0);
         }
 
-        if constexpr (IDX) {
-            read_lists<D, NT>(a, sq, kvh, row0, n_rows, keep);
-            lds_barrier();
-        }
         uint4 qf[KS];
         {
             const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
@@ -1103,6 +1117,13 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             for (int ks = 0; ks < KS; ++ks) {
                 qf[ks] = make_uint4(0, 0, 0, 0);
                 if (on) qf[ks] = *reinterpret_cast<const uint4 *>(qp + 16 * ks + 8 * lh);
+            }
+            if constexpr (IDX) {
+                read_lists<D, NT, ROWS>(a, sq, kvh, row0, n_rows, keep);
+                lds_barrier();
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
                 if constexpr (IDX) qf[ks] = keep8(qf[ks], keep[rr][ks >> 1] >> (16 * (ks & 1) + 8 * lh));
                 qf[ks].x ^= flip; qf[ks].y ^= flip; qf[ks].z ^= flip; qf[ks].w ^= flip;
             }
