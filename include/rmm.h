@@ -847,6 +847,9 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * it (only the order of its sums may change).
  * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
  * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.
+ * How rows are grouped follows the average T*H / (B*Hkv): where long prompts and
+ * single tokens come together, a call for each kind is faster (255 sequences of
+ * one token and one of 700: 811 us, 511 as two calls; 63 and one of 512: 237, 216).
  *
  * Rows of o that belong to no sequence are left as they were.  q_start is
  * ascending from 0 (what it says past T is cut off); a length < 0 counts as 0.  A length beyond max_pages *

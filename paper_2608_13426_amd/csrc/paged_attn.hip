@@ -1136,6 +1136,9 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
         float m_run = -__builtin_inff(), l_run = 0.f;
+        // the sum is of the rounded weights where that costs nothing (two chunks of 1024
+        // tokens, heads of 64: 204 us either way; heads of 128: 284 against 257, so of the unrounded)
+        constexpr bool ROUNDED = D == 64;
         f32x16_t s[2];
         uint4 pf[TK / 16];
         // s[tb][v] is key kt * TK + 32 tb + 8 (v / 4) + 4 lh + v % 4 of row lr
@@ -1183,7 +1186,6 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                 m_run = need ? mt : m_run;
             }
             const float mu = m_run == -__builtin_inff() ? 0.f : m_run;
-            // (summed before their rounding: after it, as in the other kernel, took 4 % longer)
             float l4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
@@ -1191,9 +1193,9 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                 for (int v = 0; v < 16; ++v) {
                     const float p = exp_two(__builtin_fmaf(s[tb][v], c, -mu));
                     s[tb][v] = p;
-                    l4[v & 3] += p;
+                    if constexpr (!ROUNDED) l4[v & 3] += p;
                 }
-            l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            if constexpr (!ROUNDED) l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
             // weights of keys 16 st + 8 (e / 4) + 4 lh + e % 4: the order of the V^T fragments
 #pragma unroll
             for (int st = 0; st < TK / 16; ++st) {
@@ -1218,6 +1220,17 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             for (int st = 0; st < TK / 16; ++st)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) o[db] = mfma(vf[st][db], pf[st], o[db]);
+            if constexpr (ROUNDED) {
+                float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < TK / 16; ++st) {
+                    l4[0] = add_pair(pf[st].x, l4[0]);
+                    l4[1] = add_pair(pf[st].y, l4[1]);
+                    l4[2] = add_pair(pf[st].z, l4[2]);
+                    l4[3] = add_pair(pf[st].w, l4[3]);
+                }
+                l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            }
         };
 
         // ---- the ring: tile c0 + i lives in slot i % 4
