@@ -212,6 +212,31 @@ def test_gather_reads_every_scale():
 
 
 @pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("T,Hkv,D", [(4101, 8, 128), (8203, 8, 64), (13120, 5, 128)])
+def test_gather_many(T, Hkv, D, mx):
+    """Several rows per thread: what reading the same slots in short runs gives, nothing past the end."""
+    dev = require_gpu()
+    g = _gen(dev, T)
+    raw, cache = _cache(dev, 40, Hkv, 32, D, mx, True)
+    for t in raw[:2]:
+        t.copy_(torch.randint(0, 256, t.shape, device=dev, generator=g).to(t.dtype))
+    for t in raw[2:]:
+        t.copy_(torch.randint(100, 140, t.shape, device=dev, generator=g).to(t.dtype))
+    slots = torch.randint(-20, 40 * 32 + 20, (T,), device=dev, generator=g, dtype=torch.int32)
+    K = torch.full((Hkv, T + 1, D), 3.0, dtype=torch.bfloat16, device=dev)
+    V = torch.full((T + 1, Hkv, D), 3.0, dtype=torch.bfloat16, device=dev)
+    rmm.rmm_kv_gather(cache, slots, K[:, :T].transpose(0, 1), V[:T])
+    k, v = (torch.empty(1000, Hkv, D, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    for t in range(0, T, 1000):
+        n = min(1000, T - t)
+        rmm.rmm_kv_gather(cache, slots[t:t + n], k[:n], v[:n])
+        assert torch.equal(K[:, t:t + n].transpose(0, 1), k[:n]) and torch.equal(V[t:t + n], v[:n])
+    assert bool((K[:, T] == 3.0).all()) and bool((V[T] == 3.0).all())
+    out = (slots < 0) | (slots >= 40 * 32)
+    assert bool((V[:T][out] == 0).all()) and bool((V[:T][~out] != 0).any())
+
+
+@pytest.mark.parametrize("mx", [False, True])
 def test_same_slot_twice(mx):
     """Each 8-element piece of a slot named twice is one of its tokens'."""
     dev = require_gpu()
