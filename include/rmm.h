@@ -852,9 +852,10 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * one token and one of 700: 811 us, 511 as two calls; 63 and one of 512: 237, 216).
  *
  * Rows of o that belong to no sequence are left as they were.  q_start is
- * ascending from 0 (what it says past T is cut off); a length < 0 counts as 0.  A length beyond max_pages *
- * page_size, or a page number outside the cache among the pages a sequence
- * uses, makes its outputs NaN.  Any dim outside [0, D) in a list is ignored.
+ * ascending from 0 (what it says past T is cut off); a length < 0 counts as 0.
+ * A length beyond max_pages * page_size makes its sequence's outputs NaN, a page
+ * number outside the cache those of the tokens that see a key of it (and may make
+ * others of that sequence NaN).  Any dim outside [0, D) in a list is ignored.
  *
  * q, o      : [T] bf16, H heads (batch_stride unused; o may be q).
  * page_table: int32 [B][table_stride], max_pages entries used per row.

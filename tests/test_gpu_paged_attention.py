@@ -130,6 +130,27 @@ def test_strided(mx):
 
 
 @pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("news,r", [([1, 1, 1], None), ([6, 9, 1], 0.5), ([45, 60, 20], None), ([700, 300, 1], 0.5)])
+def test_in_place(news, r, mx):
+    """o may be q: units kept whole, units cut over workgroups, and ones that are redone."""
+    dev = require_gpu()
+    lens, H, Hkv, D, page = [max(n, 40 + 700 * i) for i, n in enumerate(news)], 8, 2, 128, 32
+    cache, table, q_start, Q, idx = _setup(dev, lens, news, H, Hkv, D, page, mx, 11, r=r)
+    length = torch.tensor(lens, dtype=torch.int32, device=dev)
+    last = (table[0, (lens[0] - 1) // page] * page + (lens[0] - 1) % page).view(1)
+    bad = torch.full((1, Hkv, D), float("nan"), dtype=torch.bfloat16, device=dev)
+    for redo in (False, True):
+        if redo:
+            rmm.rmm_kv_append(bad, bad, last, cache)
+        O = torch.empty_like(Q)
+        rmm.rmm_paged_attention(Q, cache, table, length, O, q_start=q_start, idx=idx)
+        R = Q.clone()
+        rmm.rmm_paged_attention(R, cache, table, length, R, q_start=q_start, idx=idx)
+        assert torch.equal(R.view(torch.int16), O.view(torch.int16))
+        assert redo == bool(O.isnan().any())
+
+
+@pytest.mark.parametrize("mx", [False, True])
 @pytest.mark.parametrize("n", [2, 21, 40, 75])
 def test_masked_nonfinite_keys_and_values(mx, n):
     """What a token does not see has no effect on it, infinite or NaN (but on the order of its sums)."""
@@ -202,6 +223,26 @@ def test_bad_pages_and_lengths(mx):
     rmm.rmm_paged_attention(Q, cache, t2, l2, O2)
     assert O2[:3].isnan().all()
     assert torch.equal(O2[3], O[3]) and bool((O2[4] == 0).all())
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("n,D", [(30, 128), (70, 64), (300, 128)])
+def test_bad_pages_of_prompts(n, D, mx):
+    """The same with many new tokens: the tokens that see the page are NaN, other sequences as they were."""
+    dev = require_gpu()
+    lens, H, Hkv, page = [n, 3000, n, n, 20], 8, 4, 16
+    cache, table, q_start, Q, _ = _setup(dev, lens, [n] * 5, H, Hkv, D, page, mx, 6)
+    table = table[:, :190].contiguous()
+    O = torch.empty_like(Q)
+    t2, l2 = table.clone(), torch.tensor(lens, dtype=torch.int32, device=dev)
+    t2[0, 1], t2[1, 100], l2[2], l2[4] = cache.n_pages, -1, 190 * page + 1, -5
+    # (the same lengths: the order of the sums follows them)
+    rmm.rmm_paged_attention(Q, cache, table, l2, O, q_start=q_start)
+    O2 = torch.empty_like(Q)
+    rmm.rmm_paged_attention(Q, cache, t2, l2, O2, q_start=q_start)
+    o, o2 = O.split(n), O2.split(n)
+    assert o2[0][page:].isnan().all() and o2[1].isnan().all() and o2[2].isnan().all()
+    assert torch.equal(o2[3], o[3]) and bool((o2[4] == 0).all())
 
 
 def test_q_start_past_the_tokens():
