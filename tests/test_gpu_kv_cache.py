@@ -252,6 +252,26 @@ def test_same_slot_twice(mx):
     assert pieces.any(0).all()
 
 
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("T", [1, 37, 700])
+def test_append_queries_in_place(T, mx):
+    """Queries rotated where they lie, in the same rows as the keys and values that are appended."""
+    dev = require_gpu()
+    H, Hkv, D = 6, 2, 128
+    rows = _randn(_gen(dev, T), dev, T, H + 2 * Hkv, D).bfloat16()
+    slots = torch.arange(T, dtype=torch.int32, device=dev)
+    rope = rmm.Rope(*rmm.rope_tables(1000, D, device=dev))
+    got = []
+    for place in (False, True):
+        x = rows.clone()
+        q = x[:, :H] if place else torch.empty(T, H, D, dtype=x.dtype, device=dev)
+        cache = rmm.kv_cache(-(-T // 16), Hkv, 16, D, mx=mx, device=dev)
+        rmm.rmm_kv_append(x[:, H:H + Hkv], x[:, H + Hkv:], slots, cache, positions=slots, rope=rope, Q=x[:, :H], Qo=q)
+        assert torch.equal(x[:, H:], rows[:, H:])
+        got.append((q.clone(), cache.k, cache.v))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_large_cache_offsets():
     """A cache past 4 GiB: the last page is written, read and attended."""
     dev = require_gpu()
