@@ -198,6 +198,16 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _scratch(n: int, device: torch.device, stream, dtype=torch.uint8) -> torch.Tensor:
+    """n elements for a call on `stream` (None: the current one), from that stream's
+    pool: a block that the pool hands out again is then still in use at most by
+    earlier work of the same stream, which the call follows."""
+    if stream is None:
+        return torch.empty(max(n, 1), dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(n, 1), dtype=dtype, device=device)
+
+
 def _rows(t: torch.Tensor, name: str):
     """View a [U, M, K] or [M, K] tensor as U units of M rows with stride ldx."""
     if t.dim() == 2:
@@ -319,7 +329,9 @@ def rmm_check_indices(idx: torch.Tensor, K: int, bad: torch.Tensor | None = None
         raise ValueError("idx must be contiguous int32 [B, k]")
     B, k = idx.shape
     if bad is None:
-        bad = torch.empty(B, dtype=torch.int32, device=idx.device)
+        bad = _scratch(B, idx.device, stream, torch.int32)[:B]
+        if stream is not None:              # the caller reads it on the current one
+            bad.record_stream(torch.cuda.current_stream(idx.device))
     d = _dev(idx, bad)
     if bad.dtype != torch.int32 or bad.numel() != B or not bad.is_contiguous():
         raise ValueError("bad must be contiguous int32 [B]")
@@ -370,7 +382,7 @@ def rmm_reduced_gemv(X: torch.Tensor, W: torch.Tensor, idx: torch.Tensor, Y: tor
     k = idx.numel() // B
     if workspace is None:
         need = rmm_gemv_workspace_size(B, M, N, k)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=d)
+        workspace = _scratch(need, d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_reduced_gemv", lib.rmm_reduced_gemv(
         X.data_ptr(), W.data_ptr(), idx.data_ptr(), _dtype_code(X), B, M, N, K, k, ldx, ldw,
@@ -444,8 +456,7 @@ def rmm_reduced_gemm_swiglu_kmajor(Xt: torch.Tensor, Wgu: torch.Tensor, idx: tor
         raise ValueError("idx must be contiguous int32 [B, k]")
     k = idx.numel() // B
     if workspace is None:
-        workspace = torch.empty(max(rmm_gemm_swiglu_workspace_size(B, M, F), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_gemm_swiglu_workspace_size(B, M, F), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_reduced_gemm_swiglu_kmajor", lib.rmm_reduced_gemm_swiglu_kmajor(
         Xt.data_ptr(), Wgu.data_ptr(), idx.data_ptr(), B, M, F, K, k, ldxt, ldw, Ht.data_ptr(),
@@ -541,8 +552,7 @@ def rmm_reduced_attention(Q: torch.Tensor, Kc: torch.Tensor, V: torch.Tensor, id
     if scale is None:
         scale = D ** -0.5
     if workspace is None:
-        workspace = torch.empty(max(rmm_workspace_size(RMM_OP_ATTENTION, batch * H, Lk, D, k), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_workspace_size(RMM_OP_ATTENTION, batch * H, Lk, D, k), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_reduced_attention", lib.rmm_reduced_attention(
         Q.data_ptr(), Kc.data_ptr(), V.data_ptr(), idx.data_ptr(), _dtype_code(Q), batch, H, Hkv,
@@ -598,8 +608,7 @@ def rmm_reduced_attention_kmajor(Q: torch.Tensor, Kc: torch.Tensor, V: torch.Ten
     if scale is None:
         scale = D ** -0.5
     if workspace is None:
-        workspace = torch.empty(max(rmm_attention_kmajor_workspace_size(batch, H, Lq, Lk, D, k), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_attention_kmajor_workspace_size(batch, H, Lq, Lk, D, k), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_reduced_attention_kmajor", lib.rmm_reduced_attention_kmajor(
         Q.data_ptr(), Kc.data_ptr(), V.data_ptr(), idx.data_ptr(), _dtype_code(Q), batch, H, Hkv,
@@ -634,8 +643,7 @@ def rmm_reduced_pv(P: torch.Tensor, V: torch.Tensor, kt: int, O: torch.Tensor,
                                 or not idx_out.is_contiguous()):
         raise ValueError("idx_out must be contiguous int32 [batch*H*kt]")
     if workspace is None:
-        workspace = torch.empty(max(rmm_workspace_size(RMM_OP_PV, batch * H, Lq, Lk, kt), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_workspace_size(RMM_OP_PV, batch * H, Lq, Lk, kt), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_reduced_pv", lib.rmm_reduced_pv(
         P.data_ptr(), V.data_ptr(), _dtype_code(P), batch, H, Hkv, Lq, Lk, D, ldp, int(kt),
@@ -662,8 +670,7 @@ def rmm_linear(X: torch.Tensor, W: torch.Tensor, r: float, Y: torch.Tensor,
                                 or not idx_out.is_contiguous()):
         raise ValueError("idx_out must be contiguous int32 [B, k]")
     if workspace is None:
-        workspace = torch.empty(max(rmm_workspace_size(RMM_OP_LINEAR, B, M, K, k), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_workspace_size(RMM_OP_LINEAR, B, M, K, k), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_linear", lib.rmm_linear(
         X.data_ptr(), W.data_ptr(), float(r), _dtype_code(X), B, M, N, K, ldx, ldw,
@@ -722,8 +729,7 @@ def rmm_rmsnorm_kmajor(X: torch.Tensor, gamma: torch.Tensor, eps: float, Xt: tor
     if energy.dtype != torch.float64 or energy.numel() != B * K or not energy.is_contiguous():
         raise ValueError("energy must be contiguous float64 [B*K]")
     if workspace is None:
-        workspace = torch.empty(max(rmm_rmsnorm_kmajor_workspace_size(B, M, K), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_rmsnorm_kmajor_workspace_size(B, M, K), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_rmsnorm_kmajor", lib.rmm_rmsnorm_kmajor(
         X.data_ptr(), gamma.data_ptr(), float(eps), B, M, K, ldx, Xt.data_ptr(), ldxt,
@@ -759,8 +765,7 @@ def rmm_attention_weights_kmajor(S: torch.Tensor, Pt: torch.Tensor, energy: torc
     if energy.dtype != torch.float64 or energy.numel() != batch * H * Lk or not energy.is_contiguous():
         raise ValueError("energy must be contiguous float64 [batch*H*Lk]")
     if workspace is None:
-        workspace = torch.empty(max(rmm_attention_weights_kmajor_workspace_size(batch, H, Lq, Lk), 1),
-                                dtype=torch.uint8, device=d)
+        workspace = _scratch(rmm_attention_weights_kmajor_workspace_size(batch, H, Lq, Lk), d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     if (row_max is None) != (row_rinv is None):
         raise ValueError("give both row_max and row_rinv, or neither")
@@ -842,7 +847,7 @@ def rmm_decode_products(groups, workspace: torch.Tensor | None = None, stream=No
     d = groups[0][0].device
     need = int(lib.rmm_decode_step_workspace_size(arr, len(groups), B))
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=d)
+        workspace = _scratch(need, d, stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check("rmm_decode_products", lib.rmm_decode_products(arr, len(groups), B, _ptr(workspace),
                                                           ws_bytes, _stream(d, stream)))
@@ -861,7 +866,7 @@ def rmm_decode_products_shared(groups, workspace: torch.Tensor | None = None, st
     d = groups[0][0].device
     if workspace is None:
         need = int(lib.rmm_decode_products_shared_workspace_size(arr, len(groups), B))
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=d)
+        workspace = _scratch(need, d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_decode_products_shared",
            lib.rmm_decode_products_shared(arr, len(groups), B, _ptr(workspace), ws_bytes,
@@ -876,7 +881,7 @@ def rmm_decode_step_shared(groups, workspace: torch.Tensor | None = None, stream
     d = groups[0][0].device
     if workspace is None:
         need = int(lib.rmm_decode_products_shared_workspace_size(arr, len(groups), B))
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=d)
+        workspace = _scratch(need, d, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check("rmm_decode_step_shared",
            lib.rmm_decode_step_shared(arr, len(groups), B, _ptr(workspace), ws_bytes, _stream(d, stream)))
@@ -890,7 +895,7 @@ def rmm_decode_step(groups, workspace: torch.Tensor | None = None, stream=None):
     d = groups[0][0].device
     need = int(lib.rmm_decode_step_workspace_size(arr, len(groups), B))
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=d)
+        workspace = _scratch(need, d, stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check("rmm_decode_step", lib.rmm_decode_step(arr, len(groups), B, _ptr(workspace), ws_bytes,
                                                   _stream(d, stream)))
@@ -1028,13 +1033,6 @@ def _run(fn: str, device: int, stream, *args):
         raise RmmError(fn, status)
 
 
-def _workspace(n: int, like: torch.Tensor, stream) -> torch.Tensor:
-    """A workspace of this call, not reused before the call's stream is done with it."""
-    ws = torch.empty(max(n, 1), dtype=torch.uint8, device=like.device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
-
 
 def _positions(rope, positions, T: int):
     if rope is None:
@@ -1076,7 +1074,7 @@ def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor 
     ws_bytes = 0
     if energy is not None:
         if workspace is None:
-            workspace = _workspace(rmm_qk_norm_rope_workspace_size(batch, H, L, D), Q, stream)
+            workspace = _scratch(rmm_qk_norm_rope_workspace_size(batch, H, L, D), Q.device, stream)
         ws_bytes = workspace.numel() * workspace.element_size()
     _run("rmm_qk_norm_rope", d, stream, code, batch, L, D, q, qo, k, ko, _vec(gamma_q, D, dt, "gamma_q"),
          _vec(gamma_k, D, dt, "gamma_k"), eps, None if rope is None else rope._c,
@@ -1154,7 +1152,7 @@ def rmm_paged_attention(Q: torch.Tensor, cache: KvCache, page_table: torch.Tenso
         scale = D ** -0.5
     d = _device_index(Q, O, cache.k, page_table, lengths, q_start, idx, workspace)
     if workspace is None:
-        workspace = _workspace(rmm_paged_attention_workspace_size(T, B, H, cache.Hkv, D), Q, stream)
+        workspace = _scratch(rmm_paged_attention_workspace_size(T, B, H, cache.Hkv, D), Q.device, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     _run("rmm_paged_attention", d, stream, T, _heads(Q, (T, H, D), bf, "Q", "[T, H, D] of the cache's D"), cache._c,
          page_table.data_ptr(), page_table.stride(0) if B > 1 else width, width,
