@@ -190,8 +190,11 @@ def _dev(*ts: torch.Tensor) -> torch.device:
 
 
 def _stream(device: torch.device, stream) -> int:
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    return s.cuda_stream
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    if stream.device != device:
+        raise ValueError("the stream must be one of the tensors' device")
+    return stream.cuda_stream
 
 
 def _ptr(t):
@@ -1023,7 +1026,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
 
 def _run(fn: str, device: int, stream, *args):
     """The call on `device`, on its current stream unless one is given."""
-    s = _raw_stream(device) if stream is None else stream.cuda_stream
+    if stream is None:
+        s = _raw_stream(device)
+    else:
+        s = _stream(torch.device("cuda", device), stream)
     if torch.cuda.current_device() == device:
         status = getattr(lib, fn)(*args, s)
     else:

@@ -103,3 +103,25 @@ def test_every_wrapper_that_allocates_is_listed():
     src = inspect.getsource(rmm)
     assert src.count("torch.empty(") == inspect.getsource(rmm._scratch).count("torch.empty(")
     assert src.count("_scratch(") - 1 == len(CALLS)
+
+
+class _Stream:
+    cuda_stream = 7
+
+    def __init__(self, device):
+        self.device = torch.device("cuda", device)
+
+
+def test_stream_of_another_device(monkeypatch):
+    """A kernel launched on another device's stream would run there, on pointers of this one."""
+    ran = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(rmm, "lib", type("L", (), {"f": staticmethod(lambda *args: ran.append(args) or 0)}))
+    assert rmm._stream(torch.device("cuda", 0), _Stream(0)) == 7
+    rmm._run("f", 0, _Stream(0), 1)
+    assert ran == [(1, 7)]
+    with pytest.raises(ValueError, match="stream"):
+        rmm._stream(torch.device("cuda", 0), _Stream(1))
+    with pytest.raises(ValueError, match="stream"):
+        rmm._run("f", 0, _Stream(1), 1)
+    assert len(ran) == 1
