@@ -862,8 +862,8 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * lengths   : int32 [B].   q_start: int32 [B+1] or NULL.   idx: int32 [T*H*k].
  * workspace : rmm_paged_attention_workspace_size(T, B, H, Hkv, D) bytes, 256-byte
  *             aligned (partial outputs; overwritten by every call).
- * Errors    : INVALID_ARGUMENT for null pointers, T, B, max_pages < 1,
- *             table_stride < max_pages, q_start NULL with T != B, H not a
+ * Errors    : INVALID_ARGUMENT for null pointers, T, B, max_pages < 1, a scale that is
+ *             NaN or infinite (or is, times log2 e), table_stride < max_pages, q_start NULL with T != B, H not a
  *             multiple of the cache's Hkv, o's head count not H, k outside
  *             [1, D], a misaligned workspace; UNSUPPORTED for a cache or
  *             strides that break the rules above, max_pages * page_size > 2^30,

@@ -184,6 +184,8 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
         return RMM_ERR_INVALID_ARGUMENT;
     if (!q_start && T != B) return RMM_ERR_INVALID_ARGUMENT;
     rmm::PagedArgs a = {};
+    a.c = scale * 1.4426950408889634f;
+    if (!std::isfinite(a.c)) return RMM_ERR_INVALID_ARGUMENT;
     rmm_status_t st = check_cache(cache, &a.kv);
     if (st == RMM_OK) st = check_heads(q, 2, &a.q);
     if (st == RMM_OK) st = check_heads(o, 2, &a.o);
@@ -207,7 +209,6 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
     a.B = static_cast<int>(B);
     a.k = static_cast<int>(k);
     a.T = T;
-    a.c = scale * 1.4426950408889634f;
     a.causal = causal != 0;
     return from_hip(rmm::launch_paged_attn(a, static_cast<int>(cache->D), workspace, stream));
 }
