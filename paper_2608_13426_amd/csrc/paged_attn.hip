@@ -32,6 +32,7 @@
 #include "device_common.h"
 #include "kernels.h"
 #include "kv_cache.h"
+#include "paged_plan.h"
 
 namespace rmm {
 
@@ -39,11 +40,6 @@ namespace {
 
 namespace pg {
 constexpr float kTau = 8.f;               // lazy-rescale threshold, log2 units
-// Units of at most kShort blocks, no more of them than workgroups, are never cut
-// (the host then leaves out the joining launch).  One token, 32 heads of 128 on 8:
-// 500 keys uncut 11.3 us, cut 9.9 + 3.9 and a launch; 1000 keys uncut 16.4, cut
-// 10.0 + 3.9, which is even with the launch and leaves the card to others.
-constexpr int kShort = 16;
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
 template <typename F>
@@ -124,15 +120,10 @@ __device__ __forceinline__ int in_branch(int x) {
     return x;
 }
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
     const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(static_cast<uint64_t>(x) >> 32));
     return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
-}
-// a / b of non-negative values
-__device__ __forceinline__ int quot(int a, int b) {
-    return uniform(static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)));
 }
 // x or that of the lane that the DPP control CTRL names; every lane must be active
 template <int CTRL>
@@ -156,207 +147,77 @@ __device__ __forceinline__ int prefix_sum(int x) {
     return x;
 }
 
-// ---- the line.  TK keys per block, ROWS query rows per unit.  The host keeps its
-// length below 2^30 (paged_line_fits).
-struct Seq {
-    int q0, n, len;                       // first token, new tokens, keys
-    int bad;                              // longer than its row of the page table
-};
+// The workgroup's run
 template <int TK, int ROWS>
-struct Plan {
-    int grp, causal, Hkv;
-    bool whole;                           // units count one each (all are short)
-
-    __device__ __forceinline__ Seq load(const PagedArgs &a, int b) const {
-        Seq s;
-        int q1;
-        if (a.q_start) {
-            s.q0 = min(max(a.q_start[b], 0), static_cast<int>(a.T));
-            q1 = min(a.q_start[b + 1], static_cast<int>(a.T));
-        } else {
-            s.q0 = b;
-            q1 = b + 1;
+__device__ __forceinline__ bool Walk<TK, ROWS>::init(const PagedArgs &a, int min_run, int cut_cost) {
+    const int lane = threadIdx.x & 63;
+    pl.grp = a.q.n / a.kv.Hkv;
+    pl.causal = a.causal;
+    pl.Hkv = a.kv.Hkv;
+    pl.whole = false;
+    // the line's length in blocks and in units, the longest unit: lane l looks
+    // at sequences l, l + 64, ...
+    Seq mine = {0, 0, 0, 0};
+    if (lane < a.B) mine = pl.load(a, lane);
+    int most = pl.longest(mine), most2 = pl.longest_pair(mine);
+    int w0 = pl.work(mine), blocks = w0, units = pl.units(mine);
+    for (int i = lane + 64; i < a.B; i += 64) {
+        const Seq q = pl.load(a, i);
+        most = max(most, pl.longest(q));
+        most2 = max(most2, pl.longest_pair(q));
+        blocks += pl.work(q);
+        units += pl.units(q);
+    }
+    int sum0 = prefix_sum(blocks);
+    int total = __builtin_amdgcn_readlane(sum0, 63);
+    if (a.whole) {
+        pl.whole = true;
+    } else {
+        const int nu = __builtin_amdgcn_readlane(prefix_sum(units), 63);
+        const int rounds = quot(nu + a.nw - 1, a.nw), room = quot(total, a.nw) + cut_cost;
+        pl.whole = __ballot((rounds >> 1) * most2 + (rounds & 1) * most > room) == 0;
+    }
+    if (pl.whole) {
+        w0 = pl.units(mine);
+        sum0 = prefix_sum(units);
+        total = __builtin_amdgcn_readlane(sum0, 63);
+    }
+    if (a.B > 64) sum0 = prefix_sum(w0);
+    run = quot(total + a.nw - 1, a.nw);
+    run = pl.whole ? max(run, 1) : (max(run, min_run) + 3) / 4 * 4;
+    // consecutive runs on one XCD (workgroups are dealt to the 8 XCDs in turn),
+    // where units that share keys share its L2, the XCDs evenly used
+    const int i0 = static_cast<int>(blockIdx.x), runs = quot(total + run - 1, run), per = (runs + 7) >> 3;
+    wg = i0;                          // idle workgroups keep the places behind the runs
+    if ((i0 >> 3) < per) wg = (i0 & 7) * per + (i0 >> 3);
+    if ((i0 >> 3) >= per || wg >= runs) return false;
+    begin = x = wg * run;
+    end = min(total - x, run) + x;
+    // the sequence at x
+    int base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        Seq q = mine;
+        int w = w0, sum = sum0;
+        if (b0 > 0) {
+            q = b0 + lane < a.B ? pl.load(a, b0 + lane) : Seq{0, 0, 0, 0};
+            w = pl.work(q);
+            sum = prefix_sum(w);
         }
-        s.n = max(q1 - s.q0, 0);
-        const int cap = a.width << a.kv.lg_page, len = max(a.lens[b], 0);
-        s.bad = len > cap;
-        s.len = min(len, cap);
-        return s;
-    }
-    __device__ __forceinline__ int tiles(const Seq &s) const {
-        return static_cast<int>((static_cast<uint32_t>(s.n * grp) + ROWS - 1) / ROWS);
-    }
-    // keys that some row of a tile sees (at most; the last token of the tile given)
-    __device__ __forceinline__ int keys(const Seq &s, int last_tok) const {
-        return causal ? min(max(s.len - s.n + last_tok + 1, 0), s.len) : s.len;
-    }
-    __device__ __forceinline__ int last_token(const Seq &s, int tile) const {
-        return min(static_cast<int>((static_cast<uint32_t>(tile) * ROWS + ROWS - 1) / static_cast<uint32_t>(grp)), s.n - 1);
-    }
-    __device__ __forceinline__ int blocks(const Seq &s, int tile) const {
-        return max((keys(s, last_token(s, tile)) + TK - 1) / TK, 1);
-    }
-    // length on the line of a pair of tiles (p, 2 np - 1 - p)
-    __device__ __forceinline__ int pair(const Seq &s, int np) const {
-        if (np == 1 || !causal) return blocks(s, 0) + blocks(s, 2 * np - 1);
-        const int tok = static_cast<int>((static_cast<uint32_t>(np) * 2 * ROWS - 1) / static_cast<uint32_t>(grp));    // of a full last tile
-        const int k = min(max(s.len - s.n + tok + 1, 1), s.len + ROWS);
-        return blocks(s, 0) + (k + TK - 1) / TK + 2;
-    }
-    __device__ __forceinline__ int units(const Seq &s) const { return tiles(s) * Hkv; }
-    // a sequence's share of the line per kv head
-    __device__ __forceinline__ int head_work(const Seq &s) const {
-        const int t = tiles(s), np = t >> 1;
-        if (whole) return t;
-        int w = np > 0 ? np * pair(s, np) : 0;
-        if (t & 1) w += blocks(s, t - 1);
-        return w;
-    }
-    __device__ __forceinline__ int work(const Seq &s) const { return head_work(s) * Hkv; }
-    __device__ __forceinline__ int longest(const Seq &s) const {
-        return s.n > 0 ? blocks(s, tiles(s) - 1) : 0;
-    }
-    // of two units that are neighbours when none is cut
-    __device__ __forceinline__ int longest_pair(const Seq &s) const {
-        const int t = tiles(s);
-        return t > 1 ? blocks(s, 0) + blocks(s, t - 1) : 2 * longest(s);
-    }
-};
-
-// A workgroup's place on the line
-template <int TK, int ROWS>
-struct Walk {
-    Plan<TK, ROWS> pl;
-    int wg;                               // the workgroup's place among the runs
-    int x, begin, end, run;               // position, the workgroup's run, run length
-    int b, f;                             // the sequence at x, where it begins
-    Seq s;
-    // the unit at x
-    int kvh, tile, c0, c1;                // blocks [c0, c1) of it are in the run
-    int u0, u1;                           // its place on the line
-
-    // false: no work for this workgroup
-    // min_run: shortest run; cut_cost: what cutting units costs, in blocks
-    __device__ __forceinline__ bool init(const PagedArgs &a, int min_run, int cut_cost) {
-        const int lane = threadIdx.x & 63;
-        pl.grp = a.q.n / a.kv.Hkv;
-        pl.causal = a.causal;
-        pl.Hkv = a.kv.Hkv;
-        pl.whole = false;
-        // the line's length in blocks and in units, the longest unit: lane l looks
-        // at sequences l, l + 64, ...
-        Seq mine = {0, 0, 0, 0};
-        if (lane < a.B) mine = pl.load(a, lane);
-        int most = pl.longest(mine), most2 = pl.longest_pair(mine);
-        int w0 = pl.work(mine), blocks = w0, units = pl.units(mine);
-        for (int i = lane + 64; i < a.B; i += 64) {
-            const Seq q = pl.load(a, i);
-            most = max(most, pl.longest(q));
-            most2 = max(most2, pl.longest_pair(q));
-            blocks += pl.work(q);
-            units += pl.units(q);
+        const uint64_t past = __ballot(base + sum > x);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            b = b0 + l;
+            f = base + __builtin_amdgcn_readlane(sum - w, l);
+            s.q0 = __builtin_amdgcn_readlane(q.q0, l);
+            s.n = __builtin_amdgcn_readlane(q.n, l);
+            s.len = __builtin_amdgcn_readlane(q.len, l);
+            s.bad = __builtin_amdgcn_readlane(q.bad, l);
+            break;
         }
-        int sum0 = prefix_sum(blocks);
-        int total = __builtin_amdgcn_readlane(sum0, 63);
-        if (a.whole) {
-            pl.whole = true;
-        } else {
-            const int nu = __builtin_amdgcn_readlane(prefix_sum(units), 63);
-            const int rounds = quot(nu + a.nw - 1, a.nw), room = quot(total, a.nw) + cut_cost;
-            pl.whole = __ballot((rounds >> 1) * most2 + (rounds & 1) * most > room) == 0;
-        }
-        if (pl.whole) {
-            w0 = pl.units(mine);
-            sum0 = prefix_sum(units);
-            total = __builtin_amdgcn_readlane(sum0, 63);
-        }
-        if (a.B > 64) sum0 = prefix_sum(w0);
-        run = quot(total + a.nw - 1, a.nw);
-        run = pl.whole ? max(run, 1) : (max(run, min_run) + 3) / 4 * 4;
-        // consecutive runs on one XCD (workgroups are dealt to the 8 XCDs in turn),
-        // where units that share keys share its L2, the XCDs evenly used
-        const int i0 = static_cast<int>(blockIdx.x), runs = quot(total + run - 1, run), per = (runs + 7) >> 3;
-        wg = i0;                          // idle workgroups keep the places behind the runs
-        if ((i0 >> 3) < per) wg = (i0 & 7) * per + (i0 >> 3);
-        if ((i0 >> 3) >= per || wg >= runs) return false;
-        begin = x = wg * run;
-        end = min(total - x, run) + x;
-        // the sequence at x
-        int base = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 64) {
-            Seq q = mine;
-            int w = w0, sum = sum0;
-            if (b0 > 0) {
-                q = b0 + lane < a.B ? pl.load(a, b0 + lane) : Seq{0, 0, 0, 0};
-                w = pl.work(q);
-                sum = prefix_sum(w);
-            }
-            const uint64_t past = __ballot(base + sum > x);
-            if (past) {
-                const int l = __builtin_ctzll(past);
-                b = b0 + l;
-                f = base + __builtin_amdgcn_readlane(sum - w, l);
-                s.q0 = __builtin_amdgcn_readlane(q.q0, l);
-                s.n = __builtin_amdgcn_readlane(q.n, l);
-                s.len = __builtin_amdgcn_readlane(q.len, l);
-                s.bad = __builtin_amdgcn_readlane(q.bad, l);
-                break;
-            }
-            base += __builtin_amdgcn_readlane(sum, 63);
-        }
-        return true;
+        base += __builtin_amdgcn_readlane(sum, 63);
     }
-    // the unit at x (false: x is at no unit and has moved on, or at the end)
-    __device__ __forceinline__ bool locate(const PagedArgs &a) {
-        const int hw = pl.head_work(s);
-        if (x >= f + hw * pl.Hkv) {       // the next sequence with work
-            f += hw * pl.Hkv;
-            const Seq q = pl.load(a, ++b);
-            s = {uniform(q.q0), uniform(q.n), uniform(q.len), uniform(q.bad)};
-            return false;
-        }
-        kvh = quot(x - f, hw);
-        const int y = x - f - kvh * hw;
-        if (pl.whole) {                   // one place per unit, late and early tiles in turn
-            tile = y & 1 ? y >> 1 : hw - 1 - (y >> 1);
-            u0 = x;
-            u1 = x + 1;
-            c0 = 0;
-            c1 = pl.blocks(s, tile);
-            return true;
-        }
-        const int t = pl.tiles(s), np = t >> 1;
-        const int pr = np > 0 ? pl.pair(s, np) : 0;
-        int off;
-        if (y < np * pr) {
-            const int p = quot(y, pr);
-            off = y - p * pr;
-            tile = p;
-            const int wa = pl.blocks(s, p);
-            if (off >= wa) {
-                tile = 2 * np - 1 - p;
-                const int wb = pl.blocks(s, tile);
-                if (off >= wa + wb) {     // the rest of the pair's length is empty
-                    x += pr - off;
-                    return false;
-                }
-                off -= wa;
-            }
-        } else {
-            tile = t - 1;
-            off = y - np * pr;
-        }
-        u0 = x - off;
-        u1 = u0 + pl.blocks(s, tile);
-        c0 = off;
-        c1 = min(end, u1) - u0;
-        return true;
-    }
-    __device__ __forceinline__ void advance() { x = min(end, u1); }
-    __device__ __forceinline__ bool complete() const { return u0 >= begin && u1 <= end; }
-    // 1: the piece of a cut unit that begins in this run, 0: of one that began before it
-    __device__ __forceinline__ int part() const { return u0 >= begin ? 1 : 0; }
-};
+    return true;
+}
 
 // What the joining launch needs to know of a workgroup's piece of a cut unit:
 // the unit's workgroups first .. first + n - 1 (n = 0: no piece), its rows
@@ -492,23 +353,9 @@ __device__ __forceinline__ void wait_vmcnt_le() {
 }
 }  // namespace pg
 
-// ------------------------------------------------------------- few rows
-namespace few {
-constexpr int kWaves = 4, kThreads = 64 * kWaves, TK = 32;
-// Workgroups: two per CU, what the registers allow at once.  More wait their turn:
-// 64 sequences of up to 1000 keys 43 us with 512, 54 with 768, 51 with 1024.
-constexpr int kGroups = 512;
-// Chunks in a run at least: two rounds of the four waves.  Half of it is 1 us
-// faster at 1000 keys (9.1 for 10.0) and 3 slower at 8192 in the joining launch
-// (7.4 for 4.8); twice is slower at both (12.5; 14.8 for 13.0).
-constexpr int kMinRun = 8;
-// What a cut unit costs, in chunks: 64 sequences of up to 1000 keys 43 us, 47 with
-// 4, 43 with 16 (a unit's halves then end later than whole units elsewhere).
-constexpr int kCutCost = 8;
-}  // namespace few
-
 }  // namespace
 
+// ------------------------------------------------------------- few rows
 // S^T = K Q^T takes 16 key rows as they are loaded (v_mfma_f32_16x16x32: a lane
 // holds 8 dims of one key).  In its result a lane holds one query row, and with
 // key 8 g + 4 tb + i at row 4 g + i of key tile tb exactly the eight keys that
@@ -931,17 +778,8 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
     if (tid < 2 && !(held >> tid & 1)) reinterpret_cast<PieceOf *>(a.pieces)[2 * wg + tid].n = 0;
 }
 
-// ------------------------------------------------------------ many rows
-namespace rowsk {
-constexpr int NW = 8, NT = 64 * NW;       // waves of 32 query rows
-constexpr int ROWS = 32 * NW, TK = 64, NS = 4;    // rows per unit, keys per tile, ring slots
-constexpr int kGroups = 256;              // workgroups: one per CU
-// In tiles.  Cutting costs a unit's 256 rows of partial sums written and read: a
-// prompt of 4096 tokens, 32 heads, takes 166 + 5 us uncut and 192 + 42 cut.  Three
-// sequences of 700 tokens behind up to 3300: cut 102 + 20, uncut (cost 32) 123 + 5.
-constexpr int kMinRun = 4, kCutCost = 16;
-}  // namespace rowsk
 
+// ------------------------------------------------------------ many rows
 // Eight waves of 32 query rows over a ring of 64-key tiles in LDS, each filled two
 // steps (bf16, by LDS DMA) or one step (4-bit, through registers, as bf16) ahead:
 // S^T = K Q^T with v_mfma_f32_32x32x16 (a lane holds 16 keys of one row), online softmax in log2
@@ -1425,33 +1263,6 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
 
 namespace {
 
-// Query rows per unit, by the average sequence's.  A unit reads its keys once, so
-// small ones repeat reads (partly from a cache) and large ones spend matrix work and
-// registers on rows that are not there.  Measured (us, heads of 128, 8 sequences of
-// up to 9000 keys unless said, without the joining launch):
-//   bf16    16 rows: 16 per unit 37, 32: 38;   24 rows: 42, 41;   40 rows: 64, 46
-//   bf16    32 rows: 32 per unit 40, 256: 44;  64 rows: 49, 46;  128 rows: 72, 51
-//           64 sequences: 24 rows 80, 93;  40 rows 122, 98;  128 rows 210, 116
-//   4-bit   64 sequences: 24 rows, 16 per unit 59, 32: 50, 64: 60;  40 rows: 82, 81, 72
-//   4-bit   64 per unit against 256: 128 rows 54, 72;  256 rows 57, 74;  32 sequences
-//           of 256 rows 192, 179;  512 rows 100, 104.  Heads of 64: 40 rows 28, 30;
-//           64 rows 91, 121;  128 rows 42, 34
-// With a bf16 cache units of 64 rows were no better than 32 or 256 anywhere (40 rows
-// 47, 128 rows 66, 64 sequences of 40 rows 95): there is none.  A 4-bit cache keeps
-// them, since a 256-row unit turns every key into bf16 through registers into LDS.
-int unit_rows(int64_t T, int64_t B, int64_t grp, bool mx, int D) {
-    const int64_t rows = (T * grp + B - 1) / B;
-    if (rows <= 16) return 16;
-    if (rows <= 32) return 32;
-    return mx && rows <= (D == 128 ? 256 : 64) ? 64 : rowsk::ROWS;
-}
-int workgroups(int rows) { return rows <= 64 ? few::kGroups : rowsk::kGroups; }
-int block_keys(int rows) { return rows <= 64 ? few::TK : rowsk::TK; }
-// units at most: full row tiles, and a last one per sequence
-int64_t most_units(int64_t T, int64_t B, int64_t H, int64_t Hkv, int rows) {
-    return T * H / rows + (T < B ? T : B) * Hkv;
-}
-
 template <int D, bool MX, int ROWS>
 hipError_t launch(const PagedArgs &a, hipStream_t stream) {
     if constexpr (ROWS <= 64) {
@@ -1503,8 +1314,7 @@ size_t paged_workspace_bytes(int64_t T, int64_t B, int64_t H, int64_t Hkv, int D
 hipError_t launch_paged_attn(PagedArgs a, int D, void *workspace, hipStream_t stream) {
     const int rows = unit_rows(a.T, a.B, a.q.n / a.kv.Hkv, a.kv.mx, D);
     a.nw = workgroups(rows);
-    a.whole = (static_cast<int64_t>(a.width) << a.kv.lg_page) <= pg::kShort * block_keys(rows) &&
-              most_units(a.T, a.B, a.q.n, a.kv.Hkv, rows) <= a.nw;
+    a.whole = never_cut(a, rows);
     a.pieces = workspace;
     a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * a.nw * sizeof(pg::PieceOf));
     a.part_ml = a.part_o + static_cast<int64_t>(2 * a.nw) * rows * D;
