@@ -841,7 +841,7 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  *             scale * sum over d in I of q[j][h][d] K[s][d]
  * It sees s <= lengths[b] - n + j when causal (the new tokens are the cache's
  * last n), else s < lengths[b] (e.g. an encoder's states).  A token that sees
- * no key gets 0.  I = idx[(t*H + h)*k ..) for token t (rmm_select_tokens on the rows of
+ * no key gets 0, one that sees keys but only with scores of -infinity NaN.  I = idx[(t*H + h)*k ..) for token t (rmm_select_tokens on the rows of
  * q), or all dims when idx is NULL (k ignored).  A key or value that is
  * infinite or NaN in a dim outside I, or past what a token sees, does not reach
  * it (only the order of its sums may change).

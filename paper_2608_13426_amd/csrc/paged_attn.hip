@@ -102,6 +102,11 @@ __device__ __forceinline__ float add_pair(uint32_t w, float s) {
 #endif
 }
 __device__ __forceinline__ float exp_two(float x) { return __builtin_amdgcn_exp2f(x); }
+// what a row's weighted sum is multiplied with; lim: the last key that the row sees.
+// A sum of zero is a softmax of nothing but -inf (NaN), or of no key (0).
+__device__ __forceinline__ float row_scale(float sum, int lim) {
+    return sum == 0.f ? (lim < 0 ? 0.f : __builtin_nanf("")) : 1.f / sum;
+}
 // of 8 bf16 values (w), those at the set bits of m
 __device__ __forceinline__ uint4 keep8(uint4 w, uint32_t m) {
     w.x &= (m & 1 ? 0xffffu : 0u) | (m & 2 ? 0xffff0000u : 0u);
@@ -222,14 +227,14 @@ __device__ __forceinline__ bool Walk<TK, ROWS>::init(const PagedArgs &a, int min
 // What the joining launch needs to know of a workgroup's piece of a cut unit:
 // the unit's workgroups first .. first + n - 1 (n = 0: no piece), its rows
 struct PieceOf {
-    int n, first, rows, q0, kvh, row0, pad0, pad1;
+    int n, first, rows, q0, kvh, row0, lim0, pad;         // lim0: last key that the sequence's first token sees
 };
 // A workgroup has at most two pieces: of the unit its run begins inside of
 // (slot 0) and of the one it ends inside of (slot 1)
 template <int TK, int ROWS>
 __device__ __forceinline__ PieceOf piece_of(const Walk<TK, ROWS> &w, int rows) {
     const int first = quot(w.u0, w.run), last = quot(w.u1 - 1, w.run);
-    return {last - first + 1, first, rows, w.s.q0, w.kvh, w.tile * ROWS, 0, 0};
+    return {last - first + 1, first, rows, w.s.q0, w.kvh, w.tile * ROWS, w.pl.causal ? w.s.len - w.s.n : w.s.len - 1, 0};
 }
 
 // dims d, d + 1 of a cached row
@@ -705,7 +710,7 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             constexpr int N = sizeof(acc) / sizeof(float);
             if (complete) {
                 const int q = row0 + r;
-                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                const float inv = row_scale(ls, a.causal ? sq.len - sq.n + q / grp : sq.len - 1);
                 uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + q / grp) * a.o.st + (kvh * grp + q % grp) * a.o.sh + d;
                 uint32_t y[N / 2];
 #pragma unroll
@@ -1132,7 +1137,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                                      [&](int r, float m, float ls, int d, float x, float y) {
                 if (complete) {
                     const int q = row0 + r;
-                    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                    const float inv = row_scale(ls, a.causal ? sq.len - sq.n + q / grp : sq.len - 1);
                     *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.o.p) + (sq.q0 + q / grp) * a.o.st +
                                                   (kvh * grp + q % grp) * a.o.sh + d) = pack_bf16x2(x * inv, y * inv);
                 } else {
@@ -1144,7 +1149,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         } else if (on) {
             const float ls = all & 1 ? __builtin_nanf("") : l;
             if (complete) {
-                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                const float inv = row_scale(ls, lim);
                 uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + tok) * a.o.st + hd * a.o.sh + 4 * lh;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
@@ -1252,8 +1257,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
                 }
             }
             if (si == 0 && r < pc.rows) {
-                const float inv = ls == 0.f ? 0.f : 1.f / ls;
                 const int rho = pc.row0 + r;
+                const float inv = row_scale(ls, a.causal ? pc.lim0 + rho / grp : pc.lim0);
                 uint16_t *op = static_cast<uint16_t *>(a.o.p) + (pc.q0 + rho / grp) * a.o.st + (pc.kvh * grp + rho % grp) * a.o.sh + 4 * l;
                 *reinterpret_cast<uint2 *>(op) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
             }

@@ -1,0 +1,113 @@
+"""Attention over a paged cache where scores, keys or values are infinite, NaN or at the
+type's ends: units kept whole and cut ones, few query rows and many."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_13426_amd as rmm
+from tests import paged_ref as pr
+from tests.gpu_util import gpu, require_gpu
+
+pytestmark = gpu
+INF, NAN = float("inf"), float("nan")
+
+# (L, n, H, Hkv, D): one sequence of L keys, n new tokens
+FORMS = {
+    "few": (40, 1, 8, 2, 128),
+    "few_cut": (5000, 1, 8, 2, 64),
+    "few_32": (50, 7, 8, 2, 128),
+    "few_32_cut": (5000, 7, 8, 2, 128),
+    "64": (90, 12, 8, 2, 64),               # 64-row units over a 4-bit cache, 256-row ones over bf16
+    "64_cut": (5000, 12, 8, 2, 64),
+    "rows": (200, 90, 8, 2, 64),
+    "rows_cut": (6000, 90, 8, 2, 64),
+    "rows_128": (700, 500, 2, 2, 128),
+    "rows_128_cut": (9000, 300, 2, 2, 128),
+}
+PAGE = 16
+both = pytest.mark.parametrize("mx", [False, True])
+forms = pytest.mark.parametrize("form", FORMS)
+
+
+def _make(form, mx, K, V, Q, causal=True, scale=None, idx=None, length=None):
+    """(O, K, V as cached [L, Hkv, D] float64) of one call."""
+    dev = Q.device
+    L, Hkv, D = K.shape
+    cache = rmm.kv_cache(-(-L // PAGE) + 1, Hkv, PAGE, D, mx=mx, device=dev)
+    slots = torch.arange(PAGE, PAGE + L, dtype=torch.int32, device=dev)
+    rmm.rmm_kv_append(K, V, slots, cache)
+    kv = [torch.empty(L, Hkv, D, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    rmm.rmm_kv_gather(cache, slots, *kv)
+    table = torch.arange(1, 1 + -(-L // PAGE), dtype=torch.int32, device=dev)[None]
+    start = torch.tensor([0, Q.shape[0]], dtype=torch.int32, device=dev)
+    O = torch.full_like(Q, 3.0)
+    rmm.rmm_paged_attention(Q, cache, table, torch.tensor([L if length is None else length], dtype=torch.int32, device=dev),
+                            O, q_start=start, causal=causal, scale=scale, idx=idx)
+    return O, kv[0].double(), kv[1].double()
+
+
+def _inputs(form, seed):
+    dev = require_gpu()
+    L, n, H, Hkv, D = FORMS[form]
+    g = torch.Generator(device=dev).manual_seed(seed)
+    K, V = (torch.randn(L, Hkv, D, device=dev, generator=g).bfloat16() for _ in range(2))
+    return L, n, H, Hkv, D, K, V, torch.randn(n, H, D, device=dev, generator=g).bfloat16()
+
+
+def _check(O, K, V, Q, see, tokens, unrounded=True):
+    """The given tokens against float64, token j over its first see[j] keys."""
+    H, Hkv = Q.shape[1], K.shape[1]
+    grp, D = H // Hkv, Q.shape[2]
+    t = torch.as_tensor(tokens, device=Q.device)
+    if not len(t):
+        return
+    rows = torch.as_tensor(see, device=Q.device)[t][:, None].expand(-1, grp).reshape(-1)
+    for h in range(Hkv):
+        q, o = (x[t, h * grp:(h + 1) * grp].reshape(-1, D).double() for x in (Q, O))
+        pr.check(o, *pr.attend(q, K[:, h], V[:, h], rows, D ** -0.5, unrounded), what=f"kv head {h}")
+
+
+@both
+@forms
+def test_every_score_minus_infinity(form, mx):
+    """A softmax of nothing but -inf is NaN; only a token that sees no key gives 0.  The scores are
+    -3e38 * 2e38 * scale, past fp32; the other heads' tokens are ordinary."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 1)
+    K[:, 0, 5] = -2e38
+    Q[:, :, 5] = 0
+    Q[::2, 0, 5] = 3e38                     # every second token of the first query head
+    length = L if n == 1 else n - 1         # the first token sees no key
+    O, Kc, Vc = _make(form, mx, K, V, Q, length=length)
+    for j in range(n):
+        if length - n + j + 1 <= 0:
+            assert bool((O[j] == 0).all())
+        elif j % 2 == 0:
+            assert O[j, 0].isnan().all(), j
+    assert O[:, H // Hkv:].isfinite().all()
+    O, Kc, Vc = _make(form, mx, K, V, Q)
+    assert O[::2, 0].isnan().all() and O[1::2].isfinite().all()
+    Qz = Q.clone()
+    Qz[::2, 0] = 0
+    O[::2, 0] = _make(form, mx, K, V, Qz)[0][::2, 0]
+    _check(O, Kc, Vc, Qz, [L - n + j + 1 for j in range(n)], range(n))
+
+
+@both
+@forms
+def test_some_scores_minus_infinity(form, mx):
+    """A key whose score is -inf has no weight, wherever the others lie (in other pieces too)."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 2)
+    Q[:, :, 5] = 3e38
+    for lo, hi in ((0, L // 2), (L // 4, L - n), (L // 2, L - n)):
+        Kb = K.clone()
+        Kb[:, :, 5] = 0
+        Kb[lo:hi, :, 5] = -2e38
+        O, Kc, Vc = _make(form, mx, Kb, V, Q)
+        left = torch.ones(L, dtype=torch.bool, device=Q.device)
+        left[lo:hi] = False
+        Qz = Q.clone()
+        Qz[:, :, 5] = 0
+        see = [int(left[:L - n + j + 1].sum()) for j in range(n)]
+        if mx:                              # a group of 32 dims has one scale: the other keys' are as they were
+            Kc = Kc.nan_to_num()
+        _check(O, Kc[left], Vc[left], Qz, see, [j for j in range(n) if see[j]])
