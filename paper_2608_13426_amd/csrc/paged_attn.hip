@@ -1217,12 +1217,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
                 const float mn = fmaxf(m, mp);
                 const float a0 = m == -__builtin_inff() ? 0.f : exp_two(m - mn);
                 const float a1 = mp == -__builtin_inff() ? 0.f : exp_two(mp - mn);
-                // a NaN sum stays one whatever its maximum; what has no weight adds nothing
+                // a NaN sum stays one whatever its maximum, and so does an output that is not
+                // finite: a visible value was infinite or NaN, and no weight makes 0 of it
                 ls = (ls == ls ? ls * a0 : ls) + (lp == lp ? lp * a1 : lp);
-                o.x = (a0 == 0.f ? 0.f : o.x * a0) + (a1 == 0.f ? 0.f : v.x * a1);
-                o.y = (a0 == 0.f ? 0.f : o.y * a0) + (a1 == 0.f ? 0.f : v.y * a1);
-                o.z = (a0 == 0.f ? 0.f : o.z * a0) + (a1 == 0.f ? 0.f : v.z * a1);
-                o.w = (a0 == 0.f ? 0.f : o.w * a0) + (a1 == 0.f ? 0.f : v.w * a1);
+                o.x = o.x * a0 + v.x * a1;
+                o.y = o.y * a0 + v.y * a1;
+                o.z = o.z * a0 + v.z * a1;
+                o.w = o.w * a0 + v.w * a1;
                 m = mn;
             };
             if (r < pc.rows) {
@@ -1249,10 +1250,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
                         const float4 v = acc_s[ri + q * RP][l];
                         const float al = x.x == -__builtin_inff() ? 0.f : exp_two(x.x - m);
                         ls += x.y == x.y ? x.y * al : x.y;
-                        o.x += al == 0.f ? 0.f : v.x * al;
-                        o.y += al == 0.f ? 0.f : v.y * al;
-                        o.z += al == 0.f ? 0.f : v.z * al;
-                        o.w += al == 0.f ? 0.f : v.w * al;
+                        o.x += v.x * al;
+                        o.y += v.y * al;
+                        o.z += v.z * al;
+                        o.w += v.w * al;
                     }
                 }
             }

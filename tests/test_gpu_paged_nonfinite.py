@@ -111,3 +111,26 @@ def test_some_scores_minus_infinity(form, mx):
         if mx:                              # a group of 32 dims has one scale: the other keys' are as they were
             Kc = Kc.nan_to_num()
         _check(O, Kc[left], Vc[left], Qz, see, [j for j in range(n) if see[j]])
+
+
+@both
+@forms
+def test_infinite_value_without_weight(form, mx):
+    """0 * infinity is NaN: an infinite value whose weight is zero or too small for fp32 is not
+    lost on the way through pieces; the other dims are as they would be."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 3)
+    K[:, :, 5] = 0
+    K[:L // 2, :, 5] = -50
+    Q[:, :, 5] = 400                        # scores 1768 to 2500 below the others', e^-1768 = 0 in fp32
+    Vb = V.clone()
+    Vb[3, :, 70 % D] = INF
+    O, Kc, Vc = _make(form, mx, K, Vb, Q)
+    see = [max(L - n + j + 1, 0) for j in range(n)]
+    rows = [j for j in range(n) if see[j] > L // 2]
+    lost = torch.zeros(D, dtype=torch.bool, device=Q.device)
+    lost[slice(32 * (70 % D // 32), 32 * (70 % D // 32) + 32) if mx else 70 % D] = True
+    assert not O[rows][..., lost].isfinite().any()
+    assert O[rows][..., ~lost].isfinite().all()
+    O[..., lost] = 0
+    Vc[..., lost] = 0
+    _check(O, Kc, Vc, Q, see, rows)
