@@ -40,6 +40,11 @@ namespace {
 
 namespace pg {
 constexpr float kTau = 8.f;               // lazy-rescale threshold, log2 units
+// A row's reference lies this far above its maximum (log2 units): weights are 2^-24 at
+// most, so that sums over 2^23 keys of values up to the type's largest stay in fp32.
+// They are powers of two times what they would be otherwise, and bf16 has fp32's exponents;
+// values below 2^-94 lose bits to it.
+constexpr float kLift = 32.f;
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
 template <typename F>
@@ -250,7 +255,7 @@ __device__ __forceinline__ float2 cached_pair(const uint8_t *rows, const uint8_t
 // per wave with nothing shared between rows: what the units that meet an
 // infinite or NaN value are redone with, since there a weight or a query of zero
 // does not silence a key or value that a row does not see.  put(row, m, l,
-// d, o): maximum, sum and two dims of a row's output, called by every lane that holds some.
+// d, o): reference, sum and two dims of a row's output, called by every lane that holds some.
 template <int D, bool MX, bool IDX, typename Put>
 __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, int b, int kvh, int row0, int n_rows,
                                              int first, int step, int k0, int k1, const uint32_t (*keep)[D / 32], Put put) {
@@ -284,7 +289,7 @@ __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, 
             float mx = sc;
 #pragma unroll
             for (int i = 32; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i, 64));
-            const float mn = fmaxf(m, mx), use = mn == -__builtin_inff() ? 0.f : mn;
+            const float mn = fmaxf(m, mx + kLift), use = mn == -__builtin_inff() ? 0.f : mn;
             const float al = exp_two((m == -__builtin_inff() ? use : m) - use);
             const float p = bf16_to_f32(f32_to_bf16(exp_two(sc - use)));
             l *= al;
@@ -608,8 +613,8 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tb][i]);
                 mx = across_rows(mx, fmax2);
-                if (__ballot(mx > m_run[r] + kTau)) {
-                    const float m_new = fmaxf(m_run[r], mx);
+                if (__ballot(mx > m_run[r] - (kLift - kTau))) {
+                    const float m_new = fmaxf(m_run[r], mx + kLift);
                     const float al = m_new == -__builtin_inff() ? 1.f : exp_two(m_run[r] - m_new);
                     l_run[r] *= al;
 #pragma unroll
@@ -1018,15 +1023,16 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                 for (int v = 0; v < 16; ++v) m4[v & 3] = fmaxf(m4[v & 3], s[tb][v]);
             const float mx = across_halves(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fmax2);
             const float mt = mx == -__builtin_inff() ? mx : mx * c;
-            const bool need = mt > m_run + kTau;
+            const bool need = mt > m_run - (kLift - kTau);
             if (__ballot(need)) {
-                const float al = need ? exp_two(m_run - mt) : 1.f;
+                const float m_new = need ? mt + kLift : m_run;
+                const float al = need ? exp_two(m_run - m_new) : 1.f;
                 l_run *= al;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) o[db][v] *= al;
-                m_run = need ? mt : m_run;
+                m_run = m_new;
             }
             const float mu = m_run == -__builtin_inff() ? 0.f : m_run;
             float l4[4] = {0.f, 0.f, 0.f, 0.f};

@@ -134,3 +134,15 @@ def test_infinite_value_without_weight(form, mx):
     O[..., lost] = 0
     Vc[..., lost] = 0
     _check(O, Kc, Vc, Q, see, rows)
+
+
+@both
+@forms
+def test_values_at_the_types_end(form, mx):
+    """A weighted mean of finite values is finite, however large they are."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 4)
+    V = (V.sign() * 2.5e38).bfloat16()
+    V[..., 0] = 2.5e38
+    O, Kc, Vc = _make(form, mx, K, V, Q)
+    assert Vc.isfinite().all()
+    _check(O * 2.0 ** -100, Kc, Vc * 2.0 ** -100, Q, [L - n + j + 1 for j in range(n)], range(n))
