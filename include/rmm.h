@@ -842,9 +842,11 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * It sees s <= lengths[b] - n + j when causal (the new tokens are the cache's
  * last n), else s < lengths[b] (e.g. an encoder's states).  A token that sees
  * no key gets 0, one that sees keys but only with scores of -infinity NaN.  I = idx[(t*H + h)*k ..) for token t (rmm_select_tokens on the rows of
- * q), or all dims when idx is NULL (k ignored).  A key or value that is
- * infinite or NaN in a dim outside I, or past what a token sees, does not reach
- * it (only the order of its sums may change).
+ * q), or all dims when idx is NULL (k ignored).  A key that is infinite or NaN in
+ * a dim outside I, and a key or value past what a token sees, do not reach it (only
+ * the order of its sums may change).  Where one would have (a list is given, or a value
+ * lies among the last keys, which only some of the new tokens see), the rows whose
+ * result is not finite are gone through again, one row at a time: a slow path.
  * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
  * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.  Values up
  * to bf16's largest do not overflow (over 2^23 keys); below 2^-94 they lose precision.

@@ -251,19 +251,40 @@ __device__ __forceinline__ float2 cached_pair(const uint8_t *rows, const uint8_t
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
-// Query rows first, first + step, ... of a unit over its keys [k0, k1), one row
-// per wave with nothing shared between rows: what the units that meet an
-// infinite or NaN value are redone with, since there a weight or a query of zero
-// does not silence a key or value that a row does not see.  put(row, m, l,
+// whether a value of keys [k0, k1) of kv head kvh is infinite or NaN (whole waves,
+// the same answer in each)
+template <int D, bool MX>
+__device__ __forceinline__ bool odd_values(const PagedArgs &a, int b, int kvh, int k0, int k1) {
+    const int lg = a.kv.lg_page;
+    const int32_t *trow = a.table + b * a.table_ld;
+    bool odd = false;
+#pragma unroll 1
+    for (int i = threadIdx.x & 63; i < (k1 - k0) * (D / 2); i += 64) {
+        const int key = k0 + i / (D / 2), pid = trow[key >> lg], page = pid >= 0 && pid < a.kv.n_pages ? pid : 0;
+        const int64_t row = (static_cast<int64_t>(kvh) << lg) + (key & ((1 << lg) - 1));
+        const float2 v = cached_pair<D, MX>(a.kv.v + page * a.kv.v_page, a.kv.vs + page * a.kv.vs_page, row, 2 * (i % (D / 2)));
+        odd = odd || !(__builtin_fabsf(v.x) < __builtin_inff()) || !(__builtin_fabsf(v.y) < __builtin_inff());
+    }
+    return __ballot(odd) != 0;
+}
+
+// The query rows r of a unit for which wants(r) holds over its keys [k0, k1), one row
+// per wave (the first of `step`) with nothing shared between rows: what a unit's rows are
+// redone with whose result is not finite, where a weight or a query of zero may not have
+// silenced a key or value that the row does not see.  A row with a NaN weight is NaN: the
+// rest of its keys are left out.  put(row, m, l,
 // d, o): reference, sum and two dims of a row's output, called by every lane that holds some.
-template <int D, bool MX, bool IDX, typename Put>
+template <int D, bool MX, bool IDX, typename Wants, typename Put>
 __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, int b, int kvh, int row0, int n_rows,
-                                             int first, int step, int k0, int k1, const uint32_t (*keep)[D / 32], Put put) {
+                                             int first, int step, int k0, int k1, const uint32_t (*keep)[D / 32],
+                                             Wants wants, Put put) {
     const int lane = threadIdx.x & 63, grp = a.q.n / a.kv.Hkv, lg = a.kv.lg_page;
     const int32_t *trow = a.table + b * a.table_ld;
     const int d2 = 2 * lane;                               // the lane's output dims (D / 2 lanes)
+    int nth = 0;
 #pragma unroll 1
-    for (int r = first; r < n_rows; r += step) {
+    for (int r = 0; r < n_rows; ++r) {                     // wave-uniform
+        if (!wants(r) || nth++ % step != first) continue;
         const int tok = (row0 + r) / grp, hd = kvh * grp + (row0 + r) % grp;
         const int see = min(k1, a.causal ? sq.len - sq.n + tok + 1 : sq.len);
         const uint16_t *qp = static_cast<const uint16_t *>(a.q.p) + (sq.q0 + tok) * a.q.st + hd * a.q.sh;
@@ -300,6 +321,7 @@ __device__ __forceinline__ void careful_rows(const PagedArgs &a, const Seq &sq, 
 #pragma unroll
             for (int i = 32; i > 0; i >>= 1) ps += __shfl_xor(ps, i, 64);
             l += ps;
+            if (l != l) break;                             // the same in every lane
 #pragma unroll 1
             for (int i = 0; i < min(64, see - key0); ++i) {
                 const float w = __shfl(p, i, 64);
@@ -391,7 +413,8 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
     constexpr int NBUF = MX && R == 1 ? 2 : 1;            // chunks held
     __shared__ __attribute__((aligned(16))) float oj[kWaves][16][OLD];
     __shared__ float ml[kWaves][16][2];
-    __shared__ int state[kWaves];                         // bit 0: a page or length out of range, bit 1: to be redone
+    __shared__ int bad_of[kWaves];                        // a page or length out of range
+    __shared__ uint64_t odd_of[kWaves];                   // rows whose result is not finite
     __shared__ uint32_t keep[IDX ? ROWS : 1][KS];
     __shared__ uint4 qs[R > 1 ? R * RG : 1][KS][R > 1 ? 64 : 1];
 
@@ -696,9 +719,7 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
         // ---- the waves of a row group join, 16 rows at a time
         const bool complete = w.complete();
         const int part = w.part();
-        // an infinite or NaN key or value that should not count has made these NaN (zero times
-        // it, in a score or a sum)
-        bool odd = false;
+        uint64_t odd = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             l_run[r] = across_rows(l_run[r], add2);
@@ -707,9 +728,10 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
             for (int i = 0; i < DM; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) fin = fin && __builtin_fabsf(o[r][i][e]) < __builtin_inff();
-            odd = odd || (!fin && rg * WROWS + 16 * r + col < n_rows);
+            uint64_t m = __ballot(!fin && rg * WROWS + 16 * r + col < n_rows);      // row col in four lanes
+            m |= m >> 32;
+            odd |= ((m | m >> 16) & 0xffff) << (rg * WROWS + 16 * r);
         }
-        const int mine = (bad ? 1 : 0) | (__ballot(odd) ? 2 : 0);
         // row r of the unit: N dims from d on
         auto put = [&](int r, float m, float ls, int d, const auto &acc) __attribute__((always_inline)) {
             constexpr int N = sizeof(acc) / sizeof(float);
@@ -734,11 +756,15 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                 }
             }
         };
-        int all = 0;
+        bool none = false;                                 // no row of the unit has an answer
+        uint64_t redo = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             __syncthreads();
-            if (r == 0 && lane == 0) state[wave] = mine;
+            if (r == 0 && lane == 0) {
+                bad_of[wave] = bad;
+                odd_of[wave] = odd;
+            }
             if (g == 0) {
                 ml[wave][col][0] = m_run[r];
                 ml[wave][col][1] = l_run[r];
@@ -750,12 +776,22 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
                     *reinterpret_cast<float4 *>(&oj[wave][col][DM * (4 * g + e) + i]) =
                         make_float4(o[r][i][e], o[r][i + 1][e], o[r][i + 2][e], o[r][i + 3][e]);
             __syncthreads();
-            if (r == 0) all = state[0] | state[1] | state[2] | state[3];
+            if (r == 0) {
+                none = (bad_of[0] | bad_of[1] | bad_of[2] | bad_of[3]) != 0;
+                redo = odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3];
+                // an infinite or NaN key (outside a list) or value (of a key that only some rows
+                // see) that should not count has made these NaN, as zero times it; without one
+                // they are what they should be
+                if (__builtin_expect(redo != 0, 0)) {
+                    if (none || (!IDX && !odd_values<D, MX>(a, w.b, kvh, max(lo_lim + 1, w.c0 * TK), min(hi_lim + 1, w.c1 * TK))))
+                        redo = 0;
+                }
+            }
             const int rr = tid >> 4, d0 = (tid & 15) * DM;
 #pragma unroll
             for (int q = 0; q < RG; ++q) {                 // row group q is held by the waves q, q + RG, ...
                 const int row = q * WROWS + 16 * r + rr;
-                if (all == 2 || row >= n_rows) continue;
+                if (row >= n_rows || (redo >> row & 1)) continue;
                 float m = -__builtin_inff(), ls = 0.f, acc[DM];
 #pragma unroll
                 for (int v = 0; v < KG; ++v) m = fmaxf(m, ml[q + RG * v][rr][0]);
@@ -768,11 +804,12 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 #pragma unroll
                     for (int i = 0; i < DM; ++i) acc[i] += al * oj[q + RG * v][rr][d0 + i];
                 }
-                put(row, m, all & 1 ? __builtin_nanf("") : ls, d0, acc);
+                put(row, m, none ? __builtin_nanf("") : ls, d0, acc);
             }
         }
-        if (all == 2)
+        if (__builtin_expect(redo != 0, 0))
             careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, kWaves, w.c0 * TK, w.c1 * TK, keep,
+                                     [&](int r) { return (redo >> r & 1) != 0; },
                                      [&](int r, float m, float ls, int d, float y, float z) {
                                          const float acc[2] = {y, z};
                                          put(r, m, ls, d, acc);
@@ -810,7 +847,8 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     constexpr int CH = RB / 16;                           // 16-byte chunks per row
     __shared__ __attribute__((aligned(1024))) char slot0[2 * KB], slot1[2 * KB], slot2[2 * KB], slot3[2 * KB];
     __shared__ uint32_t keep[IDX ? ROWS : 1][D / 32];
-    __shared__ int state;                                 // bit 0: a page or length out of range, bit 1: to be redone
+    __shared__ int state;                                 // a page or length out of range
+    __shared__ uint32_t odd_of[NW];                       // rows whose result is not finite
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1127,19 +1165,30 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         const bool complete = w.complete();
         const int part = w.part();
         const float l = across_halves(l_run, add2);
-        // an infinite or NaN key or value that should not count has made these NaN (zero times
-        // it, in a score or a sum)
         bool odd = !(l < __builtin_inff());
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int v = 0; v < 16; ++v) odd = odd || !(__builtin_fabsf(o[db][v]) < __builtin_inff());
-        const int mine = (bad ? 1 : 0) | (__ballot(on && odd) ? 2 : 0);
-        if (mine && lane == 0) atomicOr(&state, mine);
+        const uint64_t odd_lanes = __ballot(on && odd);    // row lr in two of them
+        if (lane == 0) {
+            odd_of[wave] = static_cast<uint32_t>(odd_lanes | odd_lanes >> 32);
+            if (bad) atomicOr(&state, 1);
+        }
         __syncthreads();
-        const int all = state;
-        if (all == 2) {
+        const bool none = state != 0;                      // no row of the unit has an answer
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) any |= odd_of[i];
+        // an infinite or NaN key (outside a list) or value (of a key that only some rows see)
+        // that should not count has made these NaN, as zero times it; without one they are
+        // what they should be
+        const int lo = a.causal ? sq.len - sq.n + quot(row0, grp) : sq.len - 1;
+        const bool redo = !none && __builtin_expect(uniform(static_cast<int>(any)) != 0, 0) &&
+                          (IDX || odd_values<D, MX>(a, w.b, kvh, max(lo + 1, w.c0 * TK), min(kend, w.c1 * TK)));
+        if (__builtin_expect(redo, 0)) {
             careful_rows<D, MX, IDX>(a, sq, w.b, kvh, row0, n_rows, wave, NW, w.c0 * TK, w.c1 * TK, keep,
+                                     [&](int r) { return uniform(static_cast<int>(odd_of[r >> 5] >> (r & 31) & 1)) != 0; },
                                      [&](int r, float m, float ls, int d, float x, float y) {
                 if (complete) {
                     const int q = row0 + r;
@@ -1152,8 +1201,9 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
                     *reinterpret_cast<float2 *>(a.part_o + prow * D + d) = make_float2(x, y);
                 }
             });
-        } else if (on) {
-            const float ls = all & 1 ? __builtin_nanf("") : l;
+        }
+        if (on && !(redo && (odd_lanes >> lr | odd_lanes >> (lr + 32)) & 1)) {
+            const float ls = none ? __builtin_nanf("") : l;
             if (complete) {
                 const float inv = row_scale(ls, lim);
                 uint16_t *op = static_cast<uint16_t *>(a.o.p) + (sq.q0 + tok) * a.o.st + hd * a.o.sh + 4 * lh;

@@ -146,3 +146,70 @@ def test_values_at_the_types_end(form, mx):
     O, Kc, Vc = _make(form, mx, K, V, Q)
     assert Vc.isfinite().all()
     _check(O * 2.0 ** -100, Kc, Vc * 2.0 ** -100, Q, [L - n + j + 1 for j in range(n)], range(n))
+
+
+@both
+@forms
+def test_visible_nonfinite_values(form, mx):
+    """Infinite values that every token sees: their dims are infinite or NaN, the other dims and a
+    query of NaN leave the rest alone; with one more NaN that only the last token sees."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 5)
+    Vb, Qb = V.clone(), Q.clone()
+    Vb[L // 3 if n < L // 2 else 0, :, 40] = INF
+    lost = torch.zeros(D, dtype=torch.bool, device=Q.device)
+    lost[slice(32, 64) if mx else 40] = True
+    Qb[n // 2, H - 1, 7] = NAN
+    see = [L - n + j + 1 for j in range(n)]
+    for hidden in (False, True):
+        if hidden:
+            if n == 1:
+                break
+            Vb[L - 1] = NAN
+        O, Kc, Vc = _make(form, mx, K, Vb, Qb)
+        assert O[n // 2, H - 1].isnan().all()
+        assert not O[..., lost].isfinite().any()
+        O[..., lost] = 0
+        Vc[..., lost] = 0
+        if hidden:
+            assert O[n - 1][..., ~lost].isnan().all()
+            Vc[L - 1] = 0
+        rows = [j for j in range(n) if j != n // 2 and not (hidden and j == n - 1)]
+        _check(O, Kc, Vc, Q, see, rows)
+        if H > Hkv:                          # the NaN query's neighbours of the same token
+            assert O[n // 2, :H - 1].isfinite().all() or (hidden and n // 2 == n - 1)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("n,D", [(1, 128), (12, 64), (200, 128)])
+def test_a_poisoned_key_costs_little(n, D, mx):
+    """A NaN key and value that every token sees: the answer is NaN and takes no longer than 20
+    passes without it (a second way through the keys, one row at a time, would)."""
+    dev = require_gpu()
+    L, H, Hkv = 40000, 8, 2
+    g = torch.Generator(device=dev).manual_seed(6)
+    K, V = (torch.randn(L, Hkv, D, device=dev, generator=g).bfloat16() for _ in range(2))
+    Q = torch.randn(n, H, D, device=dev, generator=g).bfloat16()
+    cache = rmm.kv_cache(L // PAGE, Hkv, PAGE, D, mx=mx, device=dev)
+    rmm.rmm_kv_append(K, V, torch.arange(L, dtype=torch.int32, device=dev), cache)
+    table = torch.arange(L // PAGE, dtype=torch.int32, device=dev)[None]
+    length, start = (torch.tensor(x, dtype=torch.int32, device=dev) for x in ([L], [0, n]))
+    O = torch.empty_like(Q)
+
+    def passes():
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        best = 1e9
+        for _ in range(5):
+            ev[0].record()
+            rmm.rmm_paged_attention(Q, cache, table, length, O, q_start=start)
+            ev[1].record()
+            torch.cuda.synchronize()
+            best = min(best, ev[0].elapsed_time(ev[1]))
+        return best
+    clean = passes()
+    assert O.isfinite().all()
+    bad = torch.full((1, Hkv, D), NAN, dtype=torch.bfloat16, device=dev)
+    for k, v in ((bad, bad), (K[L // 2:L // 2 + 1], bad)):
+        rmm.rmm_kv_append(k, v, torch.tensor([L // 2], dtype=torch.int32, device=dev), cache)
+        slow = passes()
+        assert O.isnan().all()
+        assert slow <= 20 * clean, (clean, slow)
