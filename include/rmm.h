@@ -855,7 +855,9 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * one token and one of 700: 811 us, 511 as two calls; 63 and one of 512: 237, 216).
  *
  * Rows of o that belong to no sequence are left as they were.  q_start is
- * ascending from 0 (what it says past T is cut off); a length < 0 counts as 0.
+ * ascending from 0 (what it says past T is cut off; one that falls and rises again,
+ * so that the sequences have more than T tokens between them, makes all outputs NaN);
+ * a length < 0 counts as 0.
  * A length beyond max_pages * page_size makes its sequence's outputs NaN, a page
  * number outside the cache those of the tokens that see a key of it (and may make
  * others of that sequence NaN).  Any dim outside [0, D) in a list is ignored.

@@ -169,6 +169,7 @@ __device__ __forceinline__ bool Walk<TK, ROWS>::init(const PagedArgs &a, int min
     // at sequences l, l + 64, ...
     Seq mine = {0, 0, 0, 0};
     if (lane < a.B) mine = pl.load(a, lane);
+    int64_t tokens = mine.n;
     int most = pl.longest(mine), most2 = pl.longest_pair(mine);
     int w0 = pl.work(mine), blocks = w0, units = pl.units(mine);
     for (int i = lane + 64; i < a.B; i += 64) {
@@ -177,6 +178,14 @@ __device__ __forceinline__ bool Walk<TK, ROWS>::init(const PagedArgs &a, int min
         most2 = max(most2, pl.longest_pair(q));
         blocks += pl.work(q);
         units += pl.units(q);
+        tokens = min(tokens + q.n, a.T + 1);
+    }
+    wg = static_cast<int>(blockIdx.x);
+    over = false;
+    if (a.q_start) {                      // a lane's share is at most 2^31
+        const int lo = prefix_sum(static_cast<int>(tokens & 0xffff)), hi = prefix_sum(static_cast<int>(tokens >> 16));
+        over = (static_cast<int64_t>(__builtin_amdgcn_readlane(hi, 63)) << 16) + __builtin_amdgcn_readlane(lo, 63) > a.T;
+        if (over) return false;
     }
     int sum0 = prefix_sum(blocks);
     int total = __builtin_amdgcn_readlane(sum0, 63);
@@ -240,6 +249,17 @@ template <int TK, int ROWS>
 __device__ __forceinline__ PieceOf piece_of(const Walk<TK, ROWS> &w, int rows) {
     const int first = quot(w.u0, w.run), last = quot(w.u1 - 1, w.run);
     return {last - first + 1, first, rows, w.s.q0, w.kvh, w.tile * ROWS, w.pl.causal ? w.s.len - w.s.n : w.s.len - 1, 0};
+}
+
+// NaN for every output: what a q_start gives whose sequences overlap
+template <int D>
+__device__ __forceinline__ void all_nan(const PagedArgs &a) {
+    const int64_t n = a.T * a.o.n * (D / 8);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const int64_t row = i / (D / 8);
+        uint16_t *op = static_cast<uint16_t *>(a.o.p) + row / a.o.n * a.o.st + row % a.o.n * a.o.sh + 8 * (i % (D / 8));
+        *reinterpret_cast<uint4 *>(op) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+    }
 }
 
 // dims d, d + 1 of a cached row
@@ -429,6 +449,7 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
     Walk<TK, ROWS> w;
     bool more = w.init(a, kMinRun, kCutCost);
     const int wg = w.wg;
+    if (w.over) all_nan<D>(a);
     while (more) {
         if (!w.locate(a)) {
             more = w.x < w.end;
@@ -878,6 +899,7 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     Walk<TK, ROWS> w;
     bool more = w.init(a, kMinRun, kCutCost);
     const int wg = w.wg;
+    if (w.over) all_nan<D>(a);
     while (more) {
         if (!w.locate(a)) {
             more = w.x < w.end;

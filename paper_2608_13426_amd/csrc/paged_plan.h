@@ -104,6 +104,7 @@ template <int TK, int ROWS>
 struct Walk {
     Plan<TK, ROWS> pl;
     int wg;                               // the workgroup's place among the runs
+    bool over;                            // sequences of more than T tokens between them: no line
     int x, begin, end, run;               // position, the workgroup's run, run length
     int b, f;                             // the sequence at x, where it begins
     Seq s;

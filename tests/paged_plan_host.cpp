@@ -7,7 +7,8 @@
 // page size, page table width, T, B, 1 or 0 (q_start given), lengths [B], q_start
 // [B + 1] if given.  Output per case, one line:
 //   rows host_whole whole units run longest_piece most_units_of_a_workgroup cut blocks
-// or "error ..." for a cover that is not exact.
+// "over" where the sequences have more than T tokens between them, or "error ..." for a
+// cover that is not exact.
 #include <cstdio>
 #include <map>
 #include <tuple>
@@ -32,7 +33,7 @@ bool start(pg::Walk<TK, ROWS> &w, const PagedArgs &a, int wg, int min_run, int c
     pl.causal = a.causal;
     pl.Hkv = a.kv.Hkv;
     pl.whole = false;
-    long total = 0;
+    long total = 0, tokens = 0;
     int most = 0, most2 = 0;
     units = 0;
     for (int b = 0; b < a.B; ++b) {
@@ -41,7 +42,11 @@ bool start(pg::Walk<TK, ROWS> &w, const PagedArgs &a, int wg, int min_run, int c
         most2 = max(most2, pl.longest_pair(s));
         total += pl.work(s);
         units += pl.units(s);
+        tokens += s.n;
     }
+    w.wg = wg;
+    w.over = a.q_start && tokens > a.T;
+    if (w.over) return false;
     blocks = total;
     const long rounds = (units + a.nw - 1) / a.nw, room = total / a.nw + cut_cost;
     pl.whole = a.whole || (rounds >> 1) * most2 + (rounds & 1) * most <= room;
@@ -50,7 +55,6 @@ bool start(pg::Walk<TK, ROWS> &w, const PagedArgs &a, int wg, int min_run, int c
     w.run = static_cast<int>((total + a.nw - 1) / a.nw);
     w.run = pl.whole ? max(w.run, 1) : (max(w.run, min_run) + 3) / 4 * 4;
     const int runs = static_cast<int>((total + w.run - 1) / w.run), per = (runs + 7) >> 3;
-    w.wg = wg;
     if ((wg >> 3) < per) w.wg = (wg & 7) * per + (wg >> 3);
     if ((wg >> 3) >= per || w.wg >= runs) return false;
     w.begin = w.x = w.wg * w.run;
@@ -80,6 +84,10 @@ int check(const PagedArgs &a, int min_run, int cut_cost) {
     for (int i = 0; i < a.nw; ++i) {
         pg::Walk<TK, ROWS> w;
         const bool any = start(w, a, i, min_run, cut_cost, units, blocks);
+        if (w.over) {
+            std::printf("over\n");
+            return 0;
+        }
         if (w.wg < 0 || w.wg >= a.nw || places[w.wg]++) return error("place", i, w.wg);
         run = w.run;
         whole = w.pl.whole;

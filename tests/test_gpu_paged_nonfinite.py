@@ -213,3 +213,23 @@ def test_a_poisoned_key_costs_little(n, D, mx):
         slow = passes()
         assert O.isnan().all()
         assert slow <= 20 * clean, (clean, slow)
+
+
+@both
+@pytest.mark.parametrize("n", [1, 8, 40])
+def test_overlapping_sequences(n, mx):
+    """A q_start whose sequences have more tokens than there are: NaN, whatever else it says."""
+    dev = require_gpu()
+    B, H, Hkv, D, L = 70, 4, 2, 128, 100
+    g = torch.Generator(device=dev).manual_seed(7)
+    cache = rmm.kv_cache(8, Hkv, PAGE, D, mx=mx, device=dev)
+    table = (torch.arange(7, device=dev).expand(B, 7) + 1).int().contiguous()
+    length = torch.full((B,), L, dtype=torch.int32, device=dev)
+    Q = torch.randn(n * B, H, D, device=dev, generator=g).bfloat16()
+    rows = torch.full((n * B, H + 1, D), 3.0, dtype=torch.bfloat16, device=dev)
+    start = n * torch.arange(B + 1, dtype=torch.int32, device=dev)
+    rmm.rmm_paged_attention(Q, cache, table, length, rows[:, :H], q_start=start)
+    assert bool((rows[:, :H] == 0).all()) and bool((rows[:, H] == 3).all())      # a cache of zeros
+    start[65] = 0                            # rows 0 .. 66 n once more
+    rmm.rmm_paged_attention(Q, cache, table, length, rows[:, :H], q_start=start)
+    assert rows[:, :H].isnan().all() and bool((rows[:, H] == 3).all())

@@ -22,19 +22,18 @@ def plan(tmp_path_factory):
     subprocess.run([build.HIPCC, "-x", "hip", f"--offload-arch={build.ARCH}", "-O1", "-std=c++17",
                     os.path.join(os.path.dirname(__file__), "paged_plan_host.cpp"), "-o", exe], check=True)
 
-    def run(cases):
+    def run(cases, T=None, q_start=None):
         text = []
         for mx, D, H, Hkv, causal, page, width, lens, news in cases:
-            T = len(lens) if news is None else sum(news)
-            text += [int(mx), D, H, Hkv, int(causal), page, width, T, len(lens), int(news is not None), *lens]
-            if news is not None:
-                text += [sum(news[:b]) for b in range(len(news) + 1)]
+            starts = q_start or (news and [sum(news[:b]) for b in range(len(news) + 1)]) or []
+            n = T or (starts[-1] if starts else len(lens))
+            text += [int(mx), D, H, Hkv, int(causal), page, width, n, len(lens), int(bool(starts)), *lens, *starts]
         out = subprocess.run([exe], input=" ".join(map(str, text)), text=True, check=True, stdout=subprocess.PIPE).stdout
         lines = out.splitlines()
         assert len(lines) == len(cases)
         for c, l in zip(cases, lines):
             assert not l.startswith("error"), (l, c)
-        return [Plan(*map(int, l.split())) for l in lines]
+        return [l if l == "over" else Plan(*map(int, l.split())) for l in lines]
     return run
 
 
@@ -63,6 +62,16 @@ def test_every_key_block_once(plan):
     assert {p.rows for p in plans} == {16, 32, 64, 256}
     assert any(p.host_whole for p in plans) and any(p.whole and not p.host_whole for p in plans)
     assert any(p.cut > 100 for p in plans) and any(p.cut and p.rows == 256 for p in plans)
+
+
+def test_overlapping_sequences(plan):
+    """A q_start that falls and rises again gives sequences of more tokens than there are: past what
+    the line (and 32-bit places on it) was checked for, so such a call has no line."""
+    T, B = 1000, 2000
+    starts = [b % 2 * T for b in range(B + 1)]
+    assert plan([(0, 64, 32, 8, 1, 1024, 1000, [10 ** 6] * B, None)], T=T, q_start=starts) == ["over"]
+    starts = [0] * (B // 2) + [T] * (B // 2 + 1)               # one sequence with all, the others empty
+    assert plan([(0, 64, 32, 8, 1, 1024, 1000, [10 ** 6] * B, None)], T=T, q_start=starts)[0].units == T * 32 // 16
 
 
 def test_long_cases_reach_their_plans(plan):
