@@ -233,3 +233,23 @@ def test_overlapping_sequences(n, mx):
     start[65] = 0                            # rows 0 .. 66 n once more
     rmm.rmm_paged_attention(Q, cache, table, length, rows[:, :H], q_start=start)
     assert rows[:, :H].isnan().all() and bool((rows[:, H] == 3).all())
+
+
+@both
+@forms
+def test_scale_of_zero(form, mx):
+    """The mean of the visible values; NaN where a score is infinite, whichever sign it has."""
+    L, n, H, Hkv, D, K, V, Q = _inputs(form, 8)
+    K[:, :, 5] = 0
+    K[L - n, :, 5] = -2e38
+    Q[:, :, 5] = 0
+    O, Kc, Vc = _make(form, mx, K, V, Q, scale=0.0)
+    see = [L - n + j + 1 for j in range(n)]
+    _check(O, 0 * Kc, Vc, Q, see, range(n))
+    for sign in (1, -1):
+        Qb = Q.clone()
+        Qb[0, 0, 5] = sign * 3e38
+        Ob = _make(form, mx, K, V, Qb, scale=0.0)[0]
+        assert Ob[0, 0].isnan().all()
+        Ob[0, 0] = O[0, 0]
+        assert torch.equal(O, Ob)
