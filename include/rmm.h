@@ -823,7 +823,8 @@ rmm_status_t rmm_kv_append(int64_t T, const rmm_heads_t *k, const rmm_heads_t *v
  * Reads T cached tokens back as bf16 rows (MXFP4 values are exact in bf16 for
  * every scale rmm_kv_append writes); a slot outside the cache gives zeros.
  * k, v : [T] heads, written (any strides: e.g. [Hkv][T][D] for
- * rmm_reduced_attention).  Errors: as rmm_kv_append.
+ * rmm_reduced_attention).  Errors: as rmm_kv_append; UNSUPPORTED from 2^37 elements
+ * of k and v, or T * Hkv = 2^31, on.
  */
 rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, int64_t T, const rmm_heads_t *k,
                            const rmm_heads_t *v, hipStream_t stream);

@@ -166,7 +166,8 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
     if (st == RMM_OK) st = check_heads(v, 2, &vo);
     if (st != RMM_OK) return st;
     if (ko.n != kv.Hkv || vo.n != kv.Hkv) return RMM_ERR_INVALID_ARGUMENT;
-    if (T > kInt32Max / kv.Hkv || !aligned(slots, 4)) return RMM_ERR_UNSUPPORTED;
+    // a thread takes 8 elements of four rows, a launch holds fewer than 2^32 threads
+    if (T > (int64_t(1) << 37) / (2 * kv.Hkv * cache->D) - 1 || T > kInt32Max / kv.Hkv || !aligned(slots, 4)) return RMM_ERR_UNSUPPORTED;
     return from_hip(rmm::launch_kv_gather(kv, slots, T, ko, vo, static_cast<int>(cache->D), stream));
 }
 

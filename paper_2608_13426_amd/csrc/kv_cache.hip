@@ -34,6 +34,9 @@ namespace rmm {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
+// A grid holds fewer than 2^32 threads along an axis (a larger one is launched cut to
+// its low 32 bits): workgroups past this many go on along z.
+constexpr int kGridX = 1 << 22;
 
 // ---- 8 elements of a head
 template <typename T>
@@ -167,8 +170,10 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
 
     // tokens of this workgroup: block `blk` of the batch entry (without
     // energies the whole call is one entry of T tokens), at most 64
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) / blocks, blk = static_cast<int64_t>(blockIdx.x) % blocks;
+    const int64_t place = static_cast<int64_t>(blockIdx.z) * kGridX + blockIdx.x;
+    const int64_t unit = place / blocks, blk = place % blocks;
     const int64_t per = ENERGY ? a.L : a.T, t0 = unit * per + blk * TB;
+    if (t0 >= a.T) return;
     const int n = static_cast<int>(min(static_cast<int64_t>(TB), per - blk * TB));
     // lane i holds the position and slot of token i
     int pos_of = 0, slot_of = -1;
@@ -176,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
         if (a.rot) pos_of = a.pos[t0 + lane];
         if constexpr (KV != 0) slot_of = a.slots[t0 + lane];
     }
-    auto place = [&](int i, int64_t &b, int64_t &l) __attribute__((always_inline)) {
+    auto where = [&](int i, int64_t &b, int64_t &l) __attribute__((always_inline)) {
         const int64_t t = t0 + i;
         b = ENERGY ? unit : static_cast<int64_t>(static_cast<uint32_t>(t) / static_cast<uint32_t>(a.L));
         l = t - b * a.L;
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
     const bool turn2 = kind < 2 && a.rot && (a.interleaved ? 8 * pc.c2 < a.rot : pc.on);
     auto load = [&](Token &k, int i) __attribute__((always_inline)) {
         int64_t b, l;
-        place(i, b, l);
+        where(i, b, l);
         const T *x = in + b * isb + l * ist;
         k.r1 = *reinterpret_cast<const Raw8<T> *>(x + 8 * pc.c1);
         k.r2 = *reinterpret_cast<const Raw8<T> *>(x + 8 * pc.c2);
@@ -211,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int TB, 
     };
     auto token = [&](const Token &k, int i) __attribute__((always_inline)) {
         int64_t b, l;
-        place(i, b, l);
+        where(i, b, l);
         float x1[8], x2[8];
         load8(k.r1.x, x1);
         load8(k.r2.x, x2);
@@ -421,7 +426,8 @@ hipError_t launch(const RotateArgs &a, hipStream_t stream) {
     const int nv = a.q.n + a.k.n + a.v.n, groups = (nv + 1024 / D - 1) / (1024 / D);
     const int TB = rotate_tokens(a.T, ENERGY ? a.q.n : nv, D, ENERGY);
     const int64_t per = ENERGY ? a.L : a.T, blocks = (per + TB - 1) / TB, units = ENERGY ? a.T / a.L : 1;
-    const dim3 grid(static_cast<uint32_t>(units * blocks), static_cast<uint32_t>(groups));
+    const int64_t all = units * blocks, nz = (all + kGridX - 1) / kGridX;
+    const dim3 grid(static_cast<uint32_t>(nz > 1 ? kGridX : all), static_cast<uint32_t>(groups), static_cast<uint32_t>(nz));
     if (a.gq || a.gk) rotate_kernel<T, D, KV, true, ENERGY><<<grid, kThreads, 0, stream>>>(a, TB, blocks);
     else rotate_kernel<T, D, KV, false, ENERGY><<<grid, kThreads, 0, stream>>>(a, TB, blocks);
     return hipGetLastError();

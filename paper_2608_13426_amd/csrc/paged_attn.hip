@@ -1068,6 +1068,12 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
         };
         auto softmax = [&](int kt) __attribute__((always_inline)) {
             const int t0 = kt * TK;
+            if (__builtin_expect(a.c == 0.f, 0)) {         // 0 times an infinite score is NaN
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s[tb][v] *= a.c;
+            }
             if (t0 + TK - 1 > lim_lo) {                    // the tile crosses some row's limit
                 const int rel = in_branch(lim - t0 - 4 * lh);
 #pragma unroll

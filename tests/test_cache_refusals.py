@@ -25,3 +25,10 @@ def test_attention_scale(scale):
 @pytest.mark.parametrize("scale", [0.0, -0.0, 1e-45, -0.1, 2e38])
 def test_attention_scale_in_range(scale):
     assert attention(scale) == WS_SMALL
+
+
+@pytest.mark.parametrize("T,D", [(2 ** 27, 128), (2 ** 28, 64), (2 ** 28 - 1, 128)])
+def test_gather_past_a_grid(T, D):
+    """2^32 threads and more, of which a launch would run the low 32 bits' worth."""
+    c, h = abi.cache(D=D), abi.heads()
+    assert rmm.lib.rmm_kv_gather(ctypes.byref(c), P, T, ctypes.byref(h), ctypes.byref(h), None) == UNSUPPORTED
