@@ -805,7 +805,9 @@ typedef struct rmm_kv_cache {
  *             rmm_qk_norm_rope (values are neither normed nor rotated).
  * slots     : int32 [T]; a token whose slot is outside the cache (e.g. -1) is
  *             not appended.  Slots of one call should differ: of tokens with the same
- *             slot, each 8-element piece is some one's.
+ *             slot, each 8-element piece is some one's, and in a 4-bit cache each
+ *             scale byte too -- 8 codes of one token may come to stand under the scale of
+ *             another, for values that neither had.
  * RMM_CACHE_MX: each group of 32 dims takes the smallest scale at which its
  *             largest magnitude, rounded, is at most 6 (s kept within 8..252;
  *             255 when the group holds a NaN or an infinity), and rounds each

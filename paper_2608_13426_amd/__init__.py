@@ -1094,7 +1094,7 @@ def rmm_kv_append(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, cache: 
                   gamma_k: torch.Tensor | None = None, eps: float = 1e-6, Q: torch.Tensor | None = None,
                   Qo: torch.Tensor | None = None, gamma_q: torch.Tensor | None = None, stream=None) -> KvCache:
     """Appends K and V [T, Hkv, D] (bf16) at the slots (int32 [T]: page *
-    page_size + place; outside the cache, e.g. -1: not appended), K normed
+    page_size + place, all different; outside the cache, e.g. -1: not appended), K normed
     (gamma_k) and rotated (rope, positions int32 [T]) on the way; with Q and Qo
     [T, H, D] the tokens' queries are normed (gamma_q) and rotated in the same
     launch."""

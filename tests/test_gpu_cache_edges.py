@@ -26,3 +26,26 @@ def test_rotate_more_entries_than_a_grid():
         rmm.rmm_qk_norm_rope(Q[s], o, pos[s].contiguous(), rope, energy=f.view(-1))
         assert torch.equal(Qo[s], o) and torch.equal(e[s], f)
         assert torch.equal(f, o.view(-1, D).double().square())
+
+
+def test_same_slot_twice_with_other_scales():
+    """In a 4-bit cache every 8 codes and every scale byte of a slot named twice are one of its
+    tokens'; other slots are as they should be."""
+    dev = require_gpu()
+    Hkv, D, T = 2, 128, 6
+    g = torch.Generator(device=dev).manual_seed(5)
+    x = torch.randn(T, Hkv, D, device=dev, generator=g)
+    x = (x * 2.0 ** (3 * torch.arange(T, device=dev))[:, None, None]).bfloat16()
+    alone = rmm.kv_cache(1, Hkv, 16, D, mx=True, device=dev)
+    rmm.rmm_kv_append(x, x, torch.arange(T, dtype=torch.int32, device=dev), alone)
+    assert alone.k_scale[0, :, :T].unique().numel() >= T
+    cache = rmm.kv_cache(1, Hkv, 16, D, mx=True, device=dev)
+    rmm.rmm_kv_append(x, x, torch.tensor([3, 9, 3, 3, 11, 3], dtype=torch.int32, device=dev), cache)
+    for t, s in ((cache.k, alone.k), (cache.v, alone.v), (cache.k_scale, alone.k_scale), (cache.v_scale, alone.v_scale)):
+        n = 4 if t.shape[-1] == D // 2 else 1              # bytes of a piece
+        assert torch.equal(t[0, :, 9], s[0, :, 1]) and torch.equal(t[0, :, 11], s[0, :, 4])
+        got, of = t[0, :, 3].view(Hkv, 1, -1, n), s[0][:, [0, 2, 3, 5]].view(Hkv, 4, -1, n)
+        assert (got == of).all(-1).any(1).all()
+        rest = torch.ones(16, dtype=torch.bool, device=dev)
+        rest[[3, 9, 11]] = False
+        assert bool((t[0][:, rest] == 0).all())
