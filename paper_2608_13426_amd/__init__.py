@@ -1052,7 +1052,7 @@ def rmm_qk_norm_rope_workspace_size(batch: int, H: int, L: int, D: int) -> int:
     return int(lib.rmm_qk_norm_rope_workspace_size(int(batch), int(H), int(L), int(D)))
 
 
-def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor | None = None,
+def rmm_qk_norm_rope(Q: torch.Tensor | None, Qo: torch.Tensor | None, positions: torch.Tensor | None = None,
                      rope: Rope | None = None, K: torch.Tensor | None = None, Ko: torch.Tensor | None = None,
                      gamma_q: torch.Tensor | None = None, gamma_k: torch.Tensor | None = None, eps: float = 1e-6,
                      energy: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
@@ -1060,17 +1060,24 @@ def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor 
     """Per-head RMSNorm (with gamma_q, gamma_k [D]) and position rotation of Q
     [batch, L, H, D] into Qo [batch, H, L, D], and of K [batch, L, Hkv, D] into Ko
     [batch, Hkv, L, D]; any strides with contiguous heads (slices of a
-    projection's rows, transposed views).  positions: int32 [batch*L].  energy
+    projection's rows, transposed views); Q and Qo, or K and Ko, may be left out
+    (None).  positions: int32 [batch*L].  energy
     (float64 [batch*H*D]) receives the column energies of each head of Qo.
     `workspace` (uint8, rmm_qk_norm_rope_workspace_size(...) bytes) is allocated
     here when energy is wanted and it is not given."""
-    if Q.dim() != 4 or (K is None) != (Ko is None) or (K is not None and K.dim() != 4):
-        raise ValueError("Q must be [batch, L, H, D] and K [batch, L, Hkv, D]; K and Ko come together")
-    batch, L, H, D = Q.shape
-    dt = Q.dtype
-    code = _dtype_code(Q)
-    q = _heads(Q, (batch, L, H, D), dt, "Q", "[batch, L, H, D]", True)
-    qo = _heads(Qo, (batch, H, L, D), dt, "Qo", "[batch, H, L, D]", True, True)
+    if (Q is None) != (Qo is None) or (K is None) != (Ko is None) or (Q is None and K is None) or \
+            (Q is not None and Q.dim() != 4) or (K is not None and K.dim() != 4):
+        raise ValueError("Q must be [batch, L, H, D] and K [batch, L, Hkv, D]; Q and Qo, K and Ko come together")
+    if Q is None and energy is not None:
+        raise ValueError("the energies are the queries'")
+    x = K if Q is None else Q
+    batch, L, H, D = x.shape
+    dt = x.dtype
+    code = _dtype_code(x)
+    q = qo = None
+    if Q is not None:
+        q = _heads(Q, (batch, L, H, D), dt, "Q", "[batch, L, H, D]", True)
+        qo = _heads(Qo, (batch, H, L, D), dt, "Qo", "[batch, H, L, D]", True, True)
     k = ko = None
     if K is not None:
         Hkv = K.shape[2]
@@ -1086,7 +1093,7 @@ def rmm_qk_norm_rope(Q: torch.Tensor, Qo: torch.Tensor, positions: torch.Tensor 
          _vec(gamma_k, D, dt, "gamma_k"), eps, None if rope is None else rope._c,
          _positions(rope, positions, batch * L), _vec(energy, batch * H * D, torch.float64, "energy"),
          _ptr(workspace), ws_bytes)
-    return Qo
+    return Ko if Q is None else Qo
 
 
 def rmm_kv_append(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, cache: KvCache,

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2608_13426_amd as rmm
 from tests import test_cache_abi as abi
@@ -32,3 +33,18 @@ def test_gather_past_a_grid(T, D):
     """2^32 threads and more, of which a launch would run the low 32 bits' worth."""
     c, h = abi.cache(D=D), abi.heads()
     assert rmm.lib.rmm_kv_gather(ctypes.byref(c), P, T, ctypes.byref(h), ctypes.byref(h), None) == UNSUPPORTED
+
+
+def test_binding_keys_alone():
+    """What the binding asks of a call without queries (CPU tensors reach no launch)."""
+    K = torch.zeros(1, 3, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        rmm.rmm_qk_norm_rope(None, None, K=K, Ko=K.transpose(1, 2))
+    for args in (dict(), dict(K=K), dict(Ko=K)):
+        with pytest.raises(ValueError, match="together"):
+            rmm.rmm_qk_norm_rope(None, None, **args)
+    for q, qo in ((K, None), (None, K.transpose(1, 2))):
+        with pytest.raises(ValueError, match="together"):
+            rmm.rmm_qk_norm_rope(q, qo, K=K, Ko=K.transpose(1, 2))
+    with pytest.raises(ValueError, match="energies"):
+        rmm.rmm_qk_norm_rope(None, None, K=K, Ko=K.transpose(1, 2), energy=torch.zeros(256, dtype=torch.float64))

@@ -1,4 +1,5 @@
 """Rotation, appending and reading back at the edges of what the cache entry points take."""
+import pytest
 import torch
 
 import paper_2608_13426_amd as rmm
@@ -49,3 +50,20 @@ def test_same_slot_twice_with_other_scales():
         rest = torch.ones(16, dtype=torch.bool, device=dev)
         rest[[3, 9, 11]] = False
         assert bool((t[0][:, rest] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rotate_keys_alone(dtype):
+    """Keys without queries: as beside them, in place too."""
+    dev = require_gpu()
+    g = torch.Generator(device=dev).manual_seed(4)
+    Q, K = (torch.randn(2, 37, n, 128, device=dev, generator=g).to(dtype) for n in (6, 3))
+    rope = rmm.Rope(*rmm.rope_tables(100, 128, device=dev))
+    pos = torch.arange(74, dtype=torch.int32, device=dev)
+    gk = torch.randn(128, device=dev, generator=g).to(dtype)
+    Qo, Ko, Ka = (torch.empty(2, n, 37, 128, dtype=dtype, device=dev) for n in (6, 3, 3))
+    rmm.rmm_qk_norm_rope(Q, Qo, pos, rope, K=K, Ko=Ko, gamma_k=gk)
+    assert rmm.rmm_qk_norm_rope(None, None, pos, rope, K=K, Ko=Ka, gamma_k=gk) is Ka
+    assert torch.equal(Ka, Ko)
+    rmm.rmm_qk_norm_rope(None, None, pos, rope, K=K, Ko=K.transpose(1, 2), gamma_k=gk)
+    assert torch.equal(K.transpose(1, 2), Ko)
