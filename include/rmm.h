@@ -852,7 +852,7 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * result is not finite are gone through again, one row at a time: a slow path.
  * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
  * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.  Values up
- * to bf16's largest do not overflow (over 2^23 keys); below 2^-94 they lose precision.
+ * to bf16's largest do not overflow; below 2^-94 they lose precision.
  * How rows are grouped follows the average T*H / (B*Hkv): where long prompts and
  * single tokens come together, a call for each kind is faster (255 sequences of
  * one token and one of 700: 811 us, 511 as two calls; 63 and one of 512: 237, 216).

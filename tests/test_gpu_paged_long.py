@@ -120,3 +120,35 @@ def test_short(lens, news, H, Hkv, D, page, causal, r, scale, mx):
             kv = [torch.empty(L, Hkv, D, dtype=torch.bfloat16, device=dev) for _ in range(2)]
             _compare(O, Q, rmm.rmm_kv_gather(cache, slots, *kv), [b], lens, starts, news, Hkv,
                      D ** -0.5 if scale is None else float(np.float32(scale)), causal, unrounded, f"sequence {b}", keep)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("n,H,Hkv,D", [(1, 8, 2, 128), (7, 8, 2, 64), (12, 8, 2, 64), (40, 4, 2, 128), (90, 8, 2, 64),
+                                       (300, 4, 2, 128)])
+def test_rising_maximum(n, H, Hkv, D, mx):
+    """Two keys have all the weight, the heavier one later and in the same stream of keys: each is
+    the largest when it comes, so neither weight is rounded and what is left are the scores' errors
+    and the output's rounding.  Their values almost cancel, which makes a rounded weight show."""
+    dev = require_gpu()
+    L, page, at = 1000, 16, 130
+    g = torch.Generator(device=dev).manual_seed(n)
+    cache = rmm.kv_cache(-(-L // page), Hkv, page, D, mx=mx, device=dev)
+    K, V = torch.zeros(L, Hkv, D, device=dev), torch.zeros(L, Hkv, D, device=dev)
+    K[:, :, 5], K[0, :, 5], K[at, :, 5] = -96, 0, 2
+    V[0], V[at] = 6, torch.tensor([-1.0, -0.5, -0.25, -0.125], device=dev).repeat(D // 4)
+    slots = torch.arange(L, dtype=torch.int32, device=dev)
+    rmm.rmm_kv_append(K.bfloat16(), V.bfloat16(), slots, cache)
+    Q = torch.zeros(n, H, D, dtype=torch.bfloat16, device=dev)
+    Q[:, :, 5] = (8 + 16 * torch.rand(n, H, device=dev, generator=g)) * (D / 128) ** 0.5     # scores of 1.4 to 4.2
+    O = torch.empty_like(Q)
+    rmm.rmm_paged_attention(Q, cache, slots.view(1, -1)[:, :-(-L // page)].contiguous(),
+                            torch.tensor([L], dtype=torch.int32, device=dev), O,
+                            q_start=torch.tensor([0, n], dtype=torch.int32, device=dev))
+    k, v = (torch.empty(L, Hkv, D, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    rmm.rmm_kv_gather(cache, slots, k, v)
+    q = Q.double().view(n * H, D)
+    assert torch.equal(k, K.bfloat16()) and torch.equal(v, V.bfloat16())
+    want, _, _ = pr.attend(q, k[:, 0].double(), v[:, 0].double(), torch.full((n * H,), L, device=dev), D ** -0.5, False)
+    eps = (8 * 6 + 64) * 4 * 2.0 ** -24              # relative, of a weight: scores of up to 6, the exponential
+    limit = 1.01 * 2.0 ** -8 * want.abs() + 8 * eps
+    assert bool(((O.double().view(n * H, D) - want).abs() <= limit).all())
