@@ -849,13 +849,16 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * a dim outside I, and a key or value past what a token sees, do not reach it (only
  * the order of its sums may change).  Where one would have (a list is given, or a value
  * lies among the last keys, which only some of the new tokens see), the rows whose
- * result is not finite are gone through again, one row at a time: a slow path.
+ * result is not finite are gone through again, one row at a time: a slow path (200
+ * tokens of 8 heads of 128 behind 40000 keys, 0.08 ms: 1.2 ms where the last token's value
+ * is NaN, 17 ms where a key is NaN in a dim that no list names; 1024 behind 131000: 0.55 ms,
+ * 0.3 s both).
  * Scores and softmax in fp32, the weights rounded to bf16 for the value product,
  * fp32 accumulation, bf16 output; a fixed order for given lengths and sizes.  Values up
  * to bf16's largest do not overflow; below 2^-94 they lose precision.
  * How rows are grouped follows the average T*H / (B*Hkv): where long prompts and
  * single tokens come together, a call for each kind is faster (255 sequences of
- * one token and one of 700: 811 us, 511 as two calls; 63 and one of 512: 237, 216).
+ * one token and one of 700: 820 us, 510 as two calls; 63 and one of 512: 245, 215).
  *
  * Rows of o that belong to no sequence are left as they were.  q_start is
  * ascending from 0 (what it says past T is cut off; one that falls and rises again,
@@ -869,7 +872,10 @@ rmm_status_t rmm_kv_gather(const rmm_kv_cache_t *cache, const int32_t *slots, in
  * page_table: int32 [B][table_stride], max_pages entries used per row.
  * lengths   : int32 [B].   q_start: int32 [B+1] or NULL.   idx: int32 [T*H*k].
  * workspace : rmm_paged_attention_workspace_size(T, B, H, Hkv, D) bytes, 256-byte
- *             aligned (partial outputs; overwritten by every call).
+ *             aligned (partial outputs; overwritten by every call).  The size follows
+ *             T*H / (B*Hkv) and can be larger for fewer tokens or sequences: one buffer
+ *             for calls of several sizes takes the largest of theirs, which is at most
+ *             66 MiB for heads of 128, 34 MiB for heads of 64.
  * Errors    : INVALID_ARGUMENT for null pointers, T, B, max_pages < 1, a scale that is
  *             NaN or infinite (or is, times log2 e), table_stride < max_pages, q_start NULL with T != B, H not a
  *             multiple of the cache's Hkv, o's head count not H, k outside

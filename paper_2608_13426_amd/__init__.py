@@ -1145,8 +1145,9 @@ def rmm_paged_attention(Q: torch.Tensor, cache: KvCache, page_table: torch.Tenso
     (int32 [B, max_pages], rows contiguous) and has the new tokens q_start[b] ..
     q_start[b+1]-1 (int32 [B+1]; None: one each).  Causal: they are its last ones.
     idx (int32 [T, H, k]): the dims each (token, head) keeps.  `workspace`
-    (uint8, rmm_paged_attention_workspace_size(...) bytes, 256-byte aligned) is
-    allocated here when not given."""
+    (uint8, rmm_paged_attention_workspace_size(...) bytes, 256-byte aligned; the
+    size is not monotonous: for several T and B the largest of theirs) is allocated
+    here when not given."""
     if Q.dim() != 3:
         raise ValueError("Q must be [T, H, D]")
     T, H, _ = Q.shape

@@ -46,7 +46,8 @@ namespace pg {
 // weight is then a power of two, which bf16 holds exactly.  Following only a maximum 2^8
 // above the last one gave that weight the others' rounding (two chunks of 1024 tokens
 // 0.0020 off float64 for 0.0017, the output's own rounding being 0.0016; 5 drafted tokens
-// 0.0018 for 0.0016; single tokens 0.0017 for 0.00165) and saved 1 to 2 %.
+// 0.0018 for 0.0016; single tokens 0.0017 for 0.00165) and saved up to 3 % (the chunks
+// 250 us for 254, heads of 64 176 for 182; single tokens nothing).
 constexpr float kLift = 32.f;
 
 // f over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (all of them get the result)
@@ -859,9 +860,11 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 // workgroup take the softmax at opposite ends of a step, so that one's
 // exponentials meet the other's matrix instructions.
 // Two prompts' chunks of 1024 tokens behind 7000 cached ones, 32 heads of 128 on 8
-// (239 GFLOP): 240 to 280 us, 850 to 990 TFLOP/s of the 1103 that a large product
-// reaches, and 5 joining; from a 4-bit cache 342, since the tiles then pass through
-// registers.  At 256 registers per lane a larger tile of either kind spills.
+// (239 GFLOP): 247 to 260 us a call over the boxes, 920 to 970 TFLOP/s of the 1103 that a
+// large product reaches, 5 us of it joining; from a 4-bit cache 300 to 308, since the tiles
+// then pass through registers; heads of 64 175 to 182 (660 to 680 TFLOP/s: the
+// exponentials of as many scores beside half the matrix work).  At 256 registers per lane
+// a larger tile of either kind spills.
 template <int D, bool MX, bool IDX>
 __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
     using namespace pg;
@@ -1048,7 +1051,8 @@ __global__ __launch_bounds__(rowsk::NT, 1) void paged_rows_kernel(PagedArgs a) {
             for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
         float m_run = -__builtin_inff(), l_run = 0.f;
         // the sum is of the rounded weights where that costs nothing (two chunks of 1024
-        // tokens, heads of 64: 204 us either way; heads of 128: 284 against 257, so of the unrounded)
+        // tokens, heads of 64: 182 us, 184 unrounded; heads of 128: 268 against 254, for the same
+        // error of 0.0017, so of the unrounded)
         constexpr bool ROUNDED = D == 64;
         f32x16_t s[2];
         uint4 pf[TK / 16];

@@ -48,3 +48,13 @@ def test_binding_keys_alone():
             rmm.rmm_qk_norm_rope(q, qo, K=K, Ko=K.transpose(1, 2))
     with pytest.raises(ValueError, match="energies"):
         rmm.rmm_qk_norm_rope(None, None, K=K, Ko=K.transpose(1, 2), energy=torch.zeros(256, dtype=torch.float64))
+
+
+def test_attention_workspace_size():
+    """Not monotonous, and below what the header says."""
+    f = rmm.rmm_paged_attention_workspace_size
+    assert f(64, 64, 32, 8, 128) < f(64, 1, 32, 8, 128)
+    # 512 pieces of 256 rows of D sums, two statistics and 32 bytes: 65.02 and 33.02 MiB
+    for D, top in ((128, 66 << 20), (64, 34 << 20)):
+        sizes = [f(T, B, 8 * g, 8, D) for T in (1, 7, 64, 300, 5000, 100000) for B in (1, 3, 64, 300, 5000) for g in (1, 4, 40)]
+        assert 0 < min(sizes) and max(sizes) <= top
