@@ -860,7 +860,7 @@ __global__ __launch_bounds__(few::kThreads, 2) void paged_few_kernel(PagedArgs a
 // workgroup take the softmax at opposite ends of a step, so that one's
 // exponentials meet the other's matrix instructions.
 // Two prompts' chunks of 1024 tokens behind 7000 cached ones, 32 heads of 128 on 8
-// (239 GFLOP): 247 to 260 us a call over the boxes, 920 to 970 TFLOP/s of the 1103 that a
+// (239 GFLOP): 247 to 260 us a call over several cards, 920 to 970 TFLOP/s of the 1103 that a
 // large product reaches, 5 us of it joining; from a 4-bit cache 300 to 308, since the tiles
 // then pass through registers; heads of 64 175 to 182 (660 to 680 TFLOP/s: the
 // exponentials of as many scores beside half the matrix work).  At 256 registers per lane

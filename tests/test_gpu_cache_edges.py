@@ -67,3 +67,37 @@ def test_rotate_keys_alone(dtype):
     assert torch.equal(Ka, Ko)
     rmm.rmm_qk_norm_rope(None, None, pos, rope, K=K, Ko=K.transpose(1, 2), gamma_k=gk)
     assert torch.equal(K.transpose(1, 2), Ko)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_calls_on_two_streams_at_once(mx):
+    """Calls that allocate their own workspaces, in turn on the current stream and on another one,
+    with nothing between them to wait for: cut units, whose pieces pass through the workspace."""
+    dev = require_gpu()
+    lens, H, Hkv, D, page = [9000, 300, 4000], 8, 2, 128, 16
+    g = torch.Generator(device=dev).manual_seed(6)
+    per = -(-max(lens) // page)
+    cache = rmm.kv_cache(3 * per, Hkv, page, D, mx=mx, device=dev)
+    table = torch.arange(3 * per, dtype=torch.int32, device=dev).view(3, per)
+    for b, L in enumerate(lens):
+        kv = [torch.randn(L, Hkv, D, device=dev, generator=g).bfloat16() for _ in range(2)]
+        rmm.rmm_kv_append(*kv, torch.arange(L, dtype=torch.int32, device=dev) + b * per * page, cache)
+    length = torch.tensor(lens, dtype=torch.int32, device=dev)
+    Qs = torch.randn(8, 3, H, D, device=dev, generator=g).bfloat16()
+    want = torch.stack([rmm.rmm_paged_attention(q, cache, table, length, torch.empty_like(q)) for q in Qs])
+    L = 2000
+    X = torch.randn(8, 1, L, H, D, device=dev, generator=g).bfloat16()
+    e = torch.zeros(8, H * D, dtype=torch.float64, device=dev)
+    for x, f in zip(X, e):
+        rmm.rmm_qk_norm_rope(x, torch.empty(1, H, L, D, dtype=x.dtype, device=dev), energy=f)
+    s = torch.cuda.Stream(dev)
+    for _ in range(3):
+        O, E = torch.zeros_like(want), torch.zeros_like(e)
+        Xo = torch.empty(8, 1, H, L, D, dtype=X.dtype, device=dev)
+        torch.cuda.synchronize()
+        for i in range(8):
+            st = s if i % 2 else None
+            rmm.rmm_qk_norm_rope(X[i], Xo[i], energy=E[i], stream=st)
+            rmm.rmm_paged_attention(Qs[i], cache, table, length, O[i], stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(O, want) and torch.equal(E, e)
