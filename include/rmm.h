@@ -892,6 +892,156 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
                                  const int32_t *idx, int64_t k, float scale, int causal, const rmm_heads_t *o,
                                  void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * The reduced products with bias, activation and residual in their epilogue
+ * (Sec. 3.2 definition; Sec. 3.3 projections):
+ *
+ *   Y[b][m][n] = act(sum over j in I_b of X[b][m][j] W[j][n]  + bias[n])
+ *                + residual_scale * residual[b][m][n]
+ *
+ * evaluated in fp32 from the fp32 sums and rounded once to the output type.  act:
+ * none; relu; silu x / (1 + e^-x); gelu x Phi(x) (the normal distribution
+ * function); gelu_tanh x / (1 + e^(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3).
+ *
+ * epilogue: host struct (NULL: none of the three).  bias: N values of the
+ *           product's type, or NULL.  residual: of the product's type, [B][M][ldr]
+ *           (units M*ldr apart), or NULL (residual_scale is then not read); it may
+ *           be Y itself (ldr == ldy) and must not overlap it otherwise.  16-byte
+ *           aligned rows and bias are read fastest.
+ * Everything else as rmm_reduced_gemm (B <= 65535, M <= 65535*32),
+ * rmm_reduced_gemm_kmajor and rmm_reduced_gemv (bf16, M <= 8; workspace
+ * rmm_gemv_workspace_size).
+ * Errors  : as those, and INVALID_ARGUMENT for an unknown act, ldr < N, a
+ *           residual_scale that is NaN or infinite, residual == Y with another
+ *           ldr, bias or residual off their type's alignment.
+ */
+typedef enum rmm_act {
+    RMM_ACT_NONE = 0,
+    RMM_ACT_RELU = 1,
+    RMM_ACT_SILU = 2,
+    RMM_ACT_GELU = 3,
+    RMM_ACT_GELU_TANH = 4
+} rmm_act_t;
+typedef struct rmm_epilogue {
+    const void *bias;
+    rmm_act_t act;
+    float residual_scale;
+    const void *residual;
+    int64_t ldr;
+} rmm_epilogue_t;
+rmm_status_t rmm_reduced_gemm_epilogue(const void *X, const void *W, const int32_t *idx, rmm_dtype_t dtype,
+                                       int64_t B, int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldx,
+                                       int64_t ldw, void *Y, int64_t ldy, const rmm_epilogue_t *epilogue,
+                                       hipStream_t stream);
+rmm_status_t rmm_reduced_gemm_kmajor_epilogue(const void *Xt, const void *W, const int32_t *idx, int64_t B,
+                                              int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldxt,
+                                              int64_t ldw, void *Y, int64_t ldy,
+                                              const rmm_epilogue_t *epilogue, hipStream_t stream);
+rmm_status_t rmm_reduced_gemv_epilogue(const void *X, const void *W, const int32_t *idx, int64_t B, int64_t M,
+                                       int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw, void *Y,
+                                       int64_t ldy, const rmm_epilogue_t *epilogue, void *workspace,
+                                       size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A block's output joined to the residual stream, with the norm that feeds the
+ * next block's reduced projections (Sec. 3.2: scores from the projection's own
+ * input; the Limitations' memory movement of a separate scoring pass):
+ *
+ *   y = Y,  or  Y * r(Y) * post_gamma          (post_norm != 0: a norm after the block)
+ *   H = residual_scale * R + gate * y          stored in the stream's type
+ *   X = H * r(H) * pre_gamma                   (the norm before the next block)
+ *   r(v) = 1 / sqrt(mean over the row of v^2 + eps)
+ *
+ * The norm before the next block is of the stored H.  Mean squares are float64
+ * sums, r is rounded to fp32; every other step is one fp32 operation in the order
+ * written, and H and X are rounded once, so neither depends on sizes or strides.
+ *
+ * dtype       : RMM_BF16 or RMM_F32, of Y, X, the gammas and the gate.
+ * stream_dtype: of R and H; RMM_F32 also where dtype is RMM_BF16.
+ * Y, R        : [B][M] rows of K (units M*ld apart); either may be NULL (its term
+ *               is then left out; without Y neither post_norm nor a gate).
+ * gate        : or NULL; element (b, m, j) at b*gate_unit_stride +
+ *               m*gate_row_stride + j (strides of 0: shared).
+ * gammas      : [K], or NULL (ones).
+ * H, X        : written, [B][M] rows; either may be NULL.  H may be R and X may
+ *               be Y (same leading dimension).
+ * Xt, energy  : instead of X, its K-major copy Xt[b][j][m] (row stride ldxt, columns
+ *               past M left as they were) and energy[b*K + j] = sum over m of
+ *               Xt[b][j][m]^2 (float64, fixed order), for rmm_select and
+ *               rmm_reduced_gemm_kmajor; bf16, needs H.
+ * workspace   : rmm_block_join_workspace_size(B, M, K) bytes with Xt, 256-byte
+ *               aligned (else not used).
+ * Rows that are 16-byte aligned with K % 8 == 0 are read fastest.
+ * Errors      : INVALID_ARGUMENT for sizes < 1, both Y and R or all outputs
+ *               missing, Xt without energy or H, leading dimensions below the
+ *               widths, negative gate strides, eps negative, infinite or NaN, an
+ *               infinite or NaN residual_scale, pointers off their type's alignment;
+ *               UNSUPPORTED for both X and Xt, fp32 with a bf16 stream, K > 65536,
+ *               B*M >= 2^22, B > 65535, and with Xt unless dtype is bf16, K % 8 == 0,
+ *               ldxt % 8 == 0 and Xt, H's rows and pre_gamma are 16-byte aligned;
+ *               WORKSPACE_TOO_SMALL.
+ */
+typedef struct rmm_join {
+    rmm_dtype_t dtype, stream_dtype;
+    int64_t B, M, K;
+    const void *Y;
+    int64_t ldy;
+    const void *R;
+    int64_t ldr;
+    float residual_scale;
+    int post_norm;
+    const void *post_gamma;
+    const void *gate;
+    int64_t gate_unit_stride, gate_row_stride;
+    const void *pre_gamma;
+    float eps;
+    void *H;
+    int64_t ldh;
+    void *X;
+    int64_t ldx;
+    void *Xt;
+    int64_t ldxt;
+    double *energy;
+} rmm_join_t;
+size_t rmm_block_join_workspace_size(int64_t B, int64_t M, int64_t K);
+rmm_status_t rmm_block_join(const rmm_join_t *join, void *workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
+/*
+ * Log probabilities of given tokens, entropy and the most likely tokens of rows of
+ * logits (the read-out of an output projection, reduced or not), in one pass:
+ *
+ *   p = softmax(scale * logits[t])                     over the V logits of row t
+ *   logp[t*given + i]    = log p[tokens[t*given + i]];  0 for a token of -1 (a padded
+ *                          place), NaN for any other token outside [0, V)
+ *   entropy[t]           = - sum over i of p_i log p_i
+ *   top_idx[t*top + i]   = the token of the i-th largest logit (ties to the lower
+ *                          token, -0 equals +0, NaN above +infinity), and top_logp its log p
+ *
+ * A logit of -infinity has weight 0.  A row of nothing else has no weights: its log
+ * probabilities are -infinity and its entropy 0.  In a row with a NaN or +infinity
+ * entropy and all log probabilities are NaN.  Logits are subtracted before they are
+ * scaled, so one of the type's lowest value acts as a mask, and a row of nothing else
+ * is uniform.  Sums in fp32 per lane, joined in float64; a fixed order for given sizes.
+ *
+ * logits    : [T] rows of V, leading dimension ldl; dtype RMM_BF16 or RMM_F32.
+ * scale     : > 0 (the inverse temperature).
+ * tokens    : int32 [T][given], logp float32 [T][given]; given may be 0 (both then
+ *             unused).   entropy: float32 [T], or NULL.
+ * top       : 0 to min(V, 64); top_idx int32 and top_logp float32 [T][top].
+ * workspace : rmm_token_logprobs_workspace_size(T, V, top) bytes, 8-byte aligned (may
+ *             be NULL when that size is 0).
+ * Errors    : INVALID_ARGUMENT for null pointers, sizes < 1, ldl < V, a scale that is
+ *             not positive or infinite, negative given or top, top > V, nothing asked
+ *             for, pointers off their type's alignment; UNSUPPORTED for top > 64, T >=
+ *             2^22 or V >= 2^30; WORKSPACE_TOO_SMALL.
+ */
+size_t rmm_token_logprobs_workspace_size(int64_t T, int64_t V, int64_t top);
+rmm_status_t rmm_token_logprobs(const void *logits, rmm_dtype_t dtype, int64_t T, int64_t V, int64_t ldl,
+                                float scale, const int32_t *tokens, int64_t given, float *logp,
+                                float *entropy, int64_t top, int32_t *top_idx, float *top_logp,
+                                void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char *rmm_status_string(rmm_status_t status);
 

@@ -184,10 +184,10 @@ rmm_status_t rmm_reduced_gemm(const void *X, const void *W, const int32_t *idx, 
     if (dtype == RMM_BF16)
         return from_hip(rmm::launch_gemm_bf16(
             static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(W), idx, B, M, N, K, k,
-            ldx, ldw, static_cast<uint16_t *>(Y), ldy, stream));
+            ldx, ldw, static_cast<uint16_t *>(Y), ldy, nullptr, stream));
     return from_hip(rmm::launch_gemm_f32(static_cast<const float *>(X),
                                          static_cast<const float *>(W), idx, B, M, N, K, k, ldx,
-                                         ldw, static_cast<float *>(Y), ldy, stream));
+                                         ldw, static_cast<float *>(Y), ldy, nullptr, stream));
 }
 
 rmm_status_t rmm_select_tokens(const void *X, rmm_dtype_t dtype, int64_t B, int64_t K,
@@ -223,7 +223,7 @@ rmm_status_t rmm_reduced_gemv(const void *X, const void *W, const int32_t *idx, 
     }
     return from_hip(rmm::launch_gemv_bf16(static_cast<const uint16_t *>(X),
                                           static_cast<const uint16_t *>(W), idx, B, M, N, K, k, ldx,
-                                          ldw, static_cast<uint16_t *>(Y), ldy, workspace, stream));
+                                          ldw, static_cast<uint16_t *>(Y), ldy, workspace, nullptr, stream));
 }
 
 rmm_status_t rmm_reduced_gemm_kmajor(const void *Xt, const void *W, const int32_t *idx, int64_t B,
@@ -236,7 +236,7 @@ rmm_status_t rmm_reduced_gemm_kmajor(const void *Xt, const void *W, const int32_
     if (!kmajor_ok(Xt, W, B, M, K, ldxt, ldw)) return RMM_ERR_UNSUPPORTED;
     return from_hip(rmm::launch_gemm_kmajor_bf16(static_cast<const uint16_t *>(Xt),
                                                  static_cast<const uint16_t *>(W), idx, B, M, N, K, k,
-                                                 ldxt, ldw, static_cast<uint16_t *>(Y), ldy, stream));
+                                                 ldxt, ldw, static_cast<uint16_t *>(Y), ldy, nullptr, stream));
 }
 
 size_t rmm_gemm_swiglu_workspace_size(int64_t B, int64_t M, int64_t F) {
@@ -397,14 +397,14 @@ rmm_status_t rmm_linear(const void *X, const void *W, double r, rmm_dtype_t dtyp
     if (e != hipSuccess) return RMM_ERR_HIP;
     if (kmajor)
         e = rmm::launch_gemm_kmajor_bf16(Xt, static_cast<const uint16_t *>(W), idx, B, M, N, K, k,
-                                         xt_ld(M), ldw, static_cast<uint16_t *>(Y), ldy, stream);
+                                         xt_ld(M), ldw, static_cast<uint16_t *>(Y), ldy, nullptr, stream);
     else if (dtype == RMM_BF16)
         e = rmm::launch_gemm_bf16(static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(W),
                                   idx, B, M, N, K, k, ldx, ldw, static_cast<uint16_t *>(Y), ldy,
-                                  stream);
+                                  nullptr, stream);
     else
         e = rmm::launch_gemm_f32(static_cast<const float *>(X), static_cast<const float *>(W), idx,
-                                 B, M, N, K, k, ldx, ldw, static_cast<float *>(Y), ldy, stream);
+                                 B, M, N, K, k, ldx, ldw, static_cast<float *>(Y), ldy, nullptr, stream);
     return from_hip(e);
 }
 
@@ -460,15 +460,15 @@ rmm_status_t rmm_reduced_pv(const void *P, const void *V, rmm_dtype_t dtype, int
             if (kmajor)
                 e = rmm::launch_gemm_kmajor_bf16(Pt + u0 * Lk * xt_ld(Lq), reinterpret_cast<const uint16_t *>(Vg),
                                                  ig, grp, Lq, D, Lk, kt, xt_ld(Lq), D,
-                                                 reinterpret_cast<uint16_t *>(Og), D, stream);
+                                                 reinterpret_cast<uint16_t *>(Og), D, nullptr, stream);
             else if (bf16)
                 e = rmm::launch_gemm_bf16(static_cast<const uint16_t *>(P) + u0 * Lq * ldp,
                                           reinterpret_cast<const uint16_t *>(Vg), ig, grp, Lq, D, Lk, kt,
-                                          ldp, D, reinterpret_cast<uint16_t *>(Og), D, stream);
+                                          ldp, D, reinterpret_cast<uint16_t *>(Og), D, nullptr, stream);
             else
                 e = rmm::launch_gemm_f32(static_cast<const float *>(P) + u0 * Lq * ldp,
                                          reinterpret_cast<const float *>(Vg), ig, grp, Lq, D, Lk, kt,
-                                         ldp, D, reinterpret_cast<float *>(Og), D, stream);
+                                         ldp, D, reinterpret_cast<float *>(Og), D, nullptr, stream);
         }
     return from_hip(e);
 }

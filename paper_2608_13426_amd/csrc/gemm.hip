@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "device_common.h"
+#include "epilogue.h"
 #include "kernels.h"
 
 namespace rmm {
@@ -23,11 +24,11 @@ namespace rmm {
 namespace {
 
 // ------------------------------------------------------------------ bf16
-template <int BM, int BN, int BK, int WM, int WN, bool VECW>
+template <int BM, int BN, int BK, int WM, int WN, bool VECW, bool EP = false>
 __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W,
     const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
-    int64_t ldx, int64_t ldw, int64_t ldy) {
+    int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}) {
     constexpr int NT = WM * WN * kWave;
     constexpr int TM = BM / WM, TN = BN / WN;        // per-wave tile
     constexpr int FM = TM / 32, FN = TN / 32;        // 32x32 fragments per wave
@@ -141,7 +142,11 @@ __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int m = m0 + wm * TM + i * 32 + 8 * (v / 4) + 4 * (lane / 32) + (v % 4);
-                if (m < M && n < N) Y[static_cast<int64_t>(m) * ldy + n] = f32_to_bf16(acc[i][j][v]);
+                if (m < M && n < N) {
+                    float y = acc[i][j][v];
+                    if constexpr (EP) y = ep_value<uint16_t>(ep, y, unit * M + m, n);
+                    Y[static_cast<int64_t>(m) * ldy + n] = f32_to_bf16(y);
+                }
             }
         }
 }
@@ -383,7 +388,8 @@ __device__ __forceinline__ uint32_t swiglu_bf16(uint32_t gb, uint32_t ub) {
 //   store them),
 // and part[(unit * tiles_m + m0/256) * N/2 + c] = sum over its rows m < M of
 // Ht[unit][c][m]^2 in float64 (one row tile's share of that input's column
-// energies).
+// energies).  2: Y = act(the product + bias) + rs * residual, from the fp32
+// accumulators.
 //
 // BNT is the tile's width in n: 256 (eight waves, one workgroup per CU), or
 // 128 (four waves of the same 128 x 64 wave tile, 72 KiB of LDS, two
@@ -396,7 +402,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
     const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
     int64_t ldxt, int64_t ldw, int64_t ldy, int64_t xt_bytes, int64_t w_bytes, int tiles_m,
     int tiles_n, int vec_y, double *__restrict__ part, int64_t w_ustride = 0, int w_ugroup = 1,
-    int trim = 0, int64_t trim_off = 0) {
+    int trim = 0, int64_t trim_off = 0, Epilogue ep = {}) {
     using namespace trk;
     constexpr int ASZ = BKS * ROWB;      // X operand, one stage
     constexpr int ROWBB = BNT * 2;       // bytes per staged W row
@@ -739,6 +745,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
         }
         return;
     }
+    if constexpr (EPI == 2)
+        ep_fragments<FN, FM>(ep, acc, lane, wm * 128, n0 + wn * TWN, min(BT, M - m0),
+                             unit * static_cast<int64_t>(M) + m0, N);
     uint16_t *Yu = Y + unit * static_cast<int64_t>(M) * ldy;
     const int rows = min(BT, M - m0);
     const __amdgpu_buffer_rsrc_t yr = __builtin_amdgcn_make_buffer_rsrc(
@@ -834,10 +843,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
 // Against the 64 x 64 VALU tile it replaces (us): 128 x 512 -> 512 at k = 256
 // 46.3 -> 11.2 (launch included; 7.1 alone), 1024^3 at k = 512 131 -> 25, 4096^3
 // at k = 2048 1433 -> 908 (76 of about 150 TFLOP/s); the same error.
-template <int BM, int BN, int BK, bool VECW, bool VECY>
+template <int BM, int BN, int BK, bool VECW, bool VECY, bool EP = false>
 __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
     const float *__restrict__ X, const float *__restrict__ W, const int32_t *__restrict__ idx,
-    float *__restrict__ Y, int M, int N, int k, int64_t ldx, int64_t ldw, int64_t ldy) {
+    float *__restrict__ Y, int M, int N, int k, int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}) {
     constexpr int LS = BK + 4;                       // floats per LDS row
     constexpr int FM = BM / 32, FN = BN / 32;        // 16 x 16 fragments per wave
     constexpr int RPP = 256 / BK, XR = BM / RPP;     // X rows per pass and per thread
@@ -942,7 +951,10 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     const int n = n0 + wnb + 16 * j + lr;
-                    if (n < N) Y[static_cast<int64_t>(m) * ldy + n] = acc[j][i][r];
+                    if (n >= N) continue;
+                    float y = acc[j][i][r];
+                    if constexpr (EP) y = ep_value<float>(ep, y, unit * M + m, n);
+                    Y[static_cast<int64_t>(m) * ldy + n] = y;
                 }
             }
         return;
@@ -955,6 +967,11 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
         for (int j = 0; j < FN; ++j) {
             const int n = n0 + wnb + 16 * j + 4 * lg;
             float *p = Y + static_cast<int64_t>(m) * ldy + n;
+            if constexpr (EP) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < N) acc[j][i][r] = ep_value<float>(ep, acc[j][i][r], unit * M + m, n + r);
+            }
             if (n + 4 <= N) {
                 *reinterpret_cast<f32x4_t *>(p) = acc[j][i];
             } else {
@@ -973,14 +990,14 @@ constexpr int kBigWaves = 4;
 hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t *idx,
                             int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                             int64_t ldx, int64_t ldw, uint16_t *Y, int64_t ldy,
-                            hipStream_t stream) {
+                            const Epilogue *ep, hipStream_t stream) {
     (void)K;
     const bool vec = (reinterpret_cast<uintptr_t>(W) % 16 == 0) && (ldw % 8 == 0);
     const int64_t big_tiles = ((M + big::BM - 1) / big::BM) * ((N + big::BN - 1) / big::BN);
     const int64_t w_bytes = K * ldw * 2;
     const bool offsets_fit = static_cast<int64_t>(big::BM + 1) * ldx * 2 < (int64_t(1) << 31) &&
                              w_bytes + ldw * 2 < (int64_t(1) << 31);
-    if (vec && offsets_fit && big_tiles * B >= 128) {
+    if (vec && offsets_fit && big_tiles * B >= 128 && !ep) {
         const int tm = static_cast<int>((M + big::BM - 1) / big::BM);
         const int tn = static_cast<int>((N + big::BN - 1) / big::BN);
         dim3 grid(static_cast<unsigned>(tm * tn), static_cast<unsigned>(B));
@@ -992,6 +1009,15 @@ hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t 
     constexpr int BM = 128, BN = 128, BK = 32, WM = 2, WN = 2;
     dim3 grid(static_cast<unsigned>((N + BN - 1) / BN), static_cast<unsigned>((M + BM - 1) / BM),
               static_cast<unsigned>(B));
+    if (ep) {
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(WM * WN * kWave), 0, stream, X, W, idx, Y,
+                               static_cast<int>(M), static_cast<int>(N), static_cast<int>(k), ldx, ldw, ldy, *ep);
+            return hipGetLastError();
+        };
+        return vec ? launch(gemm_gather_bf16_kernel<BM, BN, BK, WM, WN, true, true>)
+                   : launch(gemm_gather_bf16_kernel<BM, BN, BK, WM, WN, false, true>);
+    }
     if (vec)
         hipLaunchKernelGGL((gemm_gather_bf16_kernel<BM, BN, BK, WM, WN, true>), grid,
                            dim3(WM * WN * kWave), 0, stream, X, W, idx, Y, static_cast<int>(M),
@@ -1029,7 +1055,7 @@ KmajorTile kmajor_tile(int64_t B, int64_t M, int64_t N) {
 hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t *idx, int64_t B,
                            int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldxt, int64_t ldw,
                            uint16_t *Y, int64_t ldy, int64_t w_ustride, int w_ugroup,
-                           int trim, int64_t trim_off, hipStream_t stream) {
+                           int trim, int64_t trim_off, const Epilogue *ep, hipStream_t stream) {
     const int64_t xt_bytes = K * ldxt * 2, w_bytes = K * ldw * 2;
     const bool grouped = (w_ustride != 0 && w_ugroup < B) || trim;
     // the 256 x 256 kernel addresses one tile's Y rows with 32-bit byte offsets
@@ -1045,9 +1071,19 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
     const bool tall = N <= 128 && !trim && (M + 127) / 128 * B > 1024;
     if (!big_ok || (N <= 128 && !tall) || (N > 128 && tile != KmajorTile::k256))
         return launch_gemm_kmajor_mid_bf16(tile != KmajorTile::k64, Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y,
-                                           ldy, w_ustride, w_ugroup, trim, trim_off, stream);
+                                           ldy, w_ustride, w_ugroup, trim, trim_off, ep, stream);
     const int vec_y = (reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0) ? 2
                       : (reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0) ? 1 : 0;
+    if (ep) {
+        auto launch = [&](auto kernel, int waves, int tn_) {
+            hipLaunchKernelGGL(kernel, dim3(tm * tn_, static_cast<unsigned>(B)), dim3(waves * 64), 0, stream, Xt, W,
+                               idx, Y, static_cast<int>(M), static_cast<int>(N), static_cast<int>(k), ldxt, ldw, ldy,
+                               xt_bytes, w_bytes, tm, tn_, vec_y, nullptr, w_ustride, w_ugroup, trim, trim_off, *ep);
+            return hipGetLastError();
+        };
+        return tall ? launch(gemm_kmajor_tr_kernel<4, kTrRows, kTrStages, 2, 128, 2>, 4, 1)
+                    : launch(gemm_kmajor_tr_kernel<kTrWaves, kTrRows, kTrStages, 2>, kTrWaves, tn);
+    }
     if (tall) {
         hipLaunchKernelGGL((gemm_kmajor_tr_kernel<4, kTrRows, kTrStages, 0, 128, 2>),
                            dim3(tm, static_cast<unsigned>(B)), dim3(4 * 64), 0, stream,
@@ -1069,8 +1105,8 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
 hipError_t launch_gemm_kmajor_bf16(const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
                                   int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                                   int64_t ldxt, int64_t ldw, uint16_t *Y, int64_t ldy,
-                                  hipStream_t stream) {
-    return kmajor_dispatch(Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y, ldy, 0, 1, 0, 0, stream);
+                                  const Epilogue *ep, hipStream_t stream) {
+    return kmajor_dispatch(Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y, ldy, 0, 1, 0, 0, ep, stream);
 }
 
 hipError_t launch_gemm_kmajor_grouped_bf16(const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
@@ -1079,7 +1115,7 @@ hipError_t launch_gemm_kmajor_grouped_bf16(const uint16_t *Xt, const uint16_t *W
                                           int64_t w_ustride, int w_ugroup, int trim, int64_t trim_off,
                                           hipStream_t stream) {
     return kmajor_dispatch(Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y, ldy, w_ustride, w_ugroup, trim,
-                           trim_off, stream);
+                           trim_off, nullptr, stream);
 }
 
 hipError_t launch_gemm_swiglu_kmajor_bf16(const uint16_t *Xt, const uint16_t *W,
@@ -1101,7 +1137,7 @@ hipError_t launch_gemm_swiglu_kmajor_bf16(const uint16_t *Xt, const uint16_t *W,
 
 hipError_t launch_gemm_f32(const float *X, const float *W, const int32_t *idx, int64_t B,
                            int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw,
-                           float *Y, int64_t ldy, hipStream_t stream) {
+                           float *Y, int64_t ldy, const Epilogue *ep, hipStream_t stream) {
     (void)K;
     const bool vec = reinterpret_cast<uintptr_t>(W) % 16 == 0 && ldw % 4 == 0;
     const bool vec_y = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 4 == 0;
@@ -1117,16 +1153,18 @@ hipError_t launch_gemm_f32(const float *X, const float *W, const int32_t *idx, i
         dim3 grid(static_cast<unsigned>((N + t - 1) / t), static_cast<unsigned>((M + t - 1) / t),
                   static_cast<unsigned>(B));
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, X, W, idx, Y, static_cast<int>(M),
-                           static_cast<int>(N), static_cast<int>(k), ldx, ldw, ldy);
+                           static_cast<int>(N), static_cast<int>(k), ldx, ldw, ldy, ep ? *ep : Epilogue{});
         return hipGetLastError();
     };
-    auto pick = [&](auto bm, auto bk) {
+    auto rows = [&](auto bm, auto bk, auto with) {
         constexpr int BM = decltype(bm)::value, BK = decltype(bk)::value;
-        return vec ? (vec_y ? launch(gemm_gather_f32_kernel<BM, BM, BK, true, true>)
-                            : launch(gemm_gather_f32_kernel<BM, BM, BK, true, false>))
-                   : (vec_y ? launch(gemm_gather_f32_kernel<BM, BM, BK, false, true>)
-                            : launch(gemm_gather_f32_kernel<BM, BM, BK, false, false>));
+        constexpr bool EP = decltype(with)::value;
+        return vec ? (vec_y ? launch(gemm_gather_f32_kernel<BM, BM, BK, true, true, EP>)
+                            : launch(gemm_gather_f32_kernel<BM, BM, BK, true, false, EP>))
+                   : (vec_y ? launch(gemm_gather_f32_kernel<BM, BM, BK, false, true, EP>)
+                            : launch(gemm_gather_f32_kernel<BM, BM, BK, false, false, EP>));
     };
+    auto pick = [&](auto bm, auto bk) { return ep ? rows(bm, bk, std::true_type{}) : rows(bm, bk, std::false_type{}); };
     using I16 = std::integral_constant<int, 16>;
     using I32 = std::integral_constant<int, 32>;
     using I64 = std::integral_constant<int, 64>;

@@ -34,6 +34,7 @@
 #include <type_traits>
 
 #include "device_common.h"
+#include "epilogue.h"
 #include "kernels.h"
 
 namespace rmm {
@@ -62,12 +63,12 @@ __device__ __forceinline__ int mid_swz(int r) {
 // a one-dimensional grid the units then go round fastest and the tiles with
 // the longest loops first, so that the short ones fill the tail (32 heads x
 // 4096 causal queries, 2048 kept tokens: 67 us; 107 with 256 x 128 tiles).
-template <int BM, int BN, int WM, int WN, int BKS, int S>
+template <int BM, int BN, int WM, int WN, int BKS, int S, bool EP = false>
 __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kernel(
     const uint16_t *__restrict__ Xt, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
     uint16_t *__restrict__ Y, int B, int M, int N, int k, int64_t ldxt, int64_t ldw, int64_t ldy,
     int64_t xt_bytes, int64_t w_bytes, int tiles_m, int tiles_n, int vec_y, int64_t w_ustride,
-    int w_ugroup, int trim, int64_t trim_off) {
+    int w_ugroup, int trim, int64_t trim_off, Epilogue ep = {}) {
     constexpr int NW = WM * WN, NT = NW * 64;
     constexpr int RA = BM * 2, RB = BN * 2;             // bytes per staged row
     constexpr int ASZ = BKS * RA, BSZ = BKS * RB;
@@ -271,6 +272,8 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kerne
     const int lr = lane & 31, lh = lane >> 5;
     uint16_t *Yt = Y + (static_cast<int64_t>(unit) * M + m0) * ldy;
     const int rows = min(BM, M - m0);
+    if constexpr (EP)
+        ep_fragments<FN, FM>(ep, acc, lane, wm * TM, n0 + wn * TN, rows, static_cast<int64_t>(unit) * M + m0, N);
     if constexpr (BM == 64) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -350,17 +353,22 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kerne
 template <int BM, int BN, int WM, int WN, int BKS, int S>
 hipError_t launch_mid(const uint16_t *Xt, const uint16_t *W, const int32_t *idx, int64_t B, int64_t M,
                       int64_t N, int64_t K, int64_t k, int64_t ldxt, int64_t ldw, uint16_t *Y, int64_t ldy,
-                      int64_t w_ustride, int w_ugroup, int trim, int64_t trim_off, hipStream_t stream) {
+                      int64_t w_ustride, int w_ugroup, int trim, int64_t trim_off, const Epilogue *ep,
+                      hipStream_t stream) {
     const int vec_y = (reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0) ? 2
                       : (reinterpret_cast<uintptr_t>(Y) % 8 == 0 && ldy % 4 == 0) ? 1 : 0;
     const int64_t tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const bool flat = trim && tm * tn * B <= (1 << 22);
     const dim3 grid(static_cast<unsigned>(flat ? tm * tn * B : tm * tn), static_cast<unsigned>(flat ? 1 : B));
-    hipLaunchKernelGGL((gemm_kmajor_mid_kernel<BM, BN, WM, WN, BKS, S>), grid, dim3(WM * WN * 64), 0,
-                       stream, Xt, W, idx, Y, static_cast<int>(B), static_cast<int>(M), static_cast<int>(N),
-                       static_cast<int>(k), ldxt, ldw, ldy, K * ldxt * 2, K * ldw * 2, static_cast<int>(tm),
-                       static_cast<int>(tn), vec_y, w_ustride, w_ugroup, trim, trim_off);
-    return hipGetLastError();
+    auto launch = [&](auto kernel, const Epilogue &e) {
+        hipLaunchKernelGGL(kernel, grid, dim3(WM * WN * 64), 0,
+                           stream, Xt, W, idx, Y, static_cast<int>(B), static_cast<int>(M), static_cast<int>(N),
+                           static_cast<int>(k), ldxt, ldw, ldy, K * ldxt * 2, K * ldw * 2, static_cast<int>(tm),
+                           static_cast<int>(tn), vec_y, w_ustride, w_ugroup, trim, trim_off, e);
+        return hipGetLastError();
+    };
+    return ep ? launch(gemm_kmajor_mid_kernel<BM, BN, WM, WN, BKS, S, true>, *ep)
+              : launch(gemm_kmajor_mid_kernel<BM, BN, WM, WN, BKS, S>, Epilogue{});
 }
 
 }  // namespace
@@ -368,11 +376,11 @@ hipError_t launch_mid(const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
 hipError_t launch_gemm_kmajor_mid_bf16(bool wide, const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
                                        int64_t B, int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldxt,
                                        int64_t ldw, uint16_t *Y, int64_t ldy, int64_t w_ustride, int w_ugroup,
-                                       int trim, int64_t trim_off, hipStream_t stream) {
+                                       int trim, int64_t trim_off, const Epilogue *ep, hipStream_t stream) {
     return wide ? launch_mid<128, 128, 2, 4, 32, 4>(Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y, ldy, w_ustride,
-                                                       w_ugroup, trim, trim_off, stream)
+                                                       w_ugroup, trim, trim_off, ep, stream)
                 : launch_mid<64, 64, 2, 2, 64, 4>(Xt, W, idx, B, M, N, K, k, ldxt, ldw, Y, ldy, w_ustride,
-                                                     w_ugroup, trim, trim_off, stream);
+                                                     w_ugroup, trim, trim_off, ep, stream);
 }
 
 }  // namespace rmm

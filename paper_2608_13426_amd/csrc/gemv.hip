@@ -14,6 +14,7 @@
 // order (or, with one slice, the workgroup writes Y directly), so results
 // are bit-reproducible.
 #include "device_common.h"
+#include "epilogue.h"
 #include "kernels.h"
 
 namespace rmm {
@@ -30,11 +31,12 @@ constexpr int MIN_SLICE = 64;      // retained rows per slice at least
 
 // One workgroup's share: columns chunk*CW .., slice s of unit b's retained
 // list; DIRECT writes Y, otherwise the slice's fp32 partials.
-template <int MR, bool VEC>
+template <int MR, bool VEC, bool EP = false>
 __device__ __forceinline__ void gemv_tile(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
     float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
-    int64_t ldw, int64_t ldy, int SR, int S, int chunk, int s, int b, bool DIRECT) {
+    int64_t ldw, int64_t ldy, int SR, int S, int chunk, int s, int b, bool DIRECT,
+    const Epilogue &ep = Epilogue{}) {
     using namespace gv;
     __shared__ uint32_t roff[RB];              // byte offset of each staged row in W
     __shared__ float xs[RB][MR];               // its activation value per row m
@@ -131,22 +133,24 @@ __device__ __forceinline__ void gemv_tile(
         for (int e = 0; e < 8; ++e) {
             const int n = nb + e;
             if (n < N) {
-                if (DIRECT)
-                    Y[(static_cast<int64_t>(b) * M + m) * ldy + n] = f32_to_bf16(acc[m][e]);
-                else
+                if (DIRECT) {
+                    const int64_t row = static_cast<int64_t>(b) * M + m;
+                    if constexpr (EP) acc[m][e] = ep_value<uint16_t>(ep, acc[m][e], row, n);
+                    Y[row * ldy + n] = f32_to_bf16(acc[m][e]);
+                } else
                     P[((static_cast<int64_t>(b) * S + s) * M + m) * N + n] = acc[m][e];
             }
         }
     }
 }
 
-template <int MR, bool VEC, bool DIRECT>
+template <int MR, bool VEC, bool DIRECT, bool EP = false>
 __global__ __launch_bounds__(gv::NT) void gemv_partial_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
     float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
-    int64_t ldw, int64_t ldy, int SR, int S) {
-    gemv_tile<MR, VEC>(X, W, idx, P, Y, M, N, K, k, ldx, ldw, ldy, SR, S, blockIdx.x, blockIdx.y,
-                       blockIdx.z, DIRECT);
+    int64_t ldw, int64_t ldy, int SR, int S, Epilogue ep = {}) {
+    gemv_tile<MR, VEC, EP>(X, W, idx, P, Y, M, N, K, k, ldx, ldw, ldy, SR, S, blockIdx.x, blockIdx.y,
+                           blockIdx.z, DIRECT, ep);
 }
 
 // Several independent one-row products in one launch: the workgroups of
@@ -191,14 +195,19 @@ __device__ __forceinline__ float reduce_slices(const float *__restrict__ p, int6
 
 // Y[b][m][n] = the slices' partials P[b][s][m][n] added in the order of
 // reduce_slices; workgroup (x, m, b) covers columns 64x .. 64x+63
+template <bool EP = false>
 __global__ __launch_bounds__(256) void gemv_reduce_kernel(const float *__restrict__ P,
                                                           uint16_t *__restrict__ Y, int M, int N,
-                                                          int S, int64_t ldy) {
+                                                          int S, int64_t ldy, Epilogue ep = {}) {
     const int n = blockIdx.x * 64 + (threadIdx.x & 63);
     const int m = blockIdx.y, b = blockIdx.z;
     const float *p = P + (static_cast<int64_t>(b) * S * M + m) * N + n;
-    const float sum = reduce_slices(p, static_cast<int64_t>(M) * N, S, n < N);
-    if (threadIdx.x < 64 && n < N) Y[(static_cast<int64_t>(b) * M + m) * ldy + n] = f32_to_bf16(sum);
+    float sum = reduce_slices(p, static_cast<int64_t>(M) * N, S, n < N);
+    if (threadIdx.x < 64 && n < N) {
+        const int64_t row = static_cast<int64_t>(b) * M + m;
+        if constexpr (EP) sum = ep_value<uint16_t>(ep, sum, row, n);
+        Y[row * ldy + n] = f32_to_bf16(sum);
+    }
 }
 
 // the slice reduction of every group with more than one slice: workgroup
@@ -216,37 +225,40 @@ __global__ __launch_bounds__(256) void gemv_reduce_grouped_kernel(GemvGroups G) 
     if (threadIdx.x < 64 && n < q.N) q.Y[static_cast<int64_t>(b) * q.ldy + n] = f32_to_bf16(sum);
 }
 
-template <int MR, bool VEC>
+template <int MR, bool VEC, bool EP>
 hipError_t launch_mr(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B, int64_t M,
                      int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw, uint16_t *Y,
-                     int64_t ldy, float *P, int SR, int S, hipStream_t stream) {
+                     int64_t ldy, float *P, int SR, int S, const Epilogue &ep, hipStream_t stream) {
     using namespace gv;
     dim3 grid(static_cast<unsigned>((N + CW - 1) / CW), static_cast<unsigned>(S), static_cast<unsigned>(B));
     if (S == 1) {
-        hipLaunchKernelGGL((gemv_partial_kernel<MR, VEC, true>), grid, dim3(NT), 0, stream, X, W, idx,
+        hipLaunchKernelGGL((gemv_partial_kernel<MR, VEC, true, EP>), grid, dim3(NT), 0, stream, X, W, idx,
                            P, Y, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K),
-                           static_cast<int>(k), ldx, ldw, ldy, SR, S);
+                           static_cast<int>(k), ldx, ldw, ldy, SR, S, ep);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((gemv_partial_kernel<MR, VEC, false>), grid, dim3(NT), 0, stream, X, W, idx,
                        P, Y, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K),
-                       static_cast<int>(k), ldx, ldw, ldy, SR, S);
+                       static_cast<int>(k), ldx, ldw, ldy, SR, S, Epilogue{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     dim3 rgrid(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>(M), static_cast<unsigned>(B));
-    hipLaunchKernelGGL(gemv_reduce_kernel, rgrid, dim3(256), 0, stream, P, Y, static_cast<int>(M),
-                       static_cast<int>(N), S, ldy);
+    hipLaunchKernelGGL(gemv_reduce_kernel<EP>, rgrid, dim3(256), 0, stream, P, Y, static_cast<int>(M),
+                       static_cast<int>(N), S, ldy, ep);
     return hipGetLastError();
 }
 
-template <bool VEC>
+template <bool VEC, bool EP>
 hipError_t launch_vec(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B, int64_t M,
                       int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw, uint16_t *Y,
-                      int64_t ldy, float *P, int SR, int S, hipStream_t stream) {
-    if (M == 1) return launch_mr<1, VEC>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream);
-    if (M == 2) return launch_mr<2, VEC>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream);
-    if (M <= 4) return launch_mr<4, VEC>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream);
-    return launch_mr<8, VEC>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream);
+                      int64_t ldy, float *P, int SR, int S, const Epilogue &ep, hipStream_t stream) {
+    auto go = [&](auto mr) {
+        return launch_mr<decltype(mr)::value, VEC, EP>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, ep, stream);
+    };
+    if (M == 1) return go(std::integral_constant<int, 1>{});
+    if (M == 2) return go(std::integral_constant<int, 2>{});
+    if (M <= 4) return go(std::integral_constant<int, 4>{});
+    return go(std::integral_constant<int, 8>{});
 }
 
 }  // namespace
@@ -293,13 +305,17 @@ hipError_t launch_gemv_grouped_bf16(GemvGroups G, int64_t B, hipStream_t stream)
 
 hipError_t launch_gemv_bf16(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B,
                             int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw,
-                            uint16_t *Y, int64_t ldy, void *workspace, hipStream_t stream) {
+                            uint16_t *Y, int64_t ldy, void *workspace, const Epilogue *ep,
+                            hipStream_t stream) {
     int SR, S;
     gemv_slices(B, N, k, &SR, &S);
     const bool vec = ldw % 8 == 0 && reinterpret_cast<uintptr_t>(W) % 16 == 0;
     float *P = static_cast<float *>(workspace);
-    return vec ? launch_vec<true>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream)
-               : launch_vec<false>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, stream);
+    auto go = [&](auto kernels, const Epilogue &e) {
+        return kernels(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, e, stream);
+    };
+    if (ep) return vec ? go(launch_vec<true, true>, *ep) : go(launch_vec<false, true>, *ep);
+    return vec ? go(launch_vec<true, false>, Epilogue{}) : go(launch_vec<false, false>, Epilogue{});
 }
 
 }  // namespace rmm

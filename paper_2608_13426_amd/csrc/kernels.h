@@ -62,16 +62,18 @@ hipError_t launch_check_indices(const int32_t *idx, int64_t B, int64_t k, int64_
                                 hipStream_t stream);
 
 // ------------------------------------------------------- gathered GEMM
+// ep: null, or the product's epilogue (epilogue.h)
+struct Epilogue;
 hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t *idx,
                             int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                             int64_t ldx, int64_t ldw, uint16_t *Y, int64_t ldy,
-                            hipStream_t stream);
+                            const Epilogue *ep, hipStream_t stream);
 // Xt: K-major activations [B][K][ldxt]; 16-byte aligned, ldxt % 8 == 0,
 // K*ldxt*2 and K*ldw*2 below 2^31 (checked by the caller).
 hipError_t launch_gemm_kmajor_bf16(const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
                                   int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                                   int64_t ldxt, int64_t ldw, uint16_t *Y, int64_t ldy,
-                                  hipStream_t stream);
+                                  const Epilogue *ep, hipStream_t stream);
 // the same product with per-unit weights: unit u reads W + (u / w_ugroup) *
 // w_ustride elements; with trim, Xt is known to be zero at (m, j) for
 // j > m + trim_off and each row tile stops its K loop there;
@@ -88,7 +90,7 @@ hipError_t launch_gemm_kmajor_grouped_bf16(const uint16_t *Xt, const uint16_t *W
 hipError_t launch_gemm_kmajor_mid_bf16(bool wide, const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
                                        int64_t B, int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldxt,
                                        int64_t ldw, uint16_t *Y, int64_t ldy, int64_t w_ustride, int w_ugroup,
-                                       int trim, int64_t trim_off, hipStream_t stream);
+                                       int trim, int64_t trim_off, const Epilogue *ep, hipStream_t stream);
 // the transposing scoring pass over attention scores: Pt = the K-major
 // softmax weights exp(s - rmax[m]) * rinv[m] (zero where causal drops j > m +
 // coff), and their column energies
@@ -119,7 +121,7 @@ hipError_t launch_gemm_swiglu_kmajor_bf16(const uint16_t *Xt, const uint16_t *W,
 hipError_t launch_gemm_f32(const float *X, const float *W, const int32_t *idx,
                            int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                            int64_t ldx, int64_t ldw, float *Y, int64_t ldy,
-                           hipStream_t stream);
+                           const Epilogue *ep, hipStream_t stream);
 
 // Independent one-row-per-unit products of a decode step, passed by value
 // to the grouped kernels (at most kMaxGemvGroups).  The launchers fill in
@@ -154,7 +156,8 @@ void gemv_slices(int64_t B, int64_t N, int64_t k, int *SR, int *S);
 size_t gemv_workspace_bytes(int64_t B, int64_t M, int64_t N, int64_t k);
 hipError_t launch_gemv_bf16(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B,
                             int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw,
-                            uint16_t *Y, int64_t ldy, void *workspace, hipStream_t stream);
+                            uint16_t *Y, int64_t ldy, void *workspace, const Epilogue *ep,
+                            hipStream_t stream);
 
 // --------------------------------------------------------- reduced QK^T
 // reduced attention block, bf16, D == 128, 16-byte aligned (checked by the
