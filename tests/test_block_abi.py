@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2608_13426_amd as rmm
+from paper_2608_13426_amd import _block
 
 INVALID, UNSUPPORTED, WS_SMALL = 1, 2, 3
 A = 0x100000                           # an aligned address that is never dereferenced
@@ -20,7 +21,7 @@ def at(off):
 def ep(**kw):
     d = dict(bias=A, act=0, residual_scale=1.0, residual=A + 4096, ldr=64)
     d.update(kw)
-    return ctypes.byref(rmm._EpilogueC(*d.values()))
+    return ctypes.byref(_block._EpilogueC(*d.values()))
 
 
 BAD_EPILOGUES = [(dict(act=5), INVALID), (dict(act=-1), INVALID), (dict(ldr=63), INVALID), (dict(residual_scale=math.nan), INVALID),
@@ -74,7 +75,7 @@ def join(ws=P, n=1 << 40, **kw):
              post_gamma=None, gate=None, gate_unit_stride=0, gate_row_stride=0, pre_gamma=A, eps=1e-6, H=A + 2 ** 21, ldh=64,
              X=None, ldx=0, Xt=A, ldxt=40, energy=A)
     d.update(kw)
-    return rmm.lib.rmm_block_join(ctypes.byref(rmm._JoinC(*d.values())), ws, n, None)
+    return rmm.lib.rmm_block_join(ctypes.byref(_block._JoinC(*d.values())), ws, n, None)
 
 
 def test_join_refusals():
@@ -142,15 +143,15 @@ def test_binding_refusals():
     with pytest.raises(TypeError):
         rmm.rmm_reduced_gemm_kmajor_epilogue(Xt, W, idx, h)
     with pytest.raises(ValueError):
-        rmm._epilogue(Y, (2, 3, 24), None, "tanh", None, 1.0)
+        _block._epilogue(Y, (2, 3, 24), None, "tanh", None, 1.0)
     with pytest.raises(ValueError):
-        rmm._epilogue(Y, (2, 3, 24), torch.zeros(23, dtype=bf), None, None, 1.0)
+        _block._epilogue(Y, (2, 3, 24), torch.zeros(23, dtype=bf), None, None, 1.0)
     with pytest.raises(ValueError):
-        rmm._epilogue(Y, (2, 3, 24), torch.zeros(24), None, None, 1.0)
+        _block._epilogue(Y, (2, 3, 24), torch.zeros(24), None, None, 1.0)
     with pytest.raises(ValueError):
-        rmm._epilogue(Y, (2, 3, 24), None, None, Y[:1], 1.0)
+        _block._epilogue(Y, (2, 3, 24), None, None, Y[:1], 1.0)
     with pytest.raises(ValueError, match="packed"):
-        rmm._epilogue(Y, (2, 3, 24), None, None, torch.zeros(2, 4, 24, dtype=bf)[:, :3], 1.0)
+        _block._epilogue(Y, (2, 3, 24), None, None, torch.zeros(2, 4, 24, dtype=bf)[:, :3], 1.0)
     j = rmm.rmm_block_join
     with pytest.raises(ValueError):
         j(None, None, H=X)
