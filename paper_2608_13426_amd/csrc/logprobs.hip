@@ -20,6 +20,7 @@
 // One workgroup per row, or per piece of a row where there are few rows; then a
 // second launch joins the pieces.
 #include <algorithm>
+#include <type_traits>
 
 #include "block.h"
 #include "device_common.h"
@@ -59,6 +60,17 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
     return (static_cast<uint64_t>(hi) << 32) | lo;
 }
 
+// the key of the lane before (lane 0: 0)
+__device__ __forceinline__ uint64_t key_before(uint64_t k) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(k), 0x138, 0xF, 0xF, true);          // wave_shr:1
+    const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(k >> 32), 0x138, 0xF, 0xF, true);
+    return (static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo);
+#else
+    return k;
+#endif
+}
+
 // A wave's `top` largest keys, descending over its lanes.
 struct TopList {
     uint64_t key;                        // this lane's
@@ -67,79 +79,130 @@ struct TopList {
     int top;
     __device__ void init(int n) { key = 0; last = 0; lim = -__builtin_inff(); top = n; }
     __device__ bool full() const { return last != 0; }
+    __device__ void bound() {
+        last = lane_key(key, top - 1);
+        lim = last ? key_logit(last) : -__builtin_inff();
+    }
+    // every lane offers one key (0: none) to an empty list: each goes to the lane
+    // that as many keys are larger
+    __device__ void fill(uint64_t cand) {
+        int rank = 0;
+#pragma unroll 8
+        for (int i = 0; i < 64; ++i) rank += lane_key(cand, i) > cand;
+        if (cand == 0) rank = 63;                          // ends behind every key, as 0
+        const uint64_t none = __ballot(cand == 0);
+        const uint32_t lo = __builtin_amdgcn_ds_permute(4 * rank, static_cast<int>(cand));
+        const uint32_t hi = __builtin_amdgcn_ds_permute(4 * rank, static_cast<int>(cand >> 32));
+        key = (threadIdx.x & 63) < 64 - __popcll(none) ? (static_cast<uint64_t>(hi) << 32) | lo : 0;
+        bound();
+    }
     // every lane offers one key (0: none)
     __device__ void offer(uint64_t cand) {
-        const int lane = threadIdx.x & 63;
         uint64_t todo = __ballot(cand > last);
-        while (todo) {
+        if (!todo) return;
+        const int lane = threadIdx.x & 63;
+        do {
             const int from = __builtin_ctzll(todo);
             const uint64_t k = lane_key(cand, from);
             const int pos = __popcll(__ballot(key > k));
-            const uint64_t prev = __shfl_up(key, 1);
+            const uint64_t prev = key_before(key);
             key = lane < pos ? key : lane == pos ? k : prev;
             last = lane_key(key, top - 1);
             if (lane == from) cand = 0;
             todo = __ballot(cand > last);
-        }
+        } while (todo);
         lim = last ? key_logit(last) : -__builtin_inff();
     }
 };
 
-// A wave's softmax sums of the logits it has seen: b shared, s and d per lane.
+// A wave's softmax sums of the logits it has seen: the base shared, s and d per
+// lane.  As long as it can, t = fma(z, c, -base) with base = b c rounded to fp32
+// (what that rounds is known, and taken out again at the end); in a wave that has
+// met a logit of -infinity (0 times infinity in d) or a base past 4096, t =
+// c (z - b), kept above -1e30: 8.5 operations per logit, an exponential
+// counted as four, against 10.5.
 struct Sums {
-    float b, bmax, s, d;                 // bmax: b, or -infinity while it is not set
-    bool set;
-    __device__ void init() { b = 0.f; bmax = -__builtin_inff(); s = 0.f; d = 0.f; set = false; }
+    float b, bmax, base, s, d;           // bmax: b, or -infinity while it is not set
+    bool set, careful;
+    __device__ void init() {
+        b = 0.f; bmax = -__builtin_inff(); base = 0.f; s = 0.f; d = 0.f;
+        set = false; careful = false;
+    }
+    // what base lacks of b c
+    __device__ float rest(float c) const { return careful ? 0.f : fmaf(b, c, -base); }
+    __device__ void take_care(float c) {
+        const float r = rest(c), f = __builtin_amdgcn_exp2f(-r);
+        d = (d - r * s) * f;
+        s *= f;
+        careful = true;
+    }
     // moves b to the largest of the lanes' values
     __device__ void rebase(float cm, float c) {
 #pragma unroll
         for (int sh = 1; sh < 64; sh <<= 1) cm = fmaxf(cm, __shfl_xor(cm, sh));
+        cm = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(cm)));
+        const float nb = cm * c;
+        if (!careful && !(fabsf(nb) < 4096.f)) take_care(c);
         if (set) {
-            const float delta = (b - cm) * c, f = __builtin_amdgcn_exp2f(delta);
+            const float delta = careful ? (b - cm) * c : base - nb, f = __builtin_amdgcn_exp2f(delta);
             d = f > 0.f ? (d + s * delta) * f : 0.f;
             s *= f;
         }
         b = bmax = cm;
+        base = nb;
         set = true;
     }
-    template <bool ENT>
+    template <bool ENT, bool CAREFUL>
     __device__ void add(const float (&x)[8], float c) {
         float e[8], t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = (x[i] - b) * c;
+        for (int i = 0; i < 8; ++i) t[i] = CAREFUL ? (x[i] - b) * c : fmaf(x[i], c, -base);
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(t[i]);
         s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         if constexpr (ENT) {
-            // a weight of zero (a logit of -infinity, or far below) adds nothing
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d = fmaf(e[i], fmaxf(t[i], -1e30f), d);
+            for (int i = 0; i < 8; ++i) d = fmaf(e[i], CAREFUL ? fmaxf(t[i], -1e30f) : t[i], d);
         }
     }
 };
 
+// the largest float below x; NaN, which nothing compares with, for -infinity and NaN
+__device__ __forceinline__ float below(float x) {
+    const int u = static_cast<int>(__float_as_uint(x));
+    if (!(x > -__builtin_inff())) return __builtin_nanf("");
+    if (x == 0.f) return __uint_as_float(0x80000001u);
+    return __uint_as_float(static_cast<uint32_t>(u > 0 ? u - 1 : u + 1));
+}
+
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int sh = 1; sh < 64; sh <<= 1) v += __shfl_xor(v, sh);
+    v += dpp_f64<0xB1>(v);               // lane ^ 1, lane ^ 2, then mirrors of 8 and 16 lanes
+    v += dpp_f64<0x4E>(v);
+    v += dpp_f64<0x141>(v);
+    v += dpp_f64<0x140>(v);
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
     return v;
 }
 
-// Sums of n parts, in order: the same in every thread.
-__device__ __forceinline__ Part join_parts(const Part *p, int n, float c) {
-    Part r = {0.0, 0.0, 0.f, 0};
-    for (int i = 0; i < n; ++i) {
-        if (!p[i].set) continue;
-        if (!r.set || p[i].b > r.b) r.b = p[i].b;
-        r.set = 1;
-    }
-    for (int i = 0; i < n; ++i) {
-        if (!p[i].set) continue;
-        const double delta = (static_cast<double>(p[i].b) - r.b) * c;
-        const double f = delta == 0.0 ? 1.0 : exp2(delta);
-        if (f == 0.0) continue;                              // nothing left of it
-        r.S += f * p[i].S;
-        r.D += f * (p[i].D + p[i].S * delta);
-    }
+// 2^delta for the weight of one base against another (delta <= 0): fp32, whose
+// relative error 2^-24 |delta| meets a weight of 2^delta
+__device__ __forceinline__ double base_weight(float b, float to, float c) {
+    return b == to ? 1.0 : static_cast<double>(__builtin_amdgcn_exp2f((b - to) * c));
+}
+
+// The sums of n parts (n <= 64: lane i of every wave holds part i): the same in
+// every lane.
+__device__ __forceinline__ Part join_parts(Part mine, float c) {
+    float b = mine.set ? mine.b : -__builtin_inff();
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) b = fmaxf(b, __shfl_xor(b, sh));
+    Part r = {0.0, 0.0, b, __ballot(mine.set) != 0};
+    // a NaN base (of a part whose only logits are NaN) leaves S one
+    const double f = mine.set ? base_weight(mine.b, b, c) : 0.0;
+    const bool some = mine.set && f != 0.0;
+    r.S = wave_sum(some ? f * mine.S : 0.0);
+    r.D = wave_sum(some ? f * (mine.D + mine.S * static_cast<double>((mine.b - b) * c)) : 0.0);
     return r;
 }
 
@@ -151,14 +214,16 @@ __device__ __forceinline__ float logit(const T *z, int64_t i) {
 // A row's results from its sums and its list (thread i < top holds key i).
 template <typename T>
 __device__ __forceinline__ void write_row(const LogprobArgs &a, int64_t row, const Part &p, uint64_t key) {
+    const int t = threadIdx.x;
+    if (t > 0 && t >= a.given && t >= a.top) return;
     const T *z = static_cast<const T *>(a.z) + row * a.ld;
     const double ls = log2(p.S);
     // a row without a logit above -infinity has no weights: -infinity for every token
     auto logp = [&](float x) {
         if (!p.set) return -__builtin_inff();
-        return static_cast<float>(((static_cast<double>(x) - p.b) * a.c - ls) * kLn2);
+        const double v = ((static_cast<double>(x) - p.b) * a.c - ls) * kLn2;
+        return v > 0.0 ? 0.f : static_cast<float>(v);        // what rounding left above 1
     };
-    const int t = threadIdx.x;
     if (t == 0 && a.entropy) a.entropy[row] = p.set ? static_cast<float>((ls - p.D / p.S) * kLn2) : 0.f;
     for (int i = t; i < a.given; i += blockDim.x) {
         const int tok = a.tokens[row * a.given + i];
@@ -187,84 +252,206 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t key, int top) {
     return threadIdx.x < kMaxTop ? out[threadIdx.x] : 0;
 }
 
+// One chunk of a row: 8 logits of each lane, as loaded.
+template <typename T>
+struct Raw {
+    static constexpr int N = sizeof(T) / 2;              // 16-byte loads
+    uint4 q[N];
+    __device__ float get(int e) const {
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t w = (&q[0].x)[e >> 1];
+            return __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
+        } else {
+            return __uint_as_float((&q[e >> 2].x)[e & 3]);
+        }
+    }
+};
+
+// chunks per step of a wave: 64 bytes per lane
+template <typename T>
+constexpr int group_of = sizeof(T) == 2 ? 4 : 2;
+
 template <typename T, bool VEC, bool ENT>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const int64_t row = blockIdx.x / a.pieces;
     const int piece = static_cast<int>(blockIdx.x - row * a.pieces);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T *z = static_cast<const T *>(a.z) + row * a.ld;
-    const int chunks = (a.V + kChunk - 1) / kChunk, full = a.V / kChunk;
+    const int chunks = (a.V + kChunk - 1) / kChunk;
     const int c0 = static_cast<int>(static_cast<int64_t>(chunks) * piece / a.pieces);
     const int c1 = static_cast<int>(static_cast<int64_t>(chunks) * (piece + 1) / a.pieces);
+    const int whole = min(c1, a.V / kChunk);             // chunks before this one are whole
+    constexpr int kGroup = group_of<T>;
     Sums sums;
     sums.init();
     TopList list;
     list.init(a.top > 0 ? a.top : 1);
+    bool fresh = a.top > 0;
 
     // element e of this lane in chunk ch
     auto index = [&](int ch, int e) { return ch * kChunk + (VEC ? 8 * lane + e : lane + 64 * e); };
-    auto load = [&](int ch, float (&x)[8]) {
-        if (VEC && ch < full) {
-            if constexpr (sizeof(T) == 2) {
-                const uint4 q = *reinterpret_cast<const uint4 *>(z + index(ch, 0));
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -infinity
+    auto load = [&](int ch, Raw<T> &r) {
+        if (VEC && ch < whole) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(z + index(ch, 0));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[2 * e] = __uint_as_float(w[e] << 16);
-                    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+            for (int i = 0; i < Raw<T>::N; ++i) r.q[i] = p[i];
+            return;
+        }
+        uint32_t w[4 * Raw<T>::N];
+#pragma unroll
+        for (int i = 0; i < 4 * Raw<T>::N; ++i) w[i] = kNone;
+        if (ch < c1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = index(ch, e);
+                const float x = i < a.V ? logit(z, i) : -__builtin_inff();
+                if constexpr (sizeof(T) == 2) {
+                    const uint32_t u = __float_as_uint(x) >> 16;
+                    w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xffffu) | (u << 16) : (w[e >> 1] & 0xffff0000u) | u;
+                } else {
+                    w[e] = __float_as_uint(x);
                 }
-            } else {
-                const f32x4_t *p = reinterpret_cast<const f32x4_t *>(z + index(ch, 0));
-                const f32x4_t u = p[0], v = p[1];
+            }
+        }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { x[e] = u[e]; x[4 + e] = v[e]; }
+        for (int i = 0; i < Raw<T>::N; ++i) r.q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    };
+    // the key of an element, 0 past the piece's end
+    auto key_of = [&](const Raw<T> &r, int ch, int e) {
+        const int i = index(ch, e);
+        return ch < c1 && i < a.V ? make_key(r.get(e), i) : 0;
+    };
+    // Each wave's limit: nothing below the largest can be among the row's top ones
+    // (what equals it can, with a lower index).  Read whenever: an older value only
+    // lets more through.
+    __shared__ volatile float limits[kWaves];
+    if (lane == 0) limits[wave] = -__builtin_inff();
+    // chunks ch, ch + kWaves, ... of a step; those past c1 are all -infinity
+    auto take = [&](int ch, const Raw<T> (&r)[kGroup]) {
+        float gm = -__builtin_inff();
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) gm = fmaxf(gm, r[u].get(e));
+        if (__ballot(gm > sums.bmax)) sums.rebase(gm, a.c);
+        auto add = [&](auto careful) {
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = r[u].get(e);
+                sums.template add<ENT, decltype(careful)::value>(x, a.c);
+            }
+        };
+        if (!sums.careful) {
+            const float s0 = sums.s, d0 = sums.d;
+            add(std::false_type{});
+            if (ENT && __ballot(sums.d != sums.d)) {
+                sums.s = s0;
+                sums.d = d0;
+                sums.take_care(a.c);
+                add(std::true_type{});
             }
         } else {
+            add(std::true_type{});
+        }
+        if (a.top == 0) return;
+        // the lane's largest, the first of equal ones
+        auto largest = [&]() {
+            int i = index(ch, 0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = index(ch, e);
-                x[e] = i < a.V ? logit(z, i) : -__builtin_inff();
+            for (int u = kGroup - 1; u >= 0; --u)
+#pragma unroll
+                for (int e = 7; e >= 0; --e) i = r[u].get(e) == gm ? index(ch + kWaves * u, e) : i;
+            return i < a.V ? make_key(gm, i) : 0;
+        };
+        auto above = [&](float lim) {
+            int n = 0;
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) n += !(r[u].get(e) <= lim);
+            return n;
+        };
+        const bool nan = __ballot(sums.s != sums.s) != 0;    // a NaN has made s one
+        uint64_t best = 0;
+        float lim = -__builtin_inff();
+        if (nan) {
+            fresh = false;
+        } else if (fresh) {
+            // the lanes' largest, in order; few of the others are above the top-th of
+            // them (or equal to it, with a lower index)
+            fresh = false;
+            best = largest();
+            list.fill(best);
+            lim = below(list.lim);
+        } else {
+            float l = limits[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) l = fmaxf(l, limits[w]);
+            lim = fmaxf(list.lim, below(l));
+            if (list.full()) {
+                if (!__ballot(!(gm <= lim))) return;
+                best = largest();
+                list.offer(gm <= lim ? 0 : best);
             }
         }
-    };
-    auto take = [&](int ch, const float (&x)[8]) {
-        float cm = x[0];
+        if (lane == 0) limits[wave] = list.lim;
+        // more than one of a lane's is rare: those are read again
+        if (!nan && list.full() && !__ballot(above(lim) > !(gm <= lim))) return;
+#pragma unroll 1
+        for (int u = 0; u < kGroup && ch + kWaves * u < c1; ++u) {
+            Raw<T> t;
+            load(ch + kWaves * u, t);
+            float cm = t.get(0);
 #pragma unroll
-        for (int e = 1; e < 8; ++e) cm = fmaxf(cm, x[e]);
-        if (__ballot(cm > sums.bmax)) sums.rebase(cm, a.c);
-        sums.template add<ENT>(x, a.c);
-        // a NaN among them has made s one
-        if (a.top > 0 && (!list.full() || __ballot(cm > list.lim || sums.s != sums.s))) {
+            for (int e = 1; e < 8; ++e) cm = fmaxf(cm, t.get(e));
+            if (!nan && list.full() && !__ballot(!(cm <= lim))) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int i = index(ch, e);
-                list.offer(i < a.V ? make_key(x[e], i) : 0);
+                const uint64_t k = key_of(t, ch + kWaves * u, e);
+                list.offer(k != best ? k : 0);
             }
         }
+        if (lane == 0) limits[wave] = list.lim;
     };
-    for (int ch = c0 + wave; ch < c1; ch += kWaves) {
-        float x[8];
-        load(ch, x);
-        take(ch, x);
+    Raw<T> cur[kGroup], next[kGroup];
+    auto load_group = [&](int ch, Raw<T> (&r)[kGroup]) {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) load(ch + kWaves * u, r[u]);
+    };
+    constexpr int kStep = kGroup * kWaves;
+    int ch = c0 + wave;
+    if (ch < c1) load_group(ch, cur);
+    lds_barrier();                       // the limits are set
+    for (; ch < c1; ch += kStep) {
+        if (ch + kStep < c1) load_group(ch + kStep, next);
+        take(ch, cur);
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) cur[u] = next[u];
     }
 
     __shared__ Part parts[kWaves];
-    const double S = wave_sum(sums.s), D = wave_sum(sums.d);
+    const double r = sums.rest(a.c), f = 1.0 - kLn2 * r;         // 2^-r: r is below 1e-6 of the base
+    const double S0 = wave_sum(sums.s), S = f * S0, D = f * (wave_sum(sums.d) - r * S0);
     if (lane == 0) parts[wave] = {S, D, sums.b, sums.set || S != S};
     const uint64_t key = a.top > 0 ? join_lists(list.key, a.top) : 0;
     __syncthreads();
-    const Part p = join_parts(parts, kWaves, a.c);
+    if (wave > 0 && (a.pieces > 1 || (64 * wave >= a.given && 64 * wave >= a.top))) return;
+    const Part p = join_parts(lane < kWaves ? parts[lane] : Part{0.0, 0.0, 0.f, 0}, a.c);
     if (a.pieces == 1) {
         write_row<T>(a, row, p, key);
         return;
     }
     Part *out = static_cast<Part *>(a.part);
     uint64_t *keys = reinterpret_cast<uint64_t *>(out + a.T * a.pieces);
-    if (threadIdx.x == 0) out[blockIdx.x] = p;
-    if (threadIdx.x < a.top) keys[static_cast<int64_t>(blockIdx.x) * a.top + threadIdx.x] = key;
+    if (lane == 0) out[blockIdx.x] = p;
+    if (lane < a.top) keys[static_cast<int64_t>(blockIdx.x) * a.top + lane] = key;
 }
 
-// The pieces of one row.
+// The pieces (at most kMaxPieces) of one row.
+constexpr int kMaxPieces = 64;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a) {
     const int64_t row = blockIdx.x;
@@ -272,14 +459,25 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a) {
     const Part *in = static_cast<const Part *>(a.part) + row * a.pieces;
     const uint64_t *keys = reinterpret_cast<const uint64_t *>(static_cast<const Part *>(a.part) + a.T * a.pieces) +
                            row * a.pieces * a.top;
+    const Part mine = lane < a.pieces ? in[lane] : Part{0.0, 0.0, 0.f, 0};
     uint64_t key = 0;
     if (a.top > 0) {
         TopList list;
         list.init(a.top);
-        for (int i = wave; i < a.pieces; i += kWaves) list.offer(lane < a.top ? keys[i * a.top + lane] : 0);
+        auto read = [&](int i) -> uint64_t { return i < a.pieces && lane < a.top ? keys[i * a.top + lane] : 0; };
+        // a piece's list is sorted: the first is the wave's
+        uint64_t next = read(wave + kWaves);
+        list.key = read(wave);
+        list.bound();
+        for (int i = wave + kWaves; i < a.pieces; i += kWaves) {
+            const uint64_t k = next;
+            next = read(i + kWaves);
+            list.offer(k);
+        }
         key = join_lists(list.key, a.top);
     }
-    write_row<T>(a, row, join_parts(in, a.pieces, a.c), key);
+    if (wave > 0 && 64 * wave >= a.given && 64 * wave >= a.top) return;
+    write_row<T>(a, row, join_parts(mine, a.c), key);
 }
 
 template <typename T, bool VEC>
@@ -297,10 +495,10 @@ hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// pieces of at least four chunks per wave, until there are about 1024 workgroups
+// pieces of four chunks per wave or more, until there are about 1024 workgroups
 int logprob_pieces(int64_t T, int64_t V) {
-    const int64_t most = std::max<int64_t>(1, V / (4 * kWaves * kChunk));
-    return static_cast<int>(std::max<int64_t>(1, std::min(most, 1024 / T)));
+    const int64_t most = (V + 4 * kWaves * kChunk - 1) / (4 * kWaves * kChunk);
+    return static_cast<int>(std::max<int64_t>(1, std::min({most, 1024 / T, int64_t(kMaxPieces)})));
 }
 
 size_t logprob_workspace_bytes(int64_t T, int64_t V, int64_t top) {
