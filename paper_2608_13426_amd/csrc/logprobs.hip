@@ -240,12 +240,19 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t key, int top) {
     __shared__ uint64_t lists[kWaves][kMaxTop], out[kMaxTop];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (threadIdx.x < kMaxTop) out[threadIdx.x] = 0;
-    lists[wave][lane] = lane < top ? key : 0;
+    lists[wave][lane] = lane < top ? key : 0;            // descending
     __syncthreads();
     if (lane < top && key != 0) {
-        int rank = 0;
-        for (int w = 0; w < kWaves; ++w)
-            for (int i = 0; i < top; ++i) rank += lists[w][i] > key;
+        // its place: its own, and in each other list how many are larger
+        int rank = lane;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            const uint64_t *l = lists[(wave + w) % kWaves];
+            int n = 0;
+#pragma unroll
+            for (int step = kMaxTop / 2; step > 0; step /= 2) n += l[n + step - 1] > key ? step : 0;
+            rank += n + (l[n] > key);
+        }
         if (rank < top) out[rank] = key;
     }
     __syncthreads();
@@ -271,7 +278,7 @@ struct Raw {
 template <typename T>
 constexpr int group_of = sizeof(T) == 2 ? 4 : 2;
 
-template <typename T, bool VEC, bool ENT>
+template <typename T, bool VEC, bool ENT, int kGroup>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const int64_t row = blockIdx.x / a.pieces;
     const int piece = static_cast<int>(blockIdx.x - row * a.pieces);
@@ -281,7 +288,6 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const int c0 = static_cast<int>(static_cast<int64_t>(chunks) * piece / a.pieces);
     const int c1 = static_cast<int>(static_cast<int64_t>(chunks) * (piece + 1) / a.pieces);
     const int whole = min(c1, a.V / kChunk);             // chunks before this one are whole
-    constexpr int kGroup = group_of<T>;
     Sums sums;
     sums.init();
     TopList list;
@@ -317,15 +323,11 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
 #pragma unroll
         for (int i = 0; i < Raw<T>::N; ++i) r.q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     };
-    // the key of an element, 0 past the piece's end
-    auto key_of = [&](const Raw<T> &r, int ch, int e) {
-        const int i = index(ch, e);
-        return ch < c1 && i < a.V ? make_key(r.get(e), i) : 0;
-    };
     // Each wave's limit: nothing below the largest can be among the row's top ones
     // (what equals it can, with a lower index).  Read whenever: an older value only
     // lets more through.
     __shared__ volatile float limits[kWaves];
+    __shared__ uint32_t words[kWaves][64 * 4 * Raw<T>::N * kGroup];
     if (lane == 0) limits[wave] = -__builtin_inff();
     // chunks ch, ch + kWaves, ... of a step; those past c1 are all -infinity
     auto take = [&](int ch, const Raw<T> (&r)[kGroup]) {
@@ -357,61 +359,65 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             add(std::true_type{});
         }
         if (a.top == 0) return;
-        // the lane's largest, the first of equal ones
-        auto largest = [&]() {
+        const bool nan = __ballot(sums.s != sums.s) != 0;    // a NaN has made s one
+        // nothing compares with a limit of NaN: all pass
+        float lim = __builtin_nanf("");
+        if (!nan && !fresh && list.full()) {
+            float l = limits[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) l = fmaxf(l, limits[w]);
+            lim = fmaxf(list.lim, below(l));
+            if (!__ballot(!(gm <= lim))) return;
+        }
+        uint64_t best = 0;
+        if (!nan) {
+            // the lane's largest, the first of equal ones
             int i = index(ch, 0);
 #pragma unroll
             for (int u = kGroup - 1; u >= 0; --u)
 #pragma unroll
                 for (int e = 7; e >= 0; --e) i = r[u].get(e) == gm ? index(ch + kWaves * u, e) : i;
-            return i < a.V ? make_key(gm, i) : 0;
-        };
-        auto above = [&](float lim) {
-            int n = 0;
+            best = i < a.V && !(gm <= lim) ? make_key(gm, i) : 0;
+            if (fresh) {
+                // in order; few others are above the top-th of them (or equal to it,
+                // with a lower index)
+                list.fill(best);
+                lim = list.full() ? below(list.lim) : lim;
+            } else {
+                list.offer(best);
+            }
+        }
+        fresh = false;
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) n += !(r[u].get(e) <= lim);
+        // a lane's second, third ... are rare: in a short loop over LDS
+        if (nan || __ballot(n > 1)) {
 #pragma unroll
             for (int u = 0; u < kGroup; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) n += !(r[u].get(e) <= lim);
-            return n;
-        };
-        const bool nan = __ballot(sums.s != sums.s) != 0;    // a NaN has made s one
-        uint64_t best = 0;
-        float lim = -__builtin_inff();
-        if (nan) {
-            fresh = false;
-        } else if (fresh) {
-            // the lanes' largest, in order; few of the others are above the top-th of
-            // them (or equal to it, with a lower index)
-            fresh = false;
-            best = largest();
-            list.fill(best);
-            lim = below(list.lim);
-        } else {
-            float l = limits[0];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) l = fmaxf(l, limits[w]);
-            lim = fmaxf(list.lim, below(l));
-            if (list.full()) {
-                if (!__ballot(!(gm <= lim))) return;
-                best = largest();
-                list.offer(gm <= lim ? 0 : best);
-            }
-        }
-        if (lane == 0) limits[wave] = list.lim;
-        // more than one of a lane's is rare: those are read again
-        if (!nan && list.full() && !__ballot(above(lim) > !(gm <= lim))) return;
+                for (int i = 0; i < 4 * Raw<T>::N; ++i) words[wave][(4 * Raw<T>::N * u + i) * 64 + lane] = (&r[u].q[0].x)[i];
 #pragma unroll 1
-        for (int u = 0; u < kGroup && ch + kWaves * u < c1; ++u) {
-            Raw<T> t;
-            load(ch + kWaves * u, t);
-            float cm = t.get(0);
+            for (int u = 0; u < kGroup; ++u) {
+                Raw<T> t;
 #pragma unroll
-            for (int e = 1; e < 8; ++e) cm = fmaxf(cm, t.get(e));
-            if (!nan && list.full() && !__ballot(!(cm <= lim))) continue;
+                for (int i = 0; i < 4 * Raw<T>::N; ++i) (&t.q[0].x)[i] = words[wave][(4 * Raw<T>::N * u + i) * 64 + lane];
+                int more = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint64_t k = key_of(t, ch + kWaves * u, e);
-                list.offer(k != best ? k : 0);
+                for (int e = 0; e < 8; ++e) more |= nan || !(t.get(e) <= lim) ? 1 << e : 0;
+                if (n < 2 && !nan) more = 0;
+                while (__ballot(more != 0)) {                // each lane's next
+                    const int e = __builtin_ctz(more | 256);
+                    float x = t.get(0);
+#pragma unroll
+                    for (int q = 1; q < 8; ++q) x = q == e ? t.get(q) : x;
+                    const int i = index(ch + kWaves * u, e);
+                    const uint64_t k = more != 0 && i < a.V && ch + kWaves * u < c1 ? make_key(x, i) : 0;
+                    list.offer(k != best ? k : 0);
+                    more &= more - 1;
+                }
             }
         }
         if (lane == 0) limits[wave] = list.lim;
@@ -464,15 +470,21 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a) {
     if (a.top > 0) {
         TopList list;
         list.init(a.top);
-        auto read = [&](int i) -> uint64_t { return i < a.pieces && lane < a.top ? keys[i * a.top + lane] : 0; };
-        // a piece's list is sorted: the first is the wave's
-        uint64_t next = read(wave + kWaves);
-        list.key = read(wave);
-        list.bound();
-        for (int i = wave + kWaves; i < a.pieces; i += kWaves) {
-            const uint64_t k = next;
-            next = read(i + kWaves);
-            list.offer(k);
+        // the pieces' keys, 64 at a time, four such reads ahead of their use
+        const int n = a.pieces * a.top;
+        auto read = [&](int i) -> uint64_t { return i + lane < n ? keys[i + lane] : 0; };
+        constexpr int kAhead = 4;
+        uint64_t k[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) k[u] = read(64 * (wave + kWaves * u));
+        list.fill(k[0]);
+        k[0] = 0;
+        for (int i = wave; 64 * i < n; i += kWaves * kAhead) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                list.offer(k[u]);
+                k[u] = read(64 * (i + kWaves * (u + kAhead)));
+            }
         }
         key = join_lists(list.key, a.top);
     }
@@ -480,14 +492,20 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a) {
     write_row<T>(a, row, join_parts(mine, a.c), key);
 }
 
+// Up to 2048 workgroups of one chunk per wave: one step each.  Beyond, steps of 64
+// bytes per lane.
+bool one_step(int64_t T, int64_t V) { return T * std::min<int64_t>(kMaxPieces, (V + kWaves * kChunk - 1) / (kWaves * kChunk)) <= 2048; }
+
 template <typename T, bool VEC>
 hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.T * a.pieces));
-    if (a.entropy)
-        hipLaunchKernelGGL((logprob_kernel<T, VEC, true>), grid, dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((logprob_kernel<T, VEC, false>), grid, dim3(kThreads), 0, stream, a);
-    const hipError_t e = hipGetLastError();
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a);
+        return hipGetLastError();
+    };
+    constexpr int G = group_of<T>;
+    const hipError_t e = one_step(a.T, a.V) ? a.entropy ? go(logprob_kernel<T, VEC, true, 1>) : go(logprob_kernel<T, VEC, false, 1>)
+                                            : a.entropy ? go(logprob_kernel<T, VEC, true, G>) : go(logprob_kernel<T, VEC, false, G>);
     if (e != hipSuccess || a.pieces == 1) return e;
     hipLaunchKernelGGL(logprob_join_kernel<T>, dim3(static_cast<unsigned>(a.T)), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
@@ -495,10 +513,10 @@ hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// pieces of four chunks per wave or more, until there are about 1024 workgroups
+// otherwise pieces of four chunks per wave or more, until there are about 1024 workgroups
 int logprob_pieces(int64_t T, int64_t V) {
-    const int64_t most = (V + 4 * kWaves * kChunk - 1) / (4 * kWaves * kChunk);
-    return static_cast<int>(std::max<int64_t>(1, std::min({most, 1024 / T, int64_t(kMaxPieces)})));
+    const int64_t per = kWaves * kChunk * (one_step(T, V) ? 1 : 4), most = (V + per - 1) / per;
+    return static_cast<int>(std::max<int64_t>(1, std::min({most, one_step(T, V) ? most : 1024 / T, int64_t(kMaxPieces)})));
 }
 
 size_t logprob_workspace_bytes(int64_t T, int64_t V, int64_t top) {
