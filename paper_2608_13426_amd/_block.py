@@ -35,6 +35,7 @@ class _JoinC(ctypes.Structure):
 _EPILOGUE_BYTES, _JOIN_BYTES = struct.Struct("@PifPq"), struct.Struct("@iiqqqPqPqfiPPqqPf4xPqPqPqP")
 assert _EPILOGUE_BYTES.size == ctypes.sizeof(_EpilogueC) and _JOIN_BYTES.size == ctypes.sizeof(_JoinC)
 
+_CODES = {torch.bfloat16: RMM_BF16, torch.float32: RMM_F32}
 _ACTS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 
@@ -42,6 +43,8 @@ def _unit_rows(t: torch.Tensor, shape, dtype, name: str) -> int:
     """The row stride of t, [B, M, N] (or [M, N] of one unit) of `dtype`: rows
     contiguous, units packed (M rows apart); strides of axes of one entry are
     never used."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return shape[2]
     B, M, N = shape
     if tuple(t.shape) != (B, M, N) and (B > 1 or tuple(t.shape) != (M, N)):
         raise ValueError(f"{name} must be [{B}, {M}, {N}]")
@@ -134,7 +137,7 @@ def rmm_reduced_gemv_epilogue(X: torch.Tensor, W: torch.Tensor, idx: torch.Tenso
         workspace = _scratch(rmm_gemv_workspace_size(B, M, N, k), X.device, stream)
     _run("rmm_reduced_gemv_epilogue", d, stream, X.data_ptr(), W.data_ptr(), idx.data_ptr(), B, M, N, K, k, ldx, ldw,
          Y.data_ptr(), ldy, _epilogue(Y, (B, M, N), bias, act, residual, residual_scale), workspace.data_ptr(),
-         workspace.numel() * workspace.element_size())
+         workspace.nbytes)
     return Y
 
 
@@ -159,17 +162,23 @@ def rmm_block_join(Y: torch.Tensor | None, R: torch.Tensor | None, H: torch.Tens
     some = Y if Y is not None else R
     if some is None or some.dim() not in (2, 3):
         raise ValueError("Y or R must be given, as [B, M, K] or [M, K]")
-    shape = tuple(some.shape) if some.dim() == 3 else (1, *some.shape)
+    shape = some.shape if some.dim() == 3 else (1, *some.shape)
     B, M, K = shape
-    if min(shape) < 1:
+    if B * M * K == 0:
         raise ValueError("Y and R must not be empty")
     sd = R.dtype if R is not None else H.dtype if H is not None else Y.dtype
     dt = Y.dtype if Y is not None else X.dtype if X is not None else torch.bfloat16 if Xt is not None else sd
-    code = {torch.bfloat16: RMM_BF16, torch.float32: RMM_F32}
-    if dt not in code or sd not in code:
+    if dt not in _CODES or sd not in _CODES:
         raise TypeError("rows must be bfloat16 or float32")
-    ld = [0 if t is None else _unit_rows(t, shape, d, n)
-          for t, d, n in ((Y, dt, "Y"), (R, sd, "R"), (H, sd, "H"), (X, dt, "X"))]
+    ldy = ldr = ldh = ldx = py = pr = ph = px = 0
+    if Y is not None:
+        ldy, py = _unit_rows(Y, shape, dt, "Y"), Y.data_ptr()
+    if R is not None:
+        ldr, pr = _unit_rows(R, shape, sd, "R"), R.data_ptr()
+    if H is not None:
+        ldh, ph = _unit_rows(H, shape, sd, "H"), H.data_ptr()
+    if X is not None:
+        ldx, px = _unit_rows(X, shape, dt, "X"), X.data_ptr()
     gu = gr = 0
     if gate is not None:
         if gate.dtype != dt:
@@ -188,14 +197,23 @@ def rmm_block_join(Y: torch.Tensor | None, R: torch.Tensor | None, H: torch.Tens
             ldxt = (M + 7) // 8 * 8
         if workspace is None:
             workspace = _scratch(rmm_block_join_workspace_size(B, M, K), some.device, stream)
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = workspace.nbytes
     _run("rmm_block_join", d, stream,
-         _JOIN_BYTES.pack(code[dt], code[sd], B, M, K, _ptr(Y) or 0, ld[0], _ptr(R) or 0, ld[1], residual_scale,
-                          1 if post_norm else 0, _vec(post_gamma, K, dt, "post_gamma") or 0, _ptr(gate) or 0, gu, gr,
-                          _vec(pre_gamma, K, dt, "pre_gamma") or 0, eps, _ptr(H) or 0, ld[2], _ptr(X) or 0, ld[3],
-                          _ptr(Xt) or 0, ldxt, _vec(energy, B * K, torch.float64, "energy") or 0),
+         _JOIN_BYTES.pack(_CODES[dt], _CODES[sd], B, M, K, py, ldy, pr, ldr, residual_scale, 1 if post_norm else 0,
+                          _vec(post_gamma, K, dt, "post_gamma") or 0, 0 if gate is None else gate.data_ptr(), gu, gr,
+                          _vec(pre_gamma, K, dt, "pre_gamma") or 0, eps, ph, ldh, px, ldx,
+                          0 if Xt is None else Xt.data_ptr(), ldxt, _vec(energy, B * K, torch.float64, "energy") or 0),
          _ptr(workspace), ws_bytes)
     return tuple(t for t in (H, X, Xt) if t is not None)
+
+
+def _flat(t: torch.Tensor | None, dtype, name: str):
+    """The address of a contiguous tensor whose shape has been checked."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor")
+    return t.data_ptr()
 
 
 def rmm_token_logprobs_workspace_size(T: int, V: int, top: int) -> int:
@@ -220,18 +238,20 @@ def rmm_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None,
         raise ValueError("tokens and logp, top_idx and top_logp come together")
     given = top = 0
     if tokens is not None:
-        if tokens.dim() not in (1, 2) or tokens.shape[0] != T or logp.shape != tokens.shape:
+        size = tokens.shape
+        if len(size) not in (1, 2) or size[0] != T or logp.shape != size:
             raise ValueError("tokens and logp must be [T] or [T, given]")
-        given = tokens.numel() // max(T, 1)
+        given = size[1] if len(size) == 2 else 1
     if top_idx is not None:
-        if top_idx.dim() != 2 or top_idx.shape[0] != T or top_logp.shape != top_idx.shape:
+        size = top_idx.shape
+        if len(size) != 2 or size[0] != T or top_logp.shape != size:
             raise ValueError("top_idx and top_logp must be [T, top]")
-        top = top_idx.shape[1]
+        top = size[1]
     d = _device_index(logits, tokens, logp, entropy, top_idx, top_logp, workspace)
     if workspace is None:
         workspace = _scratch(rmm_token_logprobs_workspace_size(T, V, top), logits.device, stream)
+    i32, f32 = torch.int32, torch.float32
     _run("rmm_token_logprobs", d, stream, logits.data_ptr(), _dtype_code(logits), T, V,
-         logits.stride(0) if T > 1 else V, scale, _vec(tokens, T * given, torch.int32, "tokens"), given,
-         _vec(logp, T * given, torch.float32, "logp"), _vec(entropy, T, torch.float32, "entropy"), top,
-         _vec(top_idx, T * top, torch.int32, "top_idx"), _vec(top_logp, T * top, torch.float32, "top_logp"),
-         workspace.data_ptr(), workspace.numel() * workspace.element_size())
+         logits.stride(0) if T > 1 else V, scale, _flat(tokens, i32, "tokens"), given, _flat(logp, f32, "logp"),
+         _vec(entropy, T, f32, "entropy"), top, _flat(top_idx, i32, "top_idx"), _flat(top_logp, f32, "top_logp"),
+         workspace.data_ptr(), workspace.nbytes)

@@ -453,43 +453,35 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     Part *out = static_cast<Part *>(a.part);
     uint64_t *keys = reinterpret_cast<uint64_t *>(out + a.T * a.pieces);
     if (lane == 0) out[blockIdx.x] = p;
-    if (lane < a.top) keys[static_cast<int64_t>(blockIdx.x) * a.top + lane] = key;
+    if (lane < a.top) keys[row * a.pieces * a.top + lane * a.pieces + piece] = key;
 }
 
-// The pieces (at most kMaxPieces) of one row.
+// The pieces (at most kMaxPieces) of one row, by one wave.  The keys lie by rank,
+// then by piece: 64 in a row hold one of every piece at least, so that once none
+// of them enters nothing behind them can.
 constexpr int kMaxPieces = 64;
 template <typename T>
-__global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
     const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x;
     const Part *in = static_cast<const Part *>(a.part) + row * a.pieces;
-    const uint64_t *keys = reinterpret_cast<const uint64_t *>(static_cast<const Part *>(a.part) + a.T * a.pieces) +
-                           row * a.pieces * a.top;
-    const Part mine = lane < a.pieces ? in[lane] : Part{0.0, 0.0, 0.f, 0};
-    uint64_t key = 0;
+    const int n = a.pieces * a.top;
+    const uint64_t *keys = reinterpret_cast<const uint64_t *>(static_cast<const Part *>(a.part) + a.T * a.pieces) + row * n;
+    auto read = [&](int i) -> uint64_t { return i + lane < n ? keys[i + lane] : 0; };
+    uint64_t k = read(0), next = read(64);
+    const Part p = join_parts(lane < a.pieces ? in[lane] : Part{0.0, 0.0, 0.f, 0}, a.c);
+    TopList list;
+    list.init(a.top > 0 ? a.top : 1);
     if (a.top > 0) {
-        TopList list;
-        list.init(a.top);
-        // the pieces' keys, 64 at a time, four such reads ahead of their use
-        const int n = a.pieces * a.top;
-        auto read = [&](int i) -> uint64_t { return i + lane < n ? keys[i + lane] : 0; };
-        constexpr int kAhead = 4;
-        uint64_t k[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) k[u] = read(64 * (wave + kWaves * u));
-        list.fill(k[0]);
-        k[0] = 0;
-        for (int i = wave; 64 * i < n; i += kWaves * kAhead) {
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                list.offer(k[u]);
-                k[u] = read(64 * (i + kWaves * (u + kAhead)));
-            }
+        list.fill(k);
+        for (int i = 64; i < n; i += 64) {
+            k = next;
+            next = read(i + 64);
+            if (!__ballot(k > list.last)) break;
+            list.offer(k);
         }
-        key = join_lists(list.key, a.top);
     }
-    if (wave > 0 && 64 * wave >= a.given && 64 * wave >= a.top) return;
-    write_row<T>(a, row, join_parts(mine, a.c), key);
+    write_row<T>(a, row, p, list.key);
 }
 
 // Up to 2048 workgroups of one chunk per wave: one step each.  Beyond, steps of 64
@@ -507,7 +499,7 @@ hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
     const hipError_t e = one_step(a.T, a.V) ? a.entropy ? go(logprob_kernel<T, VEC, true, 1>) : go(logprob_kernel<T, VEC, false, 1>)
                                             : a.entropy ? go(logprob_kernel<T, VEC, true, G>) : go(logprob_kernel<T, VEC, false, G>);
     if (e != hipSuccess || a.pieces == 1) return e;
-    hipLaunchKernelGGL(logprob_join_kernel<T>, dim3(static_cast<unsigned>(a.T)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(logprob_join_kernel<T>, dim3(static_cast<unsigned>(a.T)), dim3(64), 0, stream, a);
     return hipGetLastError();
 }
 
