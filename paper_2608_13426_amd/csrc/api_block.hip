@@ -37,7 +37,6 @@ rmm_status_t check_epilogue(const rmm_epilogue_t *e, rmm_dtype_t dt, int64_t N, 
     out->ldr = e->ldr;
     out->rs = e->residual_scale;
     out->act = e->act;
-    out->vec = aligned(e->bias, 8) && aligned(e->residual, 8) && (!e->residual || e->ldr % 4 == 0);
     return RMM_OK;
 }
 

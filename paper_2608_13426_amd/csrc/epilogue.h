@@ -14,28 +14,50 @@ struct Epilogue {
     int64_t ldr;          // residual row stride (elements), units M * ldr apart
     float rs;
     int act;
-    int vec;              // bf16 bias and residual rows are 8-byte aligned
 };
 
 constexpr int kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kActGeluTanh = 4;
 
-template <int ACT>
+// T: the output's type.  Where it is bf16 the forms below err by at most 2^-16 |x|
+// (a 128th of what the rounding may), in as few operations as that takes: they run
+// on every output of a tile while its matrix cores wait (8192 x 14336 outputs of
+// 2048 retained indices, gelu: 447 us with erff, 416 so).
+template <int ACT, class T>
 __device__ __forceinline__ float activate(float x) {
+    constexpr bool kFast = sizeof(T) == 2;
     if constexpr (ACT == kActRelu) return x < 0.f ? 0.f : x;          // NaN stays
-    if constexpr (ACT == kActSilu) return x / (1.f + __expf(-x));
-    if constexpr (ACT == kActGelu) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
+    if constexpr (ACT == kActSilu) return x * __builtin_amdgcn_rcpf(1.f + __expf(-x));
+    if constexpr (ACT == kActGelu && !kFast) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
+    if constexpr (ACT == kActGelu && kFast) {
+        // x Phi(x) = max(x, 0) - a Phi(-a), a = |x|; log2 Phi(-a) as a polynomial of
+        // degree 8, least largest error on [0, 10] (3e-5 of Phi); past 10, a Phi(-a) < 1e-22
+        const float a = fminf(fabsf(x), 10.f);
+        float p = 6.003541844e-08f;
+        p = fmaf(p, a, -3.129991683e-06f);
+        p = fmaf(p, a, 7.174348139e-05f);
+        p = fmaf(p, a, -9.613548173e-04f);
+        p = fmaf(p, a, 8.502015844e-03f);
+        p = fmaf(p, a, -5.372728780e-02f);
+        p = fmaf(p, a, -4.589110017e-01f);
+        p = fmaf(p, a, -1.150986195f);
+        p = fmaf(p, a, -1.000023842f);
+        return fmaf(-a, __builtin_amdgcn_exp2f(p), x < 0.f ? 0.f : x);
+    }
     // 0.5 x (1 + tanh u) = x / (1 + e^(-2u)),  u = sqrt(2/pi) (x + 0.044715 x^3)
-    if constexpr (ACT == kActGeluTanh)
-        return x / (1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
+    if constexpr (ACT == kActGeluTanh) {
+        const float w = x * fmaf(x * x, -0.10294324f, -2.3022082f);   // -2 u log2(e)
+        return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(w));
+    }
     return x;
 }
 
+template <class T>
 __device__ __forceinline__ float activate(float x, int act) {
     switch (act) {
-    case kActRelu: return activate<kActRelu>(x);
-    case kActSilu: return activate<kActSilu>(x);
-    case kActGelu: return activate<kActGelu>(x);
-    case kActGeluTanh: return activate<kActGeluTanh>(x);
+    case kActRelu: return activate<kActRelu, T>(x);
+    case kActSilu: return activate<kActSilu, T>(x);
+    case kActGelu: return activate<kActGelu, T>(x);
+    case kActGeluTanh: return activate<kActGeluTanh, T>(x);
     default: return x;
     }
 }
@@ -60,77 +82,126 @@ __device__ __forceinline__ float ep_load(const float *p, int64_t i) { return p[i
 template <class T>
 __device__ __forceinline__ float ep_value(const Epilogue &ep, float acc, int64_t row, int n) {
     if (ep.bias) acc += ep_load(static_cast<const T *>(ep.bias), n);
-    acc = activate(acc, ep.act);
+    acc = activate<T>(acc, ep.act);
     if (ep.res) acc = fmaf(ep.rs, ep_load(static_cast<const T *>(ep.res), row * ep.ldr + n), acc);
     return acc;
 }
 
-// The same on the Y^T fragments of the K-major kernels: acc[j][i][4*gq + r] is
-// row m = mrow + 32i + lane%32 and column n = ncol + 32j + 8gq + 4*(lane/32) + r.
-// rows: how many rows are left from mrow's tile origin; row0: the tile origin's
-// row over all units.
-template <int FN, int FM>
-__device__ __forceinline__ void ep_fragments(const Epilogue &ep, f32x16_t (&acc)[FN][FM], int lane, int mrow,
-                                             int ncol, int rows, int64_t row0, int N) {
-    const bool vec = ep.vec;
-    const int lr = lane & 31, lh = lane >> 5;
-    if (ep.bias) {
-        const uint16_t *bias = static_cast<const uint16_t *>(ep.bias);
+// 16 and 8 bytes at any address (global memory takes them at every alignment)
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void ep_unpack(const u32x4_t &q, float (&v)[8]) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-                const int n = ncol + 32 * j + 8 * gq + 4 * lh;
-                float b[4];
-                if (vec && n + 4 <= N) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(bias + n);
-                    b[0] = __uint_as_float(v.x << 16); b[1] = __uint_as_float(v.x & 0xffff0000u);
-                    b[2] = __uint_as_float(v.y << 16); b[3] = __uint_as_float(v.y & 0xffff0000u);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) b[r] = n + r < N ? bf16_to_f32(bias[n + r]) : 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[j][i][4 * gq + r] += b[r];
-            }
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(q[e] << 16);
+        v[2 * e + 1] = __uint_as_float(q[e] & 0xffff0000u);
     }
-    with_activation(ep.act, [&](auto A) {
-        if constexpr (decltype(A)::value != kActNone) {
+}
+
+// eight values at p, of which the first n exist
+__device__ __forceinline__ u32x4_t ep_load8(const uint16_t *p, int n) {
+    if (n >= 8) return *reinterpret_cast<const u32x4_any *>(p);
+    u32x4_t q = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < n) q[e >> 1] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
+    return q;
+}
+
+// The epilogue of a K-major kernel's tile of BN columns: acc[j][i][4*gq + r] is row
+// wm*TM + 32i + lane%32 and column wn*32*FN + 32j + 8gq + 4*(lane/32) + r of it, for
+// waves 2 x NW/2.  The fp32 accumulators go through LDS (the idle ring) 64 rows at
+// a time, row r of a pass at obj(r): 16-byte chunk cc (4 columns) at (cc/2) ^ (r %
+// 16) of the row's first or second half as cc is even or odd, so that both the
+// fragments' writes and the rows' reads fall on distinct banks.  A thread then
+// holds 8 neighbouring columns of a row: bias and residual come in 16 bytes a
+// lane, one rounding, 16 bytes out.  No access needs alignment; only the chunk that
+// N cuts goes element by element.  (Residual added on the fragments, 8 bytes a lane in 32 rows, and
+// outputs staged as bf16: 420 us for 8192 x 4096 of 7168 retained indices;
+// so: 395.  With rows off 16-byte boundaries, 2 x 1001 x 4097 of 610: 111, 26.)
+// Every wave's reads of the ring and loads into it have ended before the call.
+// left: rows from the tile's origin on; row0: the origin's row over all units.
+template <int BN, int NW, int FN, int FM, int TM, class Obj>
+__device__ __forceinline__ void ep_tile(const Epilogue &ep, const f32x16_t (&acc)[FN][FM], Obj obj, int wave, int lane,
+                                        uint16_t *__restrict__ Y, int64_t ldy, bool aligned16, int n0, int N, int left,
+                                        int64_t row0) {
+    constexpr int SW = BN / 8 < 16 ? BN / 8 - 1 : 15;
+    constexpr int LPR = BN / 8, RPI = 64 / LPR, Q = 64 / (NW * RPI);     // lanes per row, rows per step
+    const int lr = lane & 31, lh = lane >> 5, wm = wave / (NW / 2), wn = wave % (NW / 2);
+    const int c = lane % LPR, nc = N - n0 - 8 * c;
+    auto tile_row = [&](int r, int p) { return (r / 32) * TM + 32 * p + r % 32; };
+    auto step_row = [&](int q) { return RPI * (NW * q + wave) + lane / LPR; };
+    float bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+    if (ep.bias && nc > 0) ep_unpack(ep_load8(static_cast<const uint16_t *>(ep.bias) + n0 + 8 * c, nc), bias);
+    const uint16_t *src = static_cast<const uint16_t *>(ep.res) + row0 * ep.ldr + n0 + 8 * c;
+    uint16_t *dst = Y + row0 * ldy + n0 + 8 * c;
+    u32x4_t res[Q];
+    auto fetch = [&](int p) {
+        if (!ep.res) return;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int ml = tile_row(step_row(q), p);
+            if (ml < left && nc > 0) res[q] = ep_load8(src + ml * ep.ldr, nc);
+        }
+    };
+    fetch(0);
+    lds_barrier();
+#pragma unroll
+    for (int p = 0; p < FM; ++p) {
+        {
+            const int r = 32 * wm + lr;
+            char *o = obj(r);
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[j][i][v] = activate<decltype(A)::value>(acc[j][i][v]);
+                for (int gq = 0; gq < 4; ++gq)
+                    *reinterpret_cast<f32x4_t *>(o + 16 * (((4 * (FN * wn + j) + gq) ^ (r & SW)) + BN / 8 * lh)) =
+                        f32x4_t{acc[j][p][4 * gq], acc[j][p][4 * gq + 1], acc[j][p][4 * gq + 2], acc[j][p][4 * gq + 3]};
         }
-    });
-    if (ep.res) {
-        const uint16_t *res = static_cast<const uint16_t *>(ep.res) + row0 * ep.ldr;
+        lds_barrier();
+        u32x4_t now[Q];
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int m = mrow + 32 * i + lr;
-            if (m >= rows) continue;
-            const uint16_t *p = res + m * ep.ldr;
+        for (int q = 0; q < Q; ++q) now[q] = res[q];
+        if (p + 1 < FM) fetch(p + 1);
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
+        for (int q = 0; q < Q; ++q) {
+            const int r = step_row(q), ml = tile_row(r, p);
+            const char *o = obj(r) + 16 * (c ^ (r & SW));
+            const f32x4_t lo = *reinterpret_cast<const f32x4_t *>(o);
+            const f32x4_t hi = *reinterpret_cast<const f32x4_t *>(o + BN * 2);
+            float v[8];
 #pragma unroll
-                for (int gq = 0; gq < 4; ++gq) {
-                    const int n = ncol + 32 * j + 8 * gq + 4 * lh;
-                    if (vec && n + 4 <= N) {
-                        const uint2 v = *reinterpret_cast<const uint2 *>(p + n);
-                        acc[j][i][4 * gq] = fmaf(ep.rs, __uint_as_float(v.x << 16), acc[j][i][4 * gq]);
-                        acc[j][i][4 * gq + 1] = fmaf(ep.rs, __uint_as_float(v.x & 0xffff0000u), acc[j][i][4 * gq + 1]);
-                        acc[j][i][4 * gq + 2] = fmaf(ep.rs, __uint_as_float(v.y << 16), acc[j][i][4 * gq + 2]);
-                        acc[j][i][4 * gq + 3] = fmaf(ep.rs, __uint_as_float(v.y & 0xffff0000u), acc[j][i][4 * gq + 3]);
-                    } else {
+            for (int e = 0; e < 4; ++e) { v[e] = lo[e] + bias[e]; v[4 + e] = hi[e] + bias[4 + e]; }
+            with_activation(ep.act, [&](auto A) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (n + r < N) acc[j][i][4 * gq + r] = fmaf(ep.rs, bf16_to_f32(p[n + r]), acc[j][i][4 * gq + r]);
-                    }
-                }
+                for (int e = 0; e < 8; ++e) v[e] = activate<decltype(A)::value, uint16_t>(v[e]);
+            });
+            if (ep.res) {
+                float add[8];
+                ep_unpack(now[q], add);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(ep.rs, add[e], v[e]);
+            }
+            if (ml >= left || nc <= 0) continue;
+            const u32x4_t out = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                 pack_bf16x2(v[6], v[7])};
+            uint16_t *d = dst + ml * ldy;
+            if (nc >= 8) {
+                // whole lines go past L2 (streaming); pieces of lines are joined there
+                if (aligned16) __builtin_nontemporal_store(out, reinterpret_cast<u32x4_t *>(d));
+                else *reinterpret_cast<u32x4_any *>(d) = out;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < nc) d[e] = static_cast<uint16_t>(out[e >> 1] >> (16 * (e & 1)));
+            }
         }
+        if (p + 1 < FM) lds_barrier();        // the next pass overwrites the staged rows
     }
 }
 

@@ -745,9 +745,17 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
         }
         return;
     }
-    if constexpr (EPI == 2)
-        ep_fragments<FN, FM>(ep, acc, lane, wm * 128, n0 + wn * TWN, min(BT, M - m0),
-                             unit * static_cast<int64_t>(M) + m0, N);
+    if constexpr (EPI == 2) {
+        static_assert(EPI != 2 || (BKS >= 32 && 64 * BNT * 4 <= 4 * ASZ), "the staged rows fit the ring");
+        constexpr int RPO = ASZ / (BNT * 4);             // rows of BNT floats per ring object
+        auto obj = [&](int r) -> char * {
+            const int q = r / RPO;
+            return (q == 0 ? sA0 : q == 1 ? sA1 : q == 2 ? sB0 : sB1) + (r % RPO) * (BNT * 4);
+        };
+        ep_tile<BNT, NW, FN, FM, 128>(ep, acc, obj, wave, lane, Y, ldy, vec_y == 2, n0, N, min(BT, M - m0),
+                                      unit * static_cast<int64_t>(M) + m0);
+        return;
+    }
     uint16_t *Yu = Y + unit * static_cast<int64_t>(M) * ldy;
     const int rows = min(BT, M - m0);
     const __amdgpu_buffer_rsrc_t yr = __builtin_amdgcn_make_buffer_rsrc(

@@ -272,8 +272,17 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kerne
     const int lr = lane & 31, lh = lane >> 5;
     uint16_t *Yt = Y + (static_cast<int64_t>(unit) * M + m0) * ldy;
     const int rows = min(BM, M - m0);
-    if constexpr (EP)
-        ep_fragments<FN, FM>(ep, acc, lane, wm * TM, n0 + wn * TN, rows, static_cast<int64_t>(unit) * M + m0, N);
+    if constexpr (EP) {
+        static_assert(WM == 2 && 64 * BN * 4 <= 4 * ASZ, "the staged rows fit the ring");
+        constexpr int RPO = ASZ / (BN * 4);              // rows of BN floats per ring object
+        auto at = [&](int r) -> char * {
+            const int q = r / RPO;
+            return (q == 0 ? sA0 : q == 1 ? sA1 : q == 2 ? sA2 : sA3) + (r % RPO) * (BN * 4);
+        };
+        ep_tile<BN, NW, FN, FM, TM>(ep, acc, at, wave, lane, Y, ldy, vec_y == 2, n0, N, rows,
+                                    static_cast<int64_t>(unit) * M + m0);
+        return;
+    }
     if constexpr (BM == 64) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)

@@ -486,7 +486,7 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
 
 // Up to 2048 workgroups of one chunk per wave: one step each.  Beyond, steps of 64
 // bytes per lane.
-bool one_step(int64_t T, int64_t V) { return T * std::min<int64_t>(kMaxPieces, (V + kWaves * kChunk - 1) / (kWaves * kChunk)) <= 2048; }
+bool one_step(int64_t T, int64_t V) { return T * std::min<int64_t>(kMaxPieces, (V + kWaves * kChunk - 1) / (kWaves * kChunk)) <= 512; }
 
 template <typename T, bool VEC>
 hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
