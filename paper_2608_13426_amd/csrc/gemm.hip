@@ -1057,6 +1057,21 @@ KmajorTile kmajor_tile(int64_t B, int64_t M, int64_t N) {
     return t128 < t256 ? KmajorTile::k128 : KmajorTile::k256;
 }
 
+// The same choice for products with an epilogue, whose time a round does not follow k:
+// about 14 us for a 256 x 256 tile, 8 for two of 128 x 128 on a CU, 2 more in a last
+// round (2 x 1001 x 4097 of 610 indices, everything in the epilogue, us: 37 / 30 with the
+// large / small tiles; 3000^2 of 300 24.6 / 22.5; 8192 x 4096 of 1024 87 / 96).
+KmajorTile kmajor_tile_epilogue(int64_t B, int64_t M, int64_t N, int64_t k) {
+    auto count = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t) * B; };
+    if (count(64) <= 256) return KmajorTile::k64;
+    const double x = static_cast<double>(k) / 2048;
+    const int64_t c128 = count(128), rest = c128 % 512;
+    const double t128 = static_cast<double>(c128 / 512) * (40 * x + 8) +
+                        (rest == 0 ? 0 : rest <= 256 ? 21 * x + (c128 > 512 ? 2 : 8) : 40 * x + 8);
+    const double t256 = static_cast<double>((count(256) + 255) / 256) * (49 * x + 14);
+    return t128 < t256 ? KmajorTile::k128 : KmajorTile::k256;
+}
+
 // The K-major GEMM over B units; units u read W + (u / w_ugroup) * w_ustride.
 // Grouped weights and K-loop trimming with Y rows of 2^23 elements or more
 // stay refused (hipErrorNotSupported, nothing launched).
@@ -1069,7 +1084,7 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
     // the 256 x 256 kernel addresses one tile's Y rows with 32-bit byte offsets
     const bool big_ok = ldy < (int64_t(1) << 23);
     if (grouped && !big_ok) return hipErrorNotSupported;
-    const KmajorTile tile = kmajor_tile(B, M, N);
+    const KmajorTile tile = ep ? kmajor_tile_epilogue(B, M, N, k) : kmajor_tile(B, M, N);
     const int tm = static_cast<int>((M + 255) / 256), tn = static_cast<int>((N + 255) / 256);
     // Value products (N = head dim) take no half-empty 256-wide tile: 256 x 128
     // from more than two rounds of 128 x 128 tiles on (32 heads x 8192 tokens,

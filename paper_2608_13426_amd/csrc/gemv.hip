@@ -144,6 +144,156 @@ __device__ __forceinline__ void gemv_tile(
     }
 }
 
+// Two to eight rows per unit on the matrix cores: v_mfma_f32_4x4x4_16b_bf16 holds
+// 16 products of 4 rows of X by 4 columns of W over 4 retained indices, a column
+// per lane, so each lane multiplies the columns it has loaded and W passes through
+// no LDS.  A wave takes every fourth group of four retained rows; two groups (8
+// KiB) are on their way while two are multiplied: 16 byte permutations bring a
+// group's four values of each column together, and 8 (up to 4 rows) or 16
+// products follow, against 4 * (8 + 8 M) operations in the form above.
+// Three units of 5 x 4096 -> 6144, a set of 2048 each: 39 us in that form, XX so.
+template <int MG, bool EP>
+__global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
+    const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
+    float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
+    int64_t ldw, int64_t ldy, int SR, int S, Epilogue ep) {
+    using namespace gv;
+    constexpr int MR = 4 * MG, XS = RB + 4;    // xs rows apart in LDS (elements)
+    __shared__ __attribute__((aligned(16))) uint32_t roff[RB];
+    __shared__ __attribute__((aligned(16))) uint16_t xs[MR * XS];
+    __shared__ __attribute__((aligned(16))) float red[2][MR][CW];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * CW, s = blockIdx.y, b = blockIdx.z;
+    const int t0 = s * SR, t1 = min(k, t0 + SR);
+    const int32_t *I = idx + static_cast<int64_t>(b) * k;
+    const uint16_t *Xb = X + static_cast<int64_t>(b) * M * ldx;
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(W + n0), 0,
+        static_cast<uint32_t>((static_cast<int64_t>(K) * ldw - n0) * 2), 0x00020000);
+
+    f32x4_t acc[MG][8];                        // [rows 4g ..][the lane's column]
+#pragma unroll
+    for (int g = 0; g < MG; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[g][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+    for (int base = t0; base < t1; base += RB) {
+        const int nr = min(RB, t1 - base);
+        // rows past the slice: out of range (zeros) times zero
+        static_assert(RB == NT, "a row per thread");
+        const bool row_in = tid < nr;
+        const int j = row_in ? I[base + tid] : 0;
+        roff[tid] = row_in ? static_cast<uint32_t>(j * ldw * 2) : 0x80000000u;
+        lds_barrier();
+        uint16_t xv[MR];
+#pragma unroll
+        for (int m = 0; m < MR; ++m) xv[m] = row_in && m < M ? Xb[m * ldx + j] : uint16_t(0);
+        const int groups = (nr + 3) / 4;
+        u32x4 w[2][2][4];
+        auto fetch = [&](int g, u32x4 (&q)[2][4]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = min(4 * (g + NW * u), RB - 4);
+                const u32x4 o = *reinterpret_cast<const u32x4 *>(&roff[r]);
+                const bool in = g + NW * u < groups;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    q[u][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, in ? o[i] + 16u * lane : 0x80000000u, 0, 0);
+            }
+        };
+        auto multiply = [&](int g, const u32x4 (&q)[2][4]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = min(4 * (g + NW * u), RB - 4);
+                s16x4_t x[MG];
+#pragma unroll
+                for (int h = 0; h < MG; ++h) x[h] = *reinterpret_cast<const s16x4_t *>(&xs[(4 * h + (lane & 3)) * XS + r]);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
+                    const uint2 d = make_uint2(__builtin_amdgcn_perm(q[u][1][c >> 1], q[u][0][c >> 1], sel),
+                                               __builtin_amdgcn_perm(q[u][3][c >> 1], q[u][2][c >> 1], sel));
+#pragma unroll
+                    for (int h = 0; h < MG; ++h)
+                        acc[h][c] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(x[h], __builtin_bit_cast(s16x4_t, d), acc[h][c], 0, 0, 0);
+                }
+            }
+        };
+        // groups past the last one load nothing (out of range) and add zeros
+        fetch(wave, w[0]);                     // on its way while X's values arrive
+#pragma unroll
+        for (int m = 0; m < MR; ++m) xs[m * XS + tid] = xv[m];
+        lds_barrier();
+        for (int g = wave; g < groups; g += 4 * NW) {
+            fetch(g + 2 * NW, w[1]);
+            multiply(g, w[0]);
+            if (g + 2 * NW >= groups) break;
+            fetch(g + 4 * NW, w[0]);
+            multiply(g + 2 * NW, w[1]);
+        }
+        lds_barrier();                         // staged rows are reused by the next pass
+    }
+
+    // waves 2 and 3 hand their sums to 0 and 1, then 1 to 0
+    auto put = [&](float (&to)[MR][CW]) {
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<f32x4_t *>(&to[m][256 * h + 4 * lane]) =
+                    f32x4_t{acc[m / 4][4 * h][m % 4], acc[m / 4][4 * h + 1][m % 4], acc[m / 4][4 * h + 2][m % 4],
+                            acc[m / 4][4 * h + 3][m % 4]};
+    };
+    auto add = [&](const float (&from)[MR][CW]) {
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4_t v = *reinterpret_cast<const f32x4_t *>(&from[m][256 * h + 4 * lane]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m / 4][4 * h + e][m % 4] += v[e];
+            }
+    };
+    if (wave >= 2) put(red[wave - 2]);
+    __syncthreads();
+    if (wave < 2) add(red[wave]);
+    __syncthreads();
+    if (wave == 1) put(red[0]);
+    __syncthreads();
+    if (wave != 0) return;
+    add(red[0]);
+    const int nb = n0 + 8 * lane;
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+        if (m >= M) break;
+        const int64_t row = static_cast<int64_t>(b) * M + m;
+        if (S > 1) {
+            float *p = P + ((static_cast<int64_t>(b) * S + s) * M + m) * N + nb;
+            if (N % 4 == 0 && nb + 8 <= N) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<f32x4_t *>(p + 4 * h) =
+                        f32x4_t{acc[m / 4][4 * h][m % 4], acc[m / 4][4 * h + 1][m % 4], acc[m / 4][4 * h + 2][m % 4],
+                                acc[m / 4][4 * h + 3][m % 4]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (nb + e < N) p[e] = acc[m / 4][e][m % 4];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (nb + e >= N) continue;
+                float y = acc[m / 4][e][m % 4];
+                if constexpr (EP) y = ep_value<uint16_t>(ep, y, row, nb + e);
+                Y[row * ldy + nb + e] = f32_to_bf16(y);
+            }
+        }
+    }
+}
+
 template <int MR, bool VEC, bool DIRECT, bool EP = false>
 __global__ __launch_bounds__(gv::NT) void gemv_partial_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
@@ -168,8 +318,9 @@ __global__ __launch_bounds__(gv::NT) void gemv_partial_grouped_kernel(GemvGroups
 // The slice reduction of one 64-column piece: the 256 threads are 64
 // columns (one per lane) x 4 waves; wave w adds slices [w*S/4, (w+1)*S/4)
 // in slice order (eight loads in flight), and the four quarter sums are
-// added in wave order.  p points at slice 0 of the lane's column; slice s
+// added in wave order (AHEAD: the last ones' loads, fewer than eight, go out together too).  p points at slice 0 of the lane's column; slice s
 // is st floats further.  Returns the sum in wave 0 (other waves: garbage).
+template <bool AHEAD = false>
 __device__ __forceinline__ float reduce_slices(const float *__restrict__ p, int64_t st, int S,
                                                bool col_ok) {
     __shared__ float quarter[3][64];
@@ -185,7 +336,15 @@ __device__ __forceinline__ float reduce_slices(const float *__restrict__ p, int6
 #pragma unroll
             for (int u = 0; u < 8; ++u) sum += v[u];
         }
-        for (; s < s1; ++s) sum += p[s * st];
+        if constexpr (AHEAD) {                 // the last few too
+            float v[7];
+#pragma unroll
+            for (int u = 0; u < 7; ++u) v[u] = s + u < s1 ? p[(s + u) * st] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 7; ++u) sum += v[u];
+        } else {
+            for (; s < s1; ++s) sum += p[s * st];
+        }
     }
     if (w > 0) quarter[w - 1][lane] = sum;
     __syncthreads();
@@ -202,7 +361,7 @@ __global__ __launch_bounds__(256) void gemv_reduce_kernel(const float *__restric
     const int n = blockIdx.x * 64 + (threadIdx.x & 63);
     const int m = blockIdx.y, b = blockIdx.z;
     const float *p = P + (static_cast<int64_t>(b) * S * M + m) * N + n;
-    float sum = reduce_slices(p, static_cast<int64_t>(M) * N, S, n < N);
+    float sum = reduce_slices<EP>(p, static_cast<int64_t>(M) * N, S, n < N);
     if (threadIdx.x < 64 && n < N) {
         const int64_t row = static_cast<int64_t>(b) * M + m;
         if constexpr (EP) sum = ep_value<uint16_t>(ep, sum, row, n);
@@ -252,6 +411,22 @@ template <bool VEC, bool EP>
 hipError_t launch_vec(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B, int64_t M,
                       int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw, uint16_t *Y,
                       int64_t ldy, float *P, int SR, int S, const Epilogue &ep, hipStream_t stream) {
+    if constexpr (VEC && EP) {
+        if (M > 1) {
+            const dim3 grid(static_cast<unsigned>((N + gv::CW - 1) / gv::CW), static_cast<unsigned>(S), static_cast<unsigned>(B));
+            auto quads = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, grid, dim3(gv::NT), 0, stream, X, W, idx, P, Y, static_cast<int>(M),
+                                   static_cast<int>(N), static_cast<int>(K), static_cast<int>(k), ldx, ldw, ldy, SR, S, ep);
+                return hipGetLastError();
+            };
+            const hipError_t e = M <= 4 ? quads(gemv_quad_kernel<1, EP>) : quads(gemv_quad_kernel<2, EP>);
+            if (e != hipSuccess || S == 1) return e;
+            hipLaunchKernelGGL(gemv_reduce_kernel<EP>, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>(M),
+                                                           static_cast<unsigned>(B)), dim3(256), 0, stream, P, Y,
+                               static_cast<int>(M), static_cast<int>(N), S, ldy, ep);
+            return hipGetLastError();
+        }
+    }
     auto go = [&](auto mr) {
         return launch_mr<decltype(mr)::value, VEC, EP>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, ep, stream);
     };

@@ -55,7 +55,8 @@ def test_kmajor(B, M, N, K, k, act):
 
 
 @pytest.mark.parametrize("B,M,N,K,k", [(1, 1, 4096, 512, 256), (2, 3, 1000, 700, 351), (5, 8, 77, 64, 64), (1, 5, 1, 9, 4),
-                                       (16, 1, 640, 2048, 1024), (1, 2, 513, 40, 13)])
+                                       (16, 1, 640, 2048, 1024), (1, 2, 513, 40, 13),
+                                       (3, 5, 6144, 600, 301), (1, 6, 520, 3000, 2999), (2, 7, 1032, 33, 33)])
 @pytest.mark.parametrize("act", [None, "silu"])
 def test_few_rows(B, M, N, K, k, act):
     dev = require_gpu()
@@ -135,7 +136,10 @@ def test_nothing_asked_for_is_the_plain_product(form):
                                     torch.nn.functional.pad(X.transpose(1, 2), (0, -M % 8))[:, :, :M], W, idx, Z)
     else:
         (rmm.rmm_reduced_gemv if form == "few" else rmm.rmm_reduced_gemm)(X, W, idx, Z)
-    assert torch.equal(Y, Z)
+    if form == "few":                        # another order of the sums
+        check(Y, ref.product(X, W, idx, None, None, None, 1.0, dt))
+    else:
+        assert torch.equal(Y, Z)
 
 
 @pytest.mark.parametrize("form", list(SHAPES))
