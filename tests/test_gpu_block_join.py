@@ -59,7 +59,8 @@ def test_rows(dt, sd, B, M, K, post):
 
 @pytest.mark.parametrize("sd", [BF, F32])
 @pytest.mark.parametrize("B,M,K", [(1, 1, 8), (1, 7, 64), (2, 64, 72), (3, 65, 264), (1, 129, 4096), (2, 1001, 1024), (1, 33, 4104),
-                                   (1, 9, 8192), (1, 31, 16384), (1, 3000, 512), (5, 513, 128), (1, 2, 65536)])
+                                   (1, 9, 8192), (1, 31, 16384), (1, 3000, 512), (5, 513, 128), (1, 2, 65536),
+                                   (1, 4100, 1024), (2, 2100, 2056), (1, 4096, 4096), (3, 1500, 520)])
 @pytest.mark.parametrize("gate", ["none", "unit"])
 def test_kmajor(sd, B, M, K, gate):
     """The K-major outputs are the row-major ones, bit for bit, and their energies."""
@@ -114,6 +115,37 @@ def test_parts(K):
         _, Xt, e = kmajor(dev, 2, 9, K)
         rmm.rmm_block_join(Y, R, H, Xt=Xt, energy=e, post_norm=True, eps=EPS)
         assert torch.equal(Xt.transpose(1, 2), X)
+
+
+@pytest.mark.parametrize("parts", ["all", "no Y", "no R", "no gains", "in place", "strided", "channel gate", "eps 0"])
+def test_many_rows(parts):
+    """The one-pass form's inputs left out in turn, against the row-major outputs."""
+    dev = require_gpu()
+    B, M, K = 2, 2100, 1032
+    Y, R, gp, gq, gt = make(dev, BF, BF, B, M, K, "channel", seed=8)
+    if parts == "strided":
+        Y, R = (torch.cat([t, t[..., :16]], -1)[..., :K] for t in (Y, R))
+    Y[1, 7] = 0
+    kw = dict(post_norm=True, post_gamma=gp, pre_gamma=gq, residual_scale=0.5, eps=EPS)
+    if parts == "no Y":
+        kw.update(post_norm=False, post_gamma=None)
+        Y = None
+    if parts == "no R":
+        R = None
+    if parts == "no gains":
+        kw.update(post_gamma=None, pre_gamma=None)
+    if parts == "channel gate":
+        kw.update(gate=gt)
+    if parts == "eps 0":
+        kw.update(post_norm=False, post_gamma=None, eps=0.0)
+    H, X = (torch.empty(B, M, K, dtype=BF, device=dev) for _ in range(2))
+    rmm.rmm_block_join(Y, R, H, X=X, **kw)
+    held, Xt, e = kmajor(dev, B, M, K, 5.0)
+    H2 = R if parts == "in place" else torch.empty_like(H)
+    rmm.rmm_block_join(Y, R, H2, Xt=Xt, energy=e, **kw)
+    assert torch.equal(H, H2) and torch.equal(Xt.transpose(1, 2), X)
+    assert bool((held[:, :, M:] == 5.0).all())
+    check_energies(e.cpu().numpy(), X.double().square().sum(1).flatten().cpu().numpy(), M + 1)
 
 
 def test_kmajor_matches_selection_input():
