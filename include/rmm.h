@@ -906,8 +906,7 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
  * epilogue: host struct (NULL: none of the three).  bias: N values of the
  *           product's type, or NULL.  residual: of the product's type, [B][M][ldr]
  *           (units M*ldr apart), or NULL (residual_scale is then not read); it may
- *           be Y itself (ldr == ldy) and must not overlap it otherwise.  16-byte
- *           aligned rows and bias are read fastest.
+ *           be Y itself (ldr == ldy) and must not overlap it otherwise.
  * Everything else as rmm_reduced_gemm (B <= 65535, M <= 65535*32),
  * rmm_reduced_gemm_kmajor and rmm_reduced_gemv (bf16, M <= 8; workspace
  * rmm_gemv_workspace_size).
@@ -971,7 +970,6 @@ rmm_status_t rmm_reduced_gemv_epilogue(const void *X, const void *W, const int32
  *               rmm_reduced_gemm_kmajor; bf16, needs H.
  * workspace   : rmm_block_join_workspace_size(B, M, K) bytes with Xt, 256-byte
  *               aligned (else not used).
- * Rows that are 16-byte aligned with K % 8 == 0 are read fastest.
  * Errors      : INVALID_ARGUMENT for sizes < 1, both Y and R or all outputs
  *               missing, Xt without energy or H, leading dimensions below the
  *               widths, negative gate strides, eps negative, infinite or NaN, an

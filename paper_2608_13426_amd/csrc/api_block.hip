@@ -164,23 +164,23 @@ rmm_status_t rmm_block_join(const rmm_join_t *j, void *workspace, size_t workspa
     a.post = j->post_norm != 0;
     a.rs = j->residual_scale;
     a.eps = j->eps;
-    auto rows_ok = [](const void *p, int64_t ld, size_t sz) { return !p || (aligned(p, 16) && ld * sz % 16 == 0); };
-    const bool vec = K % 8 == 0 && rows_ok(a.y, a.ldy, size) && rows_ok(a.x, a.ldx, size) && rows_ok(a.r, a.ldr, ssize) &&
-                     rows_ok(a.h, a.ldh, ssize) && aligned(a.gpost, 16) && aligned(a.gpre, 16) && aligned(a.gate, 16) &&
-                     a.gate_unit * size % 16 == 0 && a.gate_row * size % 16 == 0;
     const bool bf16 = j->dtype == RMM_BF16, stream_bf16 = j->stream_dtype == RMM_BF16;
-    if (!j->Xt) return from_hip(rmm::launch_join_rows(a, bf16, stream_bf16, vec, stream));
+    if (!j->Xt) return from_hip(rmm::launch_join_rows(a, bf16, stream_bf16, stream));
     const size_t need = rmm_block_join_workspace_size(B, M, K);
     if (!workspace || workspace_bytes < need) return RMM_ERR_WORKSPACE_TOO_SMALL;
     if (!aligned(workspace, 256)) return RMM_ERR_INVALID_ARGUMENT;
     a.rscale = static_cast<float *>(workspace);
     double *partials = reinterpret_cast<double *>(static_cast<char *>(workspace) +
                                                   align256(static_cast<size_t>(B * M) * sizeof(float)));
+    auto rows_ok = [](const void *p, int64_t ld, size_t sz) { return !p || (aligned(p, 16) && ld * sz % 16 == 0); };
+    const bool vec = K % 8 == 0 && rows_ok(a.y, a.ldy, size) && rows_ok(a.x, a.ldx, size) && rows_ok(a.r, a.ldr, ssize) &&
+                     rows_ok(a.h, a.ldh, ssize) && aligned(a.gpost, 16) && aligned(a.gpre, 16) && aligned(a.gate, 16) &&
+                     a.gate_unit * size % 16 == 0 && a.gate_row * size % 16 == 0;
     if (rmm::join_block_ok(a, bf16, stream_bf16, vec)) {
         a.rscale = nullptr;
         return from_hip(rmm::launch_join_block(a, static_cast<uint16_t *>(j->Xt), j->ldxt, partials, j->energy, stream));
     }
-    const hipError_t e = rmm::launch_join_rows(a, bf16, stream_bf16, vec, stream);
+    const hipError_t e = rmm::launch_join_rows(a, bf16, stream_bf16, stream);
     if (e != hipSuccess) return RMM_ERR_HIP;
     return from_hip(rmm::launch_join_kmajor(a.h, stream_bf16, a.ldh, a.rscale, static_cast<const uint16_t *>(a.gpre), B, M,
                                             K, static_cast<uint16_t *>(j->Xt), j->ldxt, partials, j->energy, stream));
@@ -226,8 +226,7 @@ rmm_status_t rmm_token_logprobs(const void *logits, rmm_dtype_t dtype, int64_t T
     a.top_idx = top_idx;
     a.top_logp = top_logp;
     a.part = workspace;
-    const bool vec = aligned(logits, 16) && ldl * size % 16 == 0;
-    return from_hip(rmm::launch_logprobs(a, dtype == RMM_BF16, vec, stream));
+    return from_hip(rmm::launch_logprobs(a, dtype == RMM_BF16, stream));
 }
 
 }  // extern "C"

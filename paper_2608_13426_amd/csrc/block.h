@@ -23,9 +23,8 @@ struct JoinArgs {
     float *rscale;                   // [rows] 1 / rms of the stored h, or null
 };
 constexpr int64_t kJoinMaxK = 65536;
-// y_bf16: type of y, the gains, the gate and x; stream_bf16: of r and h; vec: K %
-// 8 == 0 and every given row and vector 16-byte aligned
-hipError_t launch_join_rows(const JoinArgs &a, bool y_bf16, bool stream_bf16, bool vec, hipStream_t stream);
+// y_bf16: type of y, the gains, the gate and x; stream_bf16: of r and h
+hipError_t launch_join_rows(const JoinArgs &a, bool y_bf16, bool stream_bf16, hipStream_t stream);
 // Xt[b][j][m] = bf16(H[b][m][j] * rscale[b][m] * gpre[j]) and the column energies
 // of Xt; out: energy itself when splits == 1, else [B][splits][K] partials
 int64_t join_splits(int64_t B, int64_t M, int64_t K);
@@ -34,7 +33,8 @@ hipError_t launch_join_kmajor(const void *H, bool stream_bf16, int64_t ldh, cons
                               double *energy, hipStream_t stream);
 
 // the same and the rows kernel's work in one pass (join_block_ok: bf16, K <= 4096, no
-// gate per token); partials: [B][join_blocks(M)][K] when there is more than one block
+// gate per token, and vec: K % 8 == 0 with every given row and vector 16-byte
+// aligned); partials: [B][join_blocks(M)][K] when there is more than one block
 int64_t join_blocks(int64_t M);
 bool join_block_ok(const JoinArgs &a, bool y_bf16, bool stream_bf16, bool vec);
 hipError_t launch_join_block(const JoinArgs &a, uint16_t *Xt, int64_t ldxt, double *partials, double *energy,
@@ -55,6 +55,6 @@ struct LogprobArgs {
 constexpr int kMaxTop = 64;
 int logprob_pieces(int64_t T, int64_t V);
 size_t logprob_workspace_bytes(int64_t T, int64_t V, int64_t top);
-hipError_t launch_logprobs(const LogprobArgs &a, bool bf16, bool vec, hipStream_t stream);
+hipError_t launch_logprobs(const LogprobArgs &a, bool bf16, hipStream_t stream);
 
 }  // namespace rmm

@@ -26,11 +26,27 @@ template <typename T>
 struct Raw8 {
     uint4 q[sizeof(T) / 2];
 };
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_raw(const T *p) {
-    Raw8<T> r;
+// 16 bytes at any address (global memory takes them at every alignment)
+typedef uint32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
+// the first n of them exist, the others are zeros; without TAIL all or none do
+template <bool TAIL = false, typename T>
+__device__ __forceinline__ Raw8<T> load_raw(const T *p, int n = 8) {
+    Raw8<T> r = {};
+    if (TAIL ? n >= 8 : n > 0) {
 #pragma unroll
-    for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i) {
+            const any16 v = reinterpret_cast<const any16 *>(p)[i];
+            r.q[i] = make_uint4(v.x, v.y, v.z, v.w);
+        }
+    } else if constexpr (TAIL) {
+        uint32_t *w = &r.q[0].x;
+#pragma unroll
+        for (int e = 0; e < 7; ++e) {
+            if (e >= n) continue;
+            if constexpr (sizeof(T) == 2) w[e >> 1] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
+            else w[e] = __float_as_uint(p[e]);
+        }
+    }
     return r;
 }
 __device__ __forceinline__ void unpack(const Raw8<uint16_t> &r, float (&v)[8]) {
@@ -52,27 +68,37 @@ __device__ __forceinline__ void unpack(const Raw8<float> &r, float (&v)[8]) {
 }
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, float (&v)[8]) { unpack(load_raw(p), v); }
-__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                               pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+template <bool TAIL>
+__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8], int n) {
+    const any16 q = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    if (TAIL ? n >= 8 : n > 0) {
+        *reinterpret_cast<any16 *>(p) = q;
+    } else if constexpr (TAIL) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = static_cast<uint16_t>(q[e >> 1] >> (16 * (e & 1)));
+    }
 }
-__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
-    *reinterpret_cast<f32x4_t *>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_t *>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+template <bool TAIL>
+__device__ __forceinline__ void store8(float *p, const float (&v)[8], int n) {
+    typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+    if (TAIL ? n >= 8 : n > 0) {
+        reinterpret_cast<f32x4_any *>(p)[0] = f32x4_any{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<f32x4_any *>(p)[1] = f32x4_any{v[4], v[5], v[6], v[7]};
+    } else if constexpr (TAIL) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = v[e];
+    }
 }
-__device__ __forceinline__ float load1(const uint16_t *p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ float load1(const float *p) { return *p; }
-__device__ __forceinline__ void store1(uint16_t *p, float v) { *p = f32_to_bf16(v); }
-__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 template <class T>
 __device__ __forceinline__ float rounded(float v) {
     return std::is_same<T, uint16_t>::value ? bf16_to_f32(f32_to_bf16(v)) : v;
 }
 
-// One workgroup per row.  VEC: thread t holds elements 8 (t + NT c) .. + 7 of the
-// row, c < C, and asks for all of its block's and stream's values before the
-// first sum; otherwise elements t + NT e, e < 8 C.
-template <typename TY, typename TS, int NT, int C, bool VEC>
+// One workgroup per row: thread t holds elements 8 (t + NT c) .. + 7, c < C, and
+// asks for all of its block's and stream's values before the first sum.
+template <typename TY, typename TS, bool TAIL, int NT, int C>
 __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
 #pragma clang fp contract(off)
     const int64_t row = blockIdx.x;
@@ -83,52 +109,21 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
     const TS *r = a.r ? static_cast<const TS *>(a.r) + row * a.ldr : nullptr;
     const TY *gate = a.gate ? static_cast<const TY *>(a.gate) + unit * a.gate_unit + m * a.gate_row : nullptr;
     const TY *gpost = static_cast<const TY *>(a.gpost), *gpre = static_cast<const TY *>(a.gpre);
-
-    // chunk c of a row: absent elements are zeros
-    auto load = [&](auto *p, int c, float (&v)[8]) {
-        if constexpr (VEC) {
-            const int j = 8 * (t + NT * c);
-            if (j < K) {
-                load8(p + j, v);
-            } else {
+    auto first = [&](int c) { return 8 * (t + NT * c); };
+    // chunk c of a row; absent elements are zeros
+    auto load = [&](auto *p, int c, float (&v)[8]) { unpack(load_raw<TAIL>(p + first(c), K - first(c)), v); };
+    auto store = [&](auto *p, int c, const float (&v)[8]) { store8<TAIL>(p + first(c), v, K - first(c)); };
+    Raw8<TY> yq[C];
+    Raw8<TS> rq[C];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
-            }
-        } else {
+    for (int c = 0; c < C; ++c) {
+        yq[c] = {};
+        if (y) yq[c] = load_raw<TAIL>(y + first(c), K - first(c));
+    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = t + NT * (8 * c + e);
-                v[e] = j < K ? load1(p + j) : 0.f;
-            }
-        }
-    };
-    auto store = [&](auto *p, int c, const float (&v)[8]) {
-        if constexpr (VEC) {
-            const int j = 8 * (t + NT * c);
-            if (j < K) store8(p + j, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = t + NT * (8 * c + e);
-                if (j < K) store1(p + j, v[e]);
-            }
-        }
-    };
-    Raw8<TY> yq[VEC ? C : 1];
-    Raw8<TS> rq[VEC ? C : 1];
-    if constexpr (VEC) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = 8 * (t + NT * c);
-            yq[c] = {};
-            rq[c] = {};
-            if (y && j < K) yq[c] = load_raw(y + j);
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = 8 * (t + NT * c);
-            if (r && j < K) rq[c] = load_raw(r + j);
-        }
+    for (int c = 0; c < C; ++c) {
+        rq[c] = {};
+        if (r) rq[c] = load_raw<TAIL>(r + first(c), K - first(c));
     }
     __shared__ double red[2][NT / 64];
     // 1 / rms of the row's values, the same in every thread
@@ -154,7 +149,7 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
     if (y) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if constexpr (VEC) unpack(yq[c], h[c]); else load(y, c, h[c]);
+            unpack(yq[c], h[c]);
         }
         if (a.post) {
             const float ry = inv_rms(h, 0);
@@ -180,7 +175,7 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float v[8];
-            if constexpr (VEC) unpack(rq[c], v); else load(r, c, v);
+            unpack(rq[c], v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[c][e] = y ? a.rs * v[e] + h[c][e] : a.rs * v[e];
         }
@@ -496,32 +491,26 @@ __global__ __launch_bounds__(64 * NW, 4) void join_block_kernel(JoinArgs a, uint
     }
 }
 
-template <typename TY, typename TS, bool VEC>
+// TAIL: K % 8 != 0
+template <typename TY, typename TS, bool TAIL>
 hipError_t launch_rows(const JoinArgs &a, hipStream_t stream) {
     auto go = [&](auto kernel, int nt) {
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.rows)), dim3(nt), 0, stream, a);
         return hipGetLastError();
     };
-    // up to 512 rows: as many threads as chunks, for the shortest wait (64 x 4096,
-    // 512 x 1 / 256 x 2 / 128 x 4: 4.6 / 5.0 / 6.3 us).  More: two to four chunks per
+    // Few rows: as many threads as chunks, for the shortest wait (64 x 4096, 512 x 1 /
+    // 256 x 2 / 128 x 4: 4.6 / 5.0 / 6.3 us).  From 4096 waves on: two to four chunks per
     // thread (8192 x 4096 bf16, 512 x 1 / 256 x 2 / 128 x 4 / 64 x 8: 63 / 56 / 58 / 66 us;
     // 8192 x 2048, 512 x 1 / 256 x 2 / 64 x 4: 46 / 36 / 32; 2002 x 8192 with an fp32
     // stream, 1024 x 1 / 512 x 2 / 256 x 4: 45.6 / 44.8 / 48.8)
-    if constexpr (VEC) {
-        if (a.rows > 512) {
-            if (a.K <= 64 * 8) return go(join_rows_kernel<TY, TS, 64, 1, VEC>, 64);
-            if (a.K <= 64 * 16) return go(join_rows_kernel<TY, TS, 64, 2, VEC>, 64);
-            if (a.K <= 64 * 32) return go(join_rows_kernel<TY, TS, 64, 4, VEC>, 64);
-            if (a.K <= 256 * 16) return go(join_rows_kernel<TY, TS, 256, 2, VEC>, 256);
-            if (a.K <= 512 * 16) return go(join_rows_kernel<TY, TS, 512, 2, VEC>, 512);
-            if (a.K <= 512 * 32) return go(join_rows_kernel<TY, TS, 512, 4, VEC>, 512);
-        }
-    }
-    if (a.K <= 256 * 8) return go(join_rows_kernel<TY, TS, 256, 1, VEC>, 256);
-    if (a.K <= 512 * 8) return go(join_rows_kernel<TY, TS, 512, 1, VEC>, 512);
-    if (a.K <= 1024 * 8) return go(join_rows_kernel<TY, TS, 1024, 1, VEC>, 1024);
-    if (a.K <= 1024 * 16) return go(join_rows_kernel<TY, TS, 1024, 2, VEC>, 1024);
-    return go(join_rows_kernel<TY, TS, 1024, 8, VEC>, 1024);
+    const auto many = [&](int waves) { return a.rows * waves >= 4096; };
+    if (a.K <= 64 * 8) return go(join_rows_kernel<TY, TS, TAIL, 64, 1>, 64);
+    if (a.K <= 128 * 8) return many(1) ? go(join_rows_kernel<TY, TS, TAIL, 64, 2>, 64) : go(join_rows_kernel<TY, TS, TAIL, 128, 1>, 128);
+    if (a.K <= 256 * 8) return many(1) ? go(join_rows_kernel<TY, TS, TAIL, 64, 4>, 64) : go(join_rows_kernel<TY, TS, TAIL, 256, 1>, 256);
+    if (a.K <= 512 * 8) return many(4) ? go(join_rows_kernel<TY, TS, TAIL, 256, 2>, 256) : go(join_rows_kernel<TY, TS, TAIL, 512, 1>, 512);
+    if (a.K <= 1024 * 8) return many(8) ? go(join_rows_kernel<TY, TS, TAIL, 512, 2>, 512) : go(join_rows_kernel<TY, TS, TAIL, 1024, 1>, 1024);
+    if (a.K <= 1024 * 16) return many(8) ? go(join_rows_kernel<TY, TS, TAIL, 512, 4>, 512) : go(join_rows_kernel<TY, TS, TAIL, 1024, 2>, 1024);
+    return go(join_rows_kernel<TY, TS, TAIL, 1024, 8>, 1024);
 }
 
 constexpr int64_t kJoinRows = 64;                   // rows of a K-major tile
@@ -536,12 +525,14 @@ int64_t rows_per_split(int64_t B, int64_t M, int64_t K) {
 
 }  // namespace
 
-hipError_t launch_join_rows(const JoinArgs &a, bool y_bf16, bool stream_bf16, bool vec, hipStream_t stream) {
-    if (y_bf16 && stream_bf16)
-        return vec ? launch_rows<uint16_t, uint16_t, true>(a, stream) : launch_rows<uint16_t, uint16_t, false>(a, stream);
-    if (y_bf16)
-        return vec ? launch_rows<uint16_t, float, true>(a, stream) : launch_rows<uint16_t, float, false>(a, stream);
-    return vec ? launch_rows<float, float, true>(a, stream) : launch_rows<float, float, false>(a, stream);
+hipError_t launch_join_rows(const JoinArgs &a, bool y_bf16, bool stream_bf16, hipStream_t stream) {
+    auto go = [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if (y_bf16)
+            return stream_bf16 ? launch_rows<uint16_t, uint16_t, TAIL>(a, stream) : launch_rows<uint16_t, float, TAIL>(a, stream);
+        return launch_rows<float, float, TAIL>(a, stream);
+    };
+    return a.K % 8 ? go(std::true_type{}) : go(std::false_type{});
 }
 
 int64_t join_splits(int64_t B, int64_t M, int64_t K) {

@@ -259,6 +259,9 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t key, int top) {
     return threadIdx.x < kMaxTop ? out[threadIdx.x] : 0;
 }
 
+// 16 bytes at any address (global memory takes them at every alignment)
+typedef uint32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
+
 // One chunk of a row: 8 logits of each lane, as loaded.
 template <typename T>
 struct Raw {
@@ -278,7 +281,7 @@ struct Raw {
 template <typename T>
 constexpr int group_of = sizeof(T) == 2 ? 4 : 2;
 
-template <typename T, bool VEC, bool ENT, int kGroup>
+template <typename T, bool ENT, int kGroup>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const int64_t row = blockIdx.x / a.pieces;
     const int piece = static_cast<int>(blockIdx.x - row * a.pieces);
@@ -295,13 +298,13 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     bool fresh = a.top > 0;
 
     // element e of this lane in chunk ch
-    auto index = [&](int ch, int e) { return ch * kChunk + (VEC ? 8 * lane + e : lane + 64 * e); };
+    auto index = [&](int ch, int e) { return ch * kChunk + 8 * lane + e; };
     constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -infinity
     auto load = [&](int ch, Raw<T> &r) {
-        if (VEC && ch < whole) {
-            const uint4 *p = reinterpret_cast<const uint4 *>(z + index(ch, 0));
+        if (ch < whole) {
+            const any16 *p = reinterpret_cast<const any16 *>(z + index(ch, 0));
 #pragma unroll
-            for (int i = 0; i < Raw<T>::N; ++i) r.q[i] = p[i];
+            for (int i = 0; i < Raw<T>::N; ++i) r.q[i] = make_uint4(p[i].x, p[i].y, p[i].z, p[i].w);
             return;
         }
         uint32_t w[4 * Raw<T>::N];
@@ -488,7 +491,7 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
 // bytes per lane.
 bool one_step(int64_t T, int64_t V) { return T * std::min<int64_t>(kMaxPieces, (V + kWaves * kChunk - 1) / (kWaves * kChunk)) <= 512; }
 
-template <typename T, bool VEC>
+template <typename T>
 hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.T * a.pieces));
     auto go = [&](auto kernel) {
@@ -496,8 +499,8 @@ hipError_t launch(const LogprobArgs &a, hipStream_t stream) {
         return hipGetLastError();
     };
     constexpr int G = group_of<T>;
-    const hipError_t e = one_step(a.T, a.V) ? a.entropy ? go(logprob_kernel<T, VEC, true, 1>) : go(logprob_kernel<T, VEC, false, 1>)
-                                            : a.entropy ? go(logprob_kernel<T, VEC, true, G>) : go(logprob_kernel<T, VEC, false, G>);
+    const hipError_t e = one_step(a.T, a.V) ? a.entropy ? go(logprob_kernel<T, true, 1>) : go(logprob_kernel<T, false, 1>)
+                                            : a.entropy ? go(logprob_kernel<T, true, G>) : go(logprob_kernel<T, false, G>);
     if (e != hipSuccess || a.pieces == 1) return e;
     hipLaunchKernelGGL(logprob_join_kernel<T>, dim3(static_cast<unsigned>(a.T)), dim3(64), 0, stream, a);
     return hipGetLastError();
@@ -516,9 +519,8 @@ size_t logprob_workspace_bytes(int64_t T, int64_t V, int64_t top) {
     return n == 1 ? 0 : static_cast<size_t>(T * n) * (sizeof(Part) + 8 * static_cast<size_t>(top));
 }
 
-hipError_t launch_logprobs(const LogprobArgs &a, bool bf16, bool vec, hipStream_t stream) {
-    if (bf16) return vec ? launch<uint16_t, true>(a, stream) : launch<uint16_t, false>(a, stream);
-    return vec ? launch<float, true>(a, stream) : launch<float, false>(a, stream);
+hipError_t launch_logprobs(const LogprobArgs &a, bool bf16, hipStream_t stream) {
+    return bf16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }
 
 }  // namespace rmm
