@@ -1,7 +1,6 @@
 // C-ABI of the products with an epilogue, the join with the residual stream and
 // the token log probabilities: host-side validation and dispatch.  Every check
 // happens before the first HIP call.
-#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -113,8 +112,7 @@ rmm_status_t rmm_reduced_gemv_epilogue(const void *X, const void *W, const int32
 
 size_t rmm_block_join_workspace_size(int64_t B, int64_t M, int64_t K) {
     if (B < 1 || M < 1 || K < 1 || K > rmm::kJoinMaxK || B > kGridYZMax || M >= kMaxRows / B) return 0;
-    // enough for either path (the path also depends on types and strides)
-    const int64_t S = std::max(rmm::join_splits(B, M, K), rmm::join_blocks(M));
+    const int64_t S = rmm::join_splits(B, M, K);
     return align256(static_cast<size_t>(B * M) * sizeof(float)) +
            (S == 1 ? 0 : align256(static_cast<size_t>(B * S * K) * sizeof(double)));
 }
@@ -172,14 +170,6 @@ rmm_status_t rmm_block_join(const rmm_join_t *j, void *workspace, size_t workspa
     a.rscale = static_cast<float *>(workspace);
     double *partials = reinterpret_cast<double *>(static_cast<char *>(workspace) +
                                                   align256(static_cast<size_t>(B * M) * sizeof(float)));
-    auto rows_ok = [](const void *p, int64_t ld, size_t sz) { return !p || (aligned(p, 16) && ld * sz % 16 == 0); };
-    const bool vec = K % 8 == 0 && rows_ok(a.y, a.ldy, size) && rows_ok(a.x, a.ldx, size) && rows_ok(a.r, a.ldr, ssize) &&
-                     rows_ok(a.h, a.ldh, ssize) && aligned(a.gpost, 16) && aligned(a.gpre, 16) && aligned(a.gate, 16) &&
-                     a.gate_unit * size % 16 == 0 && a.gate_row * size % 16 == 0;
-    if (rmm::join_block_ok(a, bf16, stream_bf16, vec)) {
-        a.rscale = nullptr;
-        return from_hip(rmm::launch_join_block(a, static_cast<uint16_t *>(j->Xt), j->ldxt, partials, j->energy, stream));
-    }
     const hipError_t e = rmm::launch_join_rows(a, bf16, stream_bf16, stream);
     if (e != hipSuccess) return RMM_ERR_HIP;
     return from_hip(rmm::launch_join_kmajor(a.h, stream_bf16, a.ldh, a.rscale, static_cast<const uint16_t *>(a.gpre), B, M,

@@ -32,14 +32,6 @@ hipError_t launch_join_kmajor(const void *H, bool stream_bf16, int64_t ldh, cons
                               int64_t B, int64_t M, int64_t K, uint16_t *Xt, int64_t ldxt, double *partials,
                               double *energy, hipStream_t stream);
 
-// the same and the rows kernel's work in one pass (join_block_ok: bf16, K <= 4096, no
-// gate per token, and vec: K % 8 == 0 with every given row and vector 16-byte
-// aligned); partials: [B][join_blocks(M)][K] when there is more than one block
-int64_t join_blocks(int64_t M);
-bool join_block_ok(const JoinArgs &a, bool y_bf16, bool stream_bf16, bool vec);
-hipError_t launch_join_block(const JoinArgs &a, uint16_t *Xt, int64_t ldxt, double *partials, double *energy,
-                             hipStream_t stream);
-
 // -------------------------------------------------------------- logprobs
 struct LogprobArgs {
     const void *z;                   // [T] rows of V logits

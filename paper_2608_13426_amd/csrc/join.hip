@@ -96,8 +96,9 @@ __device__ __forceinline__ float rounded(float v) {
     return std::is_same<T, uint16_t>::value ? bf16_to_f32(f32_to_bf16(v)) : v;
 }
 
-// One workgroup per row: thread t holds elements 8 (t + NT c) .. + 7, c < C, and
-// asks for all of its block's and stream's values before the first sum.
+// One workgroup per row: thread t holds elements 8 (t + NT c) .. + 7, c < C.  The
+// stream is asked for after the block's sum, all chunks together: asked for before
+// it, everything took 5 to 12 % longer (8192 x 4096 50 / 54 us, 2002 x 8192 29 / 33).
 template <typename TY, typename TS, bool TAIL, int NT, int C>
 __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
 #pragma clang fp contract(off)
@@ -119,11 +120,6 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
     for (int c = 0; c < C; ++c) {
         yq[c] = {};
         if (y) yq[c] = load_raw<TAIL>(y + first(c), K - first(c));
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        rq[c] = {};
-        if (r) rq[c] = load_raw<TAIL>(r + first(c), K - first(c));
     }
     __shared__ double red[2][NT / 64];
     // 1 / rms of the row's values, the same in every thread
@@ -170,6 +166,11 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
                 for (int e = 0; e < 8; ++e) h[c][e] = h[c][e] * g[e];
             }
         }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        rq[c] = {};
+        if (r) rq[c] = load_raw<TAIL>(r + first(c), K - first(c));
     }
     if (r) {
 #pragma unroll
@@ -280,217 +281,6 @@ __global__ __launch_bounds__(256) void join_kmajor_kernel(
     }
 }
 
-// K-major outputs in one pass, for bf16 rows of up to 4096: a workgroup holds 32
-// whole rows in registers (NW waves; lane 16 mc + jc of a wave holds rows 8 mc .. +
-// 7 and columns 8 jc .. + 7 of each of its two tiles of 32 x 128, one 16-byte load
-// per row), so that the stored stream is not read again.  The stream of a wave's
-// first tile is on its way while the rows of Y are summed.  Row sums: the lane's
-// columns, 16 lanes, then the 16 waves.  Xt goes out as 64-byte pieces (32 tokens);
-// the two blocks that share each 128-byte line run on the same XCD, whose L2 joins
-// them.  One float64 partial energy per (block, column).
-constexpr int kBlkRows = 32, kBlkCols = 128, kBlkTiles = 2, kBlkMaxWaves = 16;
-template <int NW>
-__global__ __launch_bounds__(64 * NW, 4) void join_block_kernel(JoinArgs a, uint16_t *__restrict__ Xt, int64_t ldxt,
-                                                                    double *__restrict__ out) {
-#pragma clang fp contract(off)
-    constexpr int TPW = kBlkTiles;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int jc = lane & 15, mc = lane >> 4;
-    const int64_t nblk = gridDim.x, unit = blockIdx.y;
-    const int K = a.K;
-    int64_t blk = blockIdx.x;
-    if (nblk % 16 == 0) {                          // workgroups w and w + 8 are on one XCD
-        const int64_t x = blk % 8, i = blk / 8;
-        blk = 2 * (8 * (i / 2) + x) + (i % 2);
-    }
-    const int64_t m0 = blk * kBlkRows, row0 = unit * a.M + m0;
-    const int rows = static_cast<int>(min<int64_t>(kBlkRows, a.M - m0));
-    constexpr uint32_t kOut = 0x80000000u;
-    auto rsrc = [&](const void *p, int64_t ld) {
-        return __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t *>(static_cast<const uint16_t *>(p) + (p ? row0 * ld : 0)), 0,
-            p ? static_cast<uint32_t>(rows * ld * 2) : 0u, 0x00020000);
-    };
-    const __amdgpu_buffer_rsrc_t ys = rsrc(a.y, a.ldy), rs = rsrc(a.r, a.ldr);
-    auto col = [&](int t) { return (wave + NW * t) * kBlkCols + 8 * jc; };      // K % 8 == 0: whole groups
-    auto load = [&](const __amdgpu_buffer_rsrc_t &s, int64_t ld, int t, int r) {
-        const int j = col(t);
-        const uint32_t off = j < K ? static_cast<uint32_t>(((8 * mc + r) * ld + j) * 2) : kOut;
-        const auto v = __builtin_amdgcn_raw_buffer_load_b128(s, off, 0, 0);
-        return make_uint4(v[0], v[1], v[2], v[3]);
-    };
-    // gains stay packed: bf16 ones where there are none
-    auto vec8 = [&](const void *p, int j) {
-        return p && j < K ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + j)
-                          : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-    };
-    __shared__ double red[NW][kBlkRows];
-    __shared__ float scale[kBlkRows];
-    // scale[row] = 1 / rms of each row from every lane's sums of squares; 0 for absent
-    // rows, whose zeros would meet an infinity where eps is 0
-    auto row_scales = [&](double (&s)[8]) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            s[r] += dpp_f64<0xB1>(s[r]);
-            s[r] += dpp_f64<0x4E>(s[r]);
-            s[r] += dpp_f64<0x141>(s[r]);
-            s[r] += dpp_f64<0x140>(s[r]);
-        }
-        if (jc == 0) {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) red[wave][8 * mc + r] = s[r];
-        }
-        lds_barrier();
-        for (int row = 4 * wave + mc; row < kBlkRows; row += 4 * NW) {             // uniform per wave
-            double t = jc < NW ? red[jc < NW ? jc : 0][row] : 0.0;
-            t += dpp_f64<0xB1>(t);
-            t += dpp_f64<0x4E>(t);
-            t += dpp_f64<0x141>(t);
-            t += dpp_f64<0x140>(t);
-            if (jc == 0)
-                scale[row] = row < rows ? static_cast<float>(1.0 / sqrt(t / K + static_cast<double>(a.eps))) : 0.f;
-        }
-        lds_barrier();
-    };
-    auto squares = [](const uint4 &q, double s) {
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const double x = static_cast<double>(__uint_as_float(w[e] << 16));
-            const double z = static_cast<double>(__uint_as_float(w[e] & 0xffff0000u));
-            s = fma(x, x, s);
-            s = fma(z, z, s);
-        }
-        return s;
-    };
-
-    uint4 v[TPW][8], rq[4];                        // rq: four rows of the stream at a time
-    if (a.y) {
-#pragma unroll
-        for (int t = 0; t < TPW; ++t)
-#pragma unroll
-            for (int r = 0; r < 8; ++r) v[t][r] = load(ys, a.ldy, t, r);
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) rq[r] = load(rs, a.ldr, 0, r);
-    if (a.post) {
-        double s[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            s[r] = 0.0;
-#pragma unroll
-            for (int t = 0; t < TPW; ++t) s[r] = squares(v[t][r], s[r]);
-        }
-        row_scales(s);
-    }
-    // the packed values stay the only copy: else their unpacked forms are kept too
-    auto packed = [](uint4 &q) { asm volatile("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w)); };
-    double s[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) s[r] = 0.0;
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-        const int j = col(t);
-        const uint4 gpost = vec8(a.gpost, j);
-        const uint4 gate = vec8(a.gate ? static_cast<const uint16_t *>(a.gate) + unit * a.gate_unit : nullptr, j);
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            float h[8], x[8], g[8];
-            unpack(Raw8<uint16_t>{{rq[r % 4]}}, x);
-            if (a.y) {
-                packed(v[t][r]);
-                unpack(Raw8<uint16_t>{{v[t][r]}}, h);
-                if (a.post) {
-                    const float sc = scale[8 * mc + r];
-                    unpack(Raw8<uint16_t>{{gpost}}, g);          // a gain of 1 changes nothing
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[e] = h[e] * sc * g[e];
-                }
-                if (a.gate) {
-                    unpack(Raw8<uint16_t>{{gate}}, g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[e] = h[e] * g[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = a.r ? a.rs * x[e] + h[e] : h[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = a.rs * x[e];
-            }
-            v[t][r] = make_uint4(pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3]), pack_bf16x2(h[4], h[5]),
-                                 pack_bf16x2(h[6], h[7]));
-            packed(v[t][r]);
-            s[r] = squares(j < K ? v[t][r] : make_uint4(0, 0, 0, 0), s[r]);
-            if (r == 3) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) rq[q] = load(rs, a.ldr, t, 4 + q);
-            }
-            if (r == 7 && t + 1 < TPW) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) rq[q] = load(rs, a.ldr, t + 1, q);
-            }
-        }
-    }
-    row_scales(s);
-    uint16_t *xt = Xt + unit * static_cast<int64_t>(K) * ldxt + m0 + 8 * mc;
-    double *o = out + (unit * nblk + blk) * static_cast<int64_t>(K);
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-        const int j = col(t);
-        if ((wave + NW * t) * kBlkCols >= K) break;                             // uniform per wave
-        const bool live = j < K;
-        float g[8];
-        unpack(Raw8<uint16_t>{{vec8(a.gpre, j)}}, g);
-        double acc[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.0;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            // not before: a load issued after a store would be waited for with it
-            if (live && 8 * mc + r < rows)
-                *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.h) + (row0 + 8 * mc + r) * a.ldh + j) = v[t][r];
-            const float sc = scale[8 * mc + r];
-            uint32_t w[4] = {v[t][r].x, v[t][r].y, v[t][r].z, v[t][r].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[e] = pack_bf16x2(__uint_as_float(w[e] << 16) * sc * g[2 * e],
-                                   __uint_as_float(w[e] & 0xffff0000u) * sc * g[2 * e + 1]);
-                const double ya = static_cast<double>(__uint_as_float(w[e] << 16));
-                const double yb = static_cast<double>(__uint_as_float(w[e] & 0xffff0000u));
-                acc[2 * e] = fma(ya, ya, acc[2 * e]);
-                acc[2 * e + 1] = fma(yb, yb, acc[2 * e + 1]);
-            }
-            v[t][r] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            acc[e] += __shfl_xor(acc[e], 16);
-            acc[e] += __shfl_xor(acc[e], 32);
-        }
-        if (mc == 0 && live) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[j + e] = acc[e];
-        }
-        if (!live) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-            uint32_t ow[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                ow[q] = __builtin_amdgcn_perm((&v[t][2 * q + 1].x)[e >> 1], (&v[t][2 * q].x)[e >> 1], sel);
-            uint16_t *dst = xt + static_cast<int64_t>(j + e) * ldxt;
-            if (8 * mc + 8 <= rows) {
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    if (8 * mc + r < rows) dst[r] = static_cast<uint16_t>(ow[r >> 1] >> (16 * (r & 1)));
-            }
-        }
-    }
-}
-
 // TAIL: K % 8 != 0
 template <typename TY, typename TS, bool TAIL>
 hipError_t launch_rows(const JoinArgs &a, hipStream_t stream) {
@@ -538,37 +328,6 @@ hipError_t launch_join_rows(const JoinArgs &a, bool y_bf16, bool stream_bf16, hi
 int64_t join_splits(int64_t B, int64_t M, int64_t K) {
     const int64_t rps = rows_per_split(B, M, K);
     return (M + rps - 1) / rps;
-}
-
-int64_t join_blocks(int64_t M) { return (M + kBlkRows - 1) / kBlkRows; }
-
-bool join_block_ok(const JoinArgs &a, bool y_bf16, bool stream_bf16, bool vec) {
-    // One pass is the faster from about 4096 rows on (rows x K, one pass / rows kernel
-    // and K-major kernel, us: 8192 x 4096 70 / 77, 4096 x 4096 41 / 44, 2048 x 4096 35 / 27,
-    // 8192 x 2048 38 / 44, 8192 x 1024 23 / 27, 8192 x 512 21 / 21): a workgroup takes 31 us
-    // for 32 rows of 4096, mostly of float64 arithmetic, however few there are.
-    const int64_t lim = int64_t(1) << 31, held = a.rows / a.M * join_blocks(a.M) * kBlkRows;
-    if (a.rows < 4096 || a.K <= 512 || held > a.rows / 4 * 5) return false;
-    return y_bf16 && stream_bf16 && vec && a.K <= kBlkTiles * kBlkMaxWaves * kBlkCols && a.gate_row == 0 &&
-           kBlkRows * a.ldy * 2 < lim && kBlkRows * a.ldr * 2 < lim;
-}
-
-hipError_t launch_join_block(const JoinArgs &a, uint16_t *Xt, int64_t ldxt, double *partials, double *energy,
-                             hipStream_t stream) {
-    const int64_t B = a.rows / a.M, n = join_blocks(a.M);
-    double *out = n == 1 ? energy : partials;
-    const dim3 grid(static_cast<unsigned>(n), static_cast<unsigned>(B));
-    auto go = [&](auto kernel, int waves) {
-        hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a, Xt, ldxt, out);
-    };
-    constexpr int wide = kBlkTiles * kBlkCols;               // columns per wave
-    if (a.K <= 2 * wide) go(join_block_kernel<2>, 2);
-    else if (a.K <= 4 * wide) go(join_block_kernel<4>, 4);
-    else if (a.K <= 8 * wide) go(join_block_kernel<8>, 8);
-    else go(join_block_kernel<16>, 16);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || n == 1) return e;
-    return launch_score_finalize_grouped(partials, B, n, a.K, energy, stream);
 }
 
 hipError_t launch_join_kmajor(const void *H, bool stream_bf16, int64_t ldh, const float *rscale, const uint16_t *gpre,

@@ -119,7 +119,7 @@ def test_parts(K):
 
 @pytest.mark.parametrize("parts", ["all", "no Y", "no R", "no gains", "in place", "strided", "channel gate", "eps 0"])
 def test_many_rows(parts):
-    """The one-pass form's inputs left out in turn, against the row-major outputs."""
+    """Inputs left out in turn at many rows, against the row-major outputs."""
     dev = require_gpu()
     B, M, K = 2, 2100, 1032
     Y, R, gp, gq, gt = make(dev, BF, BF, B, M, K, "channel", seed=8)
