@@ -206,8 +206,11 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
 // The K-major half: a wave takes 64 columns of a run of rows, 64 at a time.  Lane
 // 8 mc + jc holds rows 8 mc .. + 7 and columns 8 jc .. + 7 of each 64 x 64 tile,
 // transposes its 8 x 8 block in registers and writes 16 bytes (8 tokens) of each
-// of 8 Xt rows, so that the 8 lanes of one jc fill a whole 128-byte line.
-template <typename TS>
+// of 8 Xt rows, so that the 8 lanes of one jc fill 128 bytes.  LINES: these are
+// whole lines; they go past the caches, which then still hold the stream (8192 x
+// 4096, both launches: 74 us without, 66 so; where lines are shared by two tiles,
+// 2002 x 8192, 41 and 47).
+template <typename TS, bool LINES>
 __global__ __launch_bounds__(256) void join_kmajor_kernel(
     const TS *__restrict__ H, int64_t ldh, const float *__restrict__ rscale, const uint16_t *__restrict__ gpre,
     int64_t M, int K, int64_t rps, uint16_t *__restrict__ Xt, int64_t ldxt, double *__restrict__ out) {
@@ -260,7 +263,10 @@ __global__ __launch_bounds__(256) void join_kmajor_kernel(
             for (int q = 0; q < 4; ++q) o[q] = __builtin_amdgcn_perm(w[2 * q + 1][e >> 1], w[2 * q][e >> 1], sel);
             uint16_t *dst = Xt + (unit * K + j + e) * ldxt + m0;
             if (n == 8) {
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+                typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+                const u32x4 v = {o[0], o[1], o[2], o[3]};
+                if (LINES) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(dst));
+                else *reinterpret_cast<u32x4 *>(dst) = v;
             } else {
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
@@ -336,12 +342,16 @@ hipError_t launch_join_kmajor(const void *H, bool stream_bf16, int64_t ldh, cons
     const int64_t rps = rows_per_split(B, M, K), S = join_splits(B, M, K);
     const dim3 grid(static_cast<unsigned>((K + 255) / 256), static_cast<unsigned>(S), static_cast<unsigned>(B));
     double *out = S == 1 ? energy : partials;
-    if (stream_bf16)
-        hipLaunchKernelGGL(join_kmajor_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(H),
-                           ldh, rscale, gpre, M, static_cast<int>(K), rps, Xt, ldxt, out);
+    auto go = [&](auto kernel, const auto *h) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, h, ldh, rscale, gpre, M, static_cast<int>(K), rps, Xt, ldxt,
+                           out);
+    };
+    const uint16_t *hb = static_cast<const uint16_t *>(H);
+    const float *hf = static_cast<const float *>(H);
+    if (ldxt % kJoinRows == 0 && reinterpret_cast<uintptr_t>(Xt) % 128 == 0)
+        stream_bf16 ? go(join_kmajor_kernel<uint16_t, true>, hb) : go(join_kmajor_kernel<float, true>, hf);
     else
-        hipLaunchKernelGGL(join_kmajor_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(H), ldh,
-                           rscale, gpre, M, static_cast<int>(K), rps, Xt, ldxt, out);
+        stream_bf16 ? go(join_kmajor_kernel<uint16_t, false>, hb) : go(join_kmajor_kernel<float, false>, hf);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || S == 1) return e;
     return launch_score_finalize_grouped(partials, B, S, K, energy, stream);
