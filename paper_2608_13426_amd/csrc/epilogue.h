@@ -21,7 +21,7 @@ constexpr int kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kActGeluTa
 // T: the output's type.  Where it is bf16 the forms below err by at most 2^-16 |x|
 // (a 128th of what the rounding may), in as few operations as that takes: they run
 // on every output of a tile while its matrix cores wait (8192 x 14336 outputs of
-// 2048 retained indices, gelu: 447 us with erff, 416 so).
+// 2048 retained indices: 406 us as a plain product, 428 with bias and silu).
 template <int ACT, class T>
 __device__ __forceinline__ float activate(float x) {
     constexpr bool kFast = sizeof(T) == 2;
@@ -111,26 +111,33 @@ __device__ __forceinline__ u32x4_t ep_load8(const uint16_t *p, int n) {
     return q;
 }
 
-// The epilogue of a K-major kernel's tile of BN columns: acc[j][i][4*gq + r] is row
-// wm*TM + 32i + lane%32 and column wn*32*FN + 32j + 8gq + 4*(lane/32) + r of it, for
-// waves 2 x NW/2.  The fp32 accumulators go through LDS (the idle ring) 64 rows at
-// a time, row r of a pass at obj(r): 16-byte chunk cc (4 columns) at (cc/2) ^ (r %
-// 16) of the row's first or second half as cc is even or odd, so that both the
-// fragments' writes and the rows' reads fall on distinct banks.  A thread then
-// holds 8 neighbouring columns of a row: bias and residual come in 16 bytes a
-// lane, one rounding, 16 bytes out.  No access needs alignment; only the chunk that
-// N cuts goes element by element.  (Residual added on the fragments, 8 bytes a lane in 32 rows, and
-// outputs staged as bf16: 420 us for 8192 x 4096 of 7168 retained indices;
-// so: 395.  With rows off 16-byte boundaries, 2 x 1001 x 4097 of 610: 111, 26.)
+// Where a pass's fp32 sum of row r and column n (of BN) lies in row r's LDS: 16-byte
+// chunk cc = n / 4 at (cc / 2) ^ (r % 16) of the row's first or second half as cc is
+// even or odd, so that both the fragments' writes and the rows' reads fall on
+// distinct banks.
+template <int BN>
+constexpr int ep_swizzle = BN / 8 < 16 ? BN / 8 - 1 : 15;
+template <int BN>
+__device__ __forceinline__ char *ep_at(char *row, int r, int n) {
+    const int cc = n >> 2;
+    return row + 16 * (((cc >> 1) ^ (r & ep_swizzle<BN>)) + BN / 8 * (cc & 1)) + 4 * (n & 3);
+}
+
+// The epilogue of a tile of BN columns held as fp32 sums by NW waves, 2 x NW/2 of
+// them, each TM rows of its own columns.  The sums go through LDS 64 rows at a time:
+// put(p) writes, for rows r = 32 wm .. + 31 of pass p (tile rows wm * TM + 32 p ..),
+// the wave's columns to ep_at(obj(r), r, n).  A thread then holds 8 neighbouring
+// columns of a row: bias and residual come in 16 bytes a lane, one rounding, 16
+// bytes out.  No access needs alignment; only the chunk that N cuts goes element by
+// element.  (Residual added on the fragments, 8 bytes a lane in 32 rows, and outputs
+// staged as bf16: 420 us for 8192 x 4096 of 7168 retained indices; so: 404.  With
+// rows off 16-byte boundaries, 2 x 1001 x 4097 of 610, the same tiles: 111, 35.)
 // Every wave's reads of the ring and loads into it have ended before the call.
 // left: rows from the tile's origin on; row0: the origin's row over all units.
-template <int BN, int NW, int FN, int FM, int TM, class Obj>
-__device__ __forceinline__ void ep_tile(const Epilogue &ep, const f32x16_t (&acc)[FN][FM], Obj obj, int wave, int lane,
-                                        uint16_t *__restrict__ Y, int64_t ldy, bool aligned16, int n0, int N, int left,
-                                        int64_t row0) {
-    constexpr int SW = BN / 8 < 16 ? BN / 8 - 1 : 15;
+template <int BN, int NW, int PASSES, int TM, class Put, class Obj>
+__device__ __forceinline__ void ep_tile(const Epilogue &ep, Put put, Obj obj, int wave, int lane, uint16_t *__restrict__ Y,
+                                        int64_t ldy, bool aligned16, int n0, int N, int left, int64_t row0) {
     constexpr int LPR = BN / 8, RPI = 64 / LPR, Q = 64 / (NW * RPI);     // lanes per row, rows per step
-    const int lr = lane & 31, lh = lane >> 5, wm = wave / (NW / 2), wn = wave % (NW / 2);
     const int c = lane % LPR, nc = N - n0 - 8 * c;
     auto tile_row = [&](int r, int p) { return (r / 32) * TM + 32 * p + r % 32; };
     auto step_row = [&](int q) { return RPI * (NW * q + wave) + lane / LPR; };
@@ -152,28 +159,18 @@ __device__ __forceinline__ void ep_tile(const Epilogue &ep, const f32x16_t (&acc
     fetch(0);
     lds_barrier();
 #pragma unroll
-    for (int p = 0; p < FM; ++p) {
-        {
-            const int r = 32 * wm + lr;
-            char *o = obj(r);
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int gq = 0; gq < 4; ++gq)
-                    *reinterpret_cast<f32x4_t *>(o + 16 * (((4 * (FN * wn + j) + gq) ^ (r & SW)) + BN / 8 * lh)) =
-                        f32x4_t{acc[j][p][4 * gq], acc[j][p][4 * gq + 1], acc[j][p][4 * gq + 2], acc[j][p][4 * gq + 3]};
-        }
+    for (int p = 0; p < PASSES; ++p) {
+        put(p);
         lds_barrier();
         u32x4_t now[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) now[q] = res[q];
-        if (p + 1 < FM) fetch(p + 1);
+        if (p + 1 < PASSES) fetch(p + 1);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int r = step_row(q), ml = tile_row(r, p);
-            const char *o = obj(r) + 16 * (c ^ (r & SW));
-            const f32x4_t lo = *reinterpret_cast<const f32x4_t *>(o);
-            const f32x4_t hi = *reinterpret_cast<const f32x4_t *>(o + BN * 2);
+            const f32x4_t lo = *reinterpret_cast<const f32x4_t *>(ep_at<BN>(obj(r), r, 8 * c));
+            const f32x4_t hi = *reinterpret_cast<const f32x4_t *>(ep_at<BN>(obj(r), r, 8 * c + 4));
             float v[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) { v[e] = lo[e] + bias[e]; v[4 + e] = hi[e] + bias[4 + e]; }
@@ -201,7 +198,35 @@ __device__ __forceinline__ void ep_tile(const Epilogue &ep, const f32x16_t (&acc
                     if (e < nc) d[e] = static_cast<uint16_t>(out[e >> 1] >> (16 * (e & 1)));
             }
         }
-        if (p + 1 < FM) lds_barrier();        // the next pass overwrites the staged rows
+        if (p + 1 < PASSES) lds_barrier();        // the next pass overwrites the staged rows
+    }
+}
+
+// put() of the K-major kernels, whose fragments are transposed: acc[j][i][4*gq + r] is
+// row wm*TM + 32i + lane%32 and column wn*32*FN + 32j + 8gq + 4*(lane/32) + r.
+template <int BN, int NW, int FN, int FM, class Obj>
+__device__ __forceinline__ void ep_put_rows(const f32x16_t (&acc)[FN][FM], int p, Obj obj, int wave, int lane) {
+    const int wm = wave / (NW / 2), wn = wave % (NW / 2), r = 32 * wm + (lane & 31);
+    char *o = obj(r);
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq)
+            *reinterpret_cast<f32x4_t *>(ep_at<BN>(o, r, 32 * (FN * wn + j) + 8 * gq + 4 * (lane >> 5))) =
+                f32x4_t{acc[j][p][4 * gq], acc[j][p][4 * gq + 1], acc[j][p][4 * gq + 2], acc[j][p][4 * gq + 3]};
+}
+
+// and of the row-major ones: acc[i][j][v] is row wm*TM + 32i + 8*(v/4) + 4*(lane/32) +
+// v%4 and column wn*32*FN + 32j + lane%32.
+template <int BN, int NW, int FM, int FN, class Obj>
+__device__ __forceinline__ void ep_put_columns(const f32x16_t (&acc)[FM][FN], int p, Obj obj, int wave, int lane) {
+    const int wm = wave / (NW / 2), wn = wave % (NW / 2);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int r = 32 * wm + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            *reinterpret_cast<float *>(ep_at<BN>(obj(r), r, 32 * (FN * wn + j) + (lane & 31))) = acc[p][j][v];
     }
 }
 

@@ -28,7 +28,7 @@ template <int BM, int BN, int BK, int WM, int WN, bool VECW, bool EP = false>
 __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W,
     const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
-    int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}) {
+    int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}, bool vec_y = false) {
     constexpr int NT = WM * WN * kWave;
     constexpr int TM = BM / WM, TN = BN / WN;        // per-wave tile
     constexpr int FM = TM / 32, FN = TN / 32;        // 32x32 fragments per wave
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
     const int m0 = blockIdx.y * BM, n0 = blockIdx.x * BN;
     const int64_t unit = blockIdx.z;
     X += unit * static_cast<int64_t>(M) * ldx;
-    Y += unit * static_cast<int64_t>(M) * ldy;
+    if constexpr (!EP) Y += unit * static_cast<int64_t>(M) * ldy;
     idx += unit * k;
 
     const int a_t = tid % BK;                 // retained position within the tile
@@ -134,6 +134,14 @@ __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
     }
 
     // C fragment: lane holds column lr, rows 8*(v/4) + 4*(lane/32) + v%4
+    if constexpr (EP) {
+        static_assert(WM == 2, "epilogue layout");
+        __shared__ __attribute__((aligned(16))) float stage[64 * BN];
+        auto obj = [&](int r) -> char * { return reinterpret_cast<char *>(stage + r * BN); };
+        ep_tile<BN, WM * WN, FM, TM>(ep, [&](int p) { ep_put_columns<BN, WM * WN>(acc, p, obj, wave, lane); }, obj, wave,
+                                     lane, Y, ldy, vec_y, n0, N, min(BM, M - m0), unit * M + m0);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -142,11 +150,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int m = m0 + wm * TM + i * 32 + 8 * (v / 4) + 4 * (lane / 32) + (v % 4);
-                if (m < M && n < N) {
-                    float y = acc[i][j][v];
-                    if constexpr (EP) y = ep_value<uint16_t>(ep, y, unit * M + m, n);
-                    Y[static_cast<int64_t>(m) * ldy + n] = f32_to_bf16(y);
-                }
+                if (m < M && n < N) Y[static_cast<int64_t>(m) * ldy + n] = f32_to_bf16(acc[i][j][v]);
             }
         }
 }
@@ -165,11 +169,12 @@ __device__ __forceinline__ int swz(int row) { return (row ^ (row >> 3)) & 7; }
 __device__ __forceinline__ int at(int row, int chunk) { return row * BK + ((chunk ^ swz(row)) << 3); }
 }  // namespace big
 
-template <int NW>
+template <int NW, bool EP = false>
 __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_gather_bf16_big_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W,
     const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
-    int64_t ldx, int64_t ldw, int64_t ldy, int64_t w_bytes, int tiles_m, int tiles_n) {
+    int64_t ldx, int64_t ldw, int64_t ldy, int64_t w_bytes, int tiles_m, int tiles_n, Epilogue ep = {},
+    bool vec_y = false) {
     using namespace big;
     constexpr int NT = NW * 64;
     constexpr int WN = NW / 2;            // waves along N (2 along M)
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_gather_bf16_big_kernel(
     const int n0 = ((lin % gsz) / gm) * BN;
     const int64_t unit = blockIdx.y;
     X += unit * static_cast<int64_t>(M) * ldx;
-    Y += unit * static_cast<int64_t>(M) * ldy;
+    if constexpr (!EP) Y += unit * static_cast<int64_t>(M) * ldy;
     idx += unit * k;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -324,6 +329,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_gather_bf16_big_kernel(
         __syncthreads();
     }
 
+    if constexpr (EP) {
+        auto obj = [&](int r) -> char * { return reinterpret_cast<char *>(lds) + r * (BN * 4); };
+        ep_tile<BN, NW, 4, 128>(ep, [&](int q) { ep_put_columns<BN, NW>(acc, q, obj, wave, lane); }, obj, wave, lane, Y,
+                                ldy, vec_y, n0, N, min(BM, M - m0), unit * M + m0);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -752,8 +763,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
             const int q = r / RPO;
             return (q == 0 ? sA0 : q == 1 ? sA1 : q == 2 ? sB0 : sB1) + (r % RPO) * (BNT * 4);
         };
-        ep_tile<BNT, NW, FN, FM, 128>(ep, acc, obj, wave, lane, Y, ldy, vec_y == 2, n0, N, min(BT, M - m0),
-                                      unit * static_cast<int64_t>(M) + m0);
+        ep_tile<BNT, NW, FM, 128>(ep, [&](int p) { ep_put_rows<BNT, NW>(acc, p, obj, wave, lane); }, obj, wave, lane, Y,
+                                  ldy, vec_y == 2, n0, N, min(BT, M - m0), unit * static_cast<int64_t>(M) + m0);
         return;
     }
     uint16_t *Yu = Y + unit * static_cast<int64_t>(M) * ldy;
@@ -877,9 +888,12 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) wj[i] = w_on && t0 + wk + i < k ? idx[t0 + wk + i] : -1;
     };
-    float xv[XR];
-    f32x4_t wv[4];
-    auto gather = [&]() {
+    constexpr int SETS = EP ? 2 : 1;                 // tiles on their way in registers
+    float xset[SETS][XR];
+    f32x4_t wset[SETS][4];
+    auto gather = [&](auto set) {
+        float(&xv)[XR] = xset[decltype(set)::value];
+        f32x4_t(&wv)[4] = wset[decltype(set)::value];
 #pragma unroll
         for (int i = 0; i < XR; ++i) {
             const int m = min(m0 + xr0 + i * RPP, M - 1);
@@ -899,7 +913,9 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
             }
         }
     };
-    auto stash = [&](int buf) {
+    auto stash = [&](auto set, int buf) {
+        const float(&xv)[XR] = xset[decltype(set)::value];
+        const f32x4_t(&wv)[4] = wset[decltype(set)::value];
 #pragma unroll
         for (int i = 0; i < XR; ++i) As[buf][(xr0 + i * RPP) * LS + xt] = xv[i];
         if (w_on) {
@@ -916,16 +932,9 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
         for (int i = 0; i < FM; ++i) acc[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const int lr = lane & 15, lg = lane >> 4;
     const int wm = (wave >> 1) * (BM / 2), wnb = (wave & 1) * (BN / 2);
-    fetch_idx(0);
-    gather();
-    fetch_idx(BK);
-    stash(0);
-    __syncthreads();
-    for (int t0 = 0, buf = 0; t0 < k; t0 += BK, buf ^= 1) {
-        if (t0 + BK < k) {
-            gather();
-            fetch_idx(t0 + 2 * BK);
-        }
+    using Set0 = std::integral_constant<int, 0>;
+    using Set1 = std::integral_constant<int, SETS - 1>;
+    auto multiply = [&](int buf) {
 #pragma unroll
         for (int ks = 0; ks < BK; ks += 16) {
             f32x4_t a[FM], b[FN];
@@ -944,8 +953,43 @@ __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
                         acc[j][i] = VECY ? __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[j][i], 0, 0, 0)
                                          : __builtin_amdgcn_mfma_f32_16x16x4f32(a[i][e], b[j][e], acc[j][i], 0, 0, 0);
         }
-        if (t0 + BK < k) stash(buf ^ 1);
+    };
+    fetch_idx(0);
+    gather(Set0{});
+    fetch_idx(BK);
+    stash(Set0{}, 0);
+    if constexpr (EP) {
+        // two tiles ahead: a tile's values have two steps to arrive (1031 x 2048 -> 4096, k
+        // = 1024: 156 us one ahead, 141 so; 517 x 1024 -> 771, k = 512: 17 us both)
+        gather(Set1{});
+        fetch_idx(2 * BK);
+        gather(Set0{});
+        fetch_idx(3 * BK);
         __syncthreads();
+        auto step = [&](auto set, int t0, int buf) {
+            multiply(buf);
+            if (t0 + BK < k) stash(set, buf ^ 1);
+            if (t0 + 3 * BK < k) {
+                gather(set);
+                fetch_idx(t0 + 4 * BK);
+            }
+            lds_barrier();                           // does not wait for the loads on their way
+        };
+        for (int t0 = 0; t0 < k; t0 += 2 * BK) {
+            step(Set1{}, t0, 0);
+            if (t0 + BK < k) step(Set0{}, t0 + BK, 1);
+        }
+    } else {
+        __syncthreads();
+        for (int t0 = 0, buf = 0; t0 < k; t0 += BK, buf ^= 1) {
+            if (t0 + BK < k) {
+                gather(Set0{});
+                fetch_idx(t0 + 2 * BK);
+            }
+            multiply(buf);
+            if (t0 + BK < k) stash(Set0{}, buf ^ 1);
+            __syncthreads();
+        }
     }
     // VECY: acc[j][i][r] is n = n0 + wnb + 16j + 4*(lane/16) + r, m = m0 + wm + 16i +
     // lane%16; else m = m0 + wm + 16i + 4*(lane/16) + r, n = n0 + wnb + 16j + lane%16
@@ -1005,10 +1049,17 @@ hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t 
     const int64_t w_bytes = K * ldw * 2;
     const bool offsets_fit = static_cast<int64_t>(big::BM + 1) * ldx * 2 < (int64_t(1) << 31) &&
                              w_bytes + ldw * 2 < (int64_t(1) << 31);
-    if (vec && offsets_fit && big_tiles * B >= 128 && !ep) {
+    const bool vec_y = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0;
+    if (vec && offsets_fit && big_tiles * B >= 128) {
         const int tm = static_cast<int>((M + big::BM - 1) / big::BM);
         const int tn = static_cast<int>((N + big::BN - 1) / big::BN);
         dim3 grid(static_cast<unsigned>(tm * tn), static_cast<unsigned>(B));
+        if (ep) {
+            hipLaunchKernelGGL((gemm_gather_bf16_big_kernel<kBigWaves, true>), grid, dim3(kBigWaves * 64), 0,
+                               stream, X, W, idx, Y, static_cast<int>(M), static_cast<int>(N),
+                               static_cast<int>(k), ldx, ldw, ldy, w_bytes, tm, tn, *ep, vec_y);
+            return hipGetLastError();
+        }
         hipLaunchKernelGGL(gemm_gather_bf16_big_kernel<kBigWaves>, grid, dim3(kBigWaves * 64), 0,
                            stream, X, W, idx, Y, static_cast<int>(M), static_cast<int>(N),
                            static_cast<int>(k), ldx, ldw, ldy, w_bytes, tm, tn);
@@ -1020,7 +1071,8 @@ hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t 
     if (ep) {
         auto launch = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, grid, dim3(WM * WN * kWave), 0, stream, X, W, idx, Y,
-                               static_cast<int>(M), static_cast<int>(N), static_cast<int>(k), ldx, ldw, ldy, *ep);
+                               static_cast<int>(M), static_cast<int>(N), static_cast<int>(k), ldx, ldw, ldy, *ep,
+                               vec_y);
             return hipGetLastError();
         };
         return vec ? launch(gemm_gather_bf16_kernel<BM, BN, BK, WM, WN, true, true>)

@@ -279,8 +279,8 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kerne
             const int q = r / RPO;
             return (q == 0 ? sA0 : q == 1 ? sA1 : q == 2 ? sA2 : sA3) + (r % RPO) * (BN * 4);
         };
-        ep_tile<BN, NW, FN, FM, TM>(ep, acc, at, wave, lane, Y, ldy, vec_y == 2, n0, N, rows,
-                                    static_cast<int64_t>(unit) * M + m0);
+        ep_tile<BN, NW, FM, TM>(ep, [&](int p) { ep_put_rows<BN, NW>(acc, p, at, wave, lane); }, at, wave, lane, Y, ldy,
+                                vec_y == 2, n0, N, rows, static_cast<int64_t>(unit) * M + m0);
         return;
     }
     if constexpr (BM == 64) {

@@ -68,7 +68,7 @@ def test_few_rows(B, M, N, K, k, act):
 
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("B,M,N,K,k", [(1, 37, 131, 100, 51), (2, 300, 513, 64, 64), (3, 1, 5, 7, 3), (1, 600, 2100, 200, 17),
-                                       (1, 4000, 4000, 64, 40)])
+                                       (1, 4000, 4000, 64, 40), (2, 3000, 2100, 96, 70)])
 def test_row_major(dt, B, M, N, K, k):
     dev = require_gpu()
     X, W, idx, b, R = make(dev, dt, B, M, N, K, k, seed=2)
