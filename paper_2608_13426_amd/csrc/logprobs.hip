@@ -459,7 +459,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     }
 
     __shared__ Part parts[kWaves];
-    const double r = sums.rest(a.c), f = 1.0 - kLn2 * r;         // 2^-r: r is below 1e-6 of the base
+    const double r = sums.rest(a.c), f = 1.0 - kLn2 * r;         // 2^-r: r is at most 2^-12
     const double S0 = wave_sum(sums.s), S = f * S0, D = f * (wave_sum(sums.d) - r * S0);
     if (lane == 0) parts[wave] = {S, D, sums.b, sums.set || S != S};
     const uint64_t key = a.top > 0 ? join_lists(list.key, a.top) : 0;
