@@ -71,29 +71,45 @@ __device__ __forceinline__ uint64_t key_before(uint64_t k) {
 #endif
 }
 
+// LDS accesses of a wave's lanes stay in this order (the hardware keeps a wave's LDS
+// accesses in program order)
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A wave's `top` largest keys, descending over its lanes.
 struct TopList {
     uint64_t key;                        // this lane's
     uint64_t last;                       // the top-th, 0 while there are fewer
     float lim;                           // its logit: only what is above can enter
     int top;
-    __device__ void init(int n) { key = 0; last = 0; lim = -__builtin_inff(); top = n; }
+    uint64_t *scratch;                   // 64 keys of LDS, this wave's alone, 16-byte aligned
+    __device__ void init(int n, uint64_t *lds) { key = 0; last = 0; lim = -__builtin_inff(); top = n; scratch = lds; }
     __device__ bool full() const { return last != 0; }
     __device__ void bound() {
         last = lane_key(key, top - 1);
         lim = last ? key_logit(last) : -__builtin_inff();
     }
     // every lane offers one key (0: none) to an empty list: each goes to the lane
-    // that as many keys are larger
+    // that as many keys are larger.  Two keys per LDS read that all lanes share (1000
+    // cycles; one by one from the other lanes' registers 3300)
     __device__ void fill(uint64_t cand) {
+        const int lane = threadIdx.x & 63;
+        scratch[lane] = cand;
+        wave_lds_order();
         int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < 64; ++i) rank += lane_key(cand, i) > cand;
-        if (cand == 0) rank = 63;                          // ends behind every key, as 0
-        const uint64_t none = __ballot(cand == 0);
-        const uint32_t lo = __builtin_amdgcn_ds_permute(4 * rank, static_cast<int>(cand));
-        const uint32_t hi = __builtin_amdgcn_ds_permute(4 * rank, static_cast<int>(cand >> 32));
-        key = (threadIdx.x & 63) < 64 - __popcll(none) ? (static_cast<uint64_t>(hi) << 32) | lo : 0;
+#pragma unroll 16
+        for (int i = 0; i < 64; i += 2) {
+            const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(scratch + i);
+            rank += k.x > cand;
+            rank += k.y > cand;
+        }
+        const int held = 64 - __popcll(__ballot(cand == 0));
+        wave_lds_order();
+        if (cand != 0) scratch[rank] = cand;
+        wave_lds_order();
+        key = lane < held ? scratch[lane] : 0;
         bound();
     }
     // every lane offers one key (0: none)
@@ -114,6 +130,38 @@ struct TopList {
         lim = last ? key_logit(last) : -__builtin_inff();
     }
 };
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __uint_as_float(static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(x)), CTRL, 0xF, 0xF, false)));
+#else
+    return x;
+#endif
+}
+__device__ __forceinline__ float lane_f32(float v, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+// over the wave, the same in every lane: lane ^ 1, lane ^ 2, mirrors of 8 and 16
+// lanes, then the four rows of 16
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, dpp_f32<0xB1>(v));
+    v = fmaxf(v, dpp_f32<0x4E>(v));
+    v = fmaxf(v, dpp_f32<0x141>(v));
+    v = fmaxf(v, dpp_f32<0x140>(v));
+    return fmaxf(fmaxf(lane_f32(v, 0), lane_f32(v, 16)), fmaxf(lane_f32(v, 32), lane_f32(v, 48)));
+}
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+    return __longlong_as_double(static_cast<long long>(lane_key(static_cast<uint64_t>(__double_as_longlong(v)), lane)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v += dpp_f64<0xB1>(v);
+    v += dpp_f64<0x4E>(v);
+    v += dpp_f64<0x141>(v);
+    v += dpp_f64<0x140>(v);
+    return (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
+}
 
 // A wave's softmax sums of the logits it has seen: the base shared, s and d per
 // lane.  As long as it can, t = fma(z, c, -base) with base = b c rounded to fp32
@@ -138,9 +186,7 @@ struct Sums {
     }
     // moves b to the largest of the lanes' values
     __device__ void rebase(float cm, float c) {
-#pragma unroll
-        for (int sh = 1; sh < 64; sh <<= 1) cm = fmaxf(cm, __shfl_xor(cm, sh));
-        cm = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(cm)));
+        cm = wave_max(cm);
         const float nb = cm * c;
         if (!careful && !(fabsf(nb) < 4096.f)) take_care(c);
         if (set) {
@@ -175,16 +221,6 @@ __device__ __forceinline__ float below(float x) {
     return __uint_as_float(static_cast<uint32_t>(u > 0 ? u - 1 : u + 1));
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-    v += dpp_f64<0xB1>(v);               // lane ^ 1, lane ^ 2, then mirrors of 8 and 16 lanes
-    v += dpp_f64<0x4E>(v);
-    v += dpp_f64<0x141>(v);
-    v += dpp_f64<0x140>(v);
-    v += __shfl_xor(v, 16);
-    v += __shfl_xor(v, 32);
-    return v;
-}
-
 // 2^delta for the weight of one base against another (delta <= 0): fp32, whose
 // relative error 2^-24 |delta| meets a weight of 2^delta
 __device__ __forceinline__ double base_weight(float b, float to, float c) {
@@ -194,9 +230,7 @@ __device__ __forceinline__ double base_weight(float b, float to, float c) {
 // The sums of n parts (n <= 64: lane i of every wave holds part i): the same in
 // every lane.
 __device__ __forceinline__ Part join_parts(Part mine, float c) {
-    float b = mine.set ? mine.b : -__builtin_inff();
-#pragma unroll
-    for (int sh = 1; sh < 64; sh <<= 1) b = fmaxf(b, __shfl_xor(b, sh));
+    const float b = wave_max(mine.set ? mine.b : -__builtin_inff());
     Part r = {0.0, 0.0, b, __ballot(mine.set) != 0};
     // a NaN base (of a part whose only logits are NaN) leaves S one
     const double f = mine.set ? base_weight(mine.b, b, c) : 0.0;
@@ -237,7 +271,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs &a, int64_t row, con
 
 // The workgroup's four lists as one: key i of the result in thread i < top.
 __device__ __forceinline__ uint64_t join_lists(uint64_t key, int top) {
-    __shared__ uint64_t lists[kWaves][kMaxTop], out[kMaxTop];
+    __shared__ __attribute__((aligned(16))) uint64_t lists[kWaves][kMaxTop], out[kMaxTop];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (threadIdx.x < kMaxTop) out[threadIdx.x] = 0;
     lists[wave][lane] = lane < top ? key : 0;            // descending
@@ -245,13 +279,24 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t key, int top) {
     if (lane < top && key != 0) {
         // its place: its own, and in each other list how many are larger
         int rank = lane;
+        if (top <= 8) {                                      // by one read of each
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            const uint64_t *l = lists[(wave + w) % kWaves];
-            int n = 0;
+            for (int w = 1; w < kWaves; ++w)
 #pragma unroll
-            for (int step = kMaxTop / 2; step > 0; step /= 2) n += l[n + step - 1] > key ? step : 0;
-            rank += n + (l[n] > key);
+                for (int i = 0; i < 8; i += 2) {
+                    const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(&lists[(wave + w) % kWaves][i]);
+                    rank += k.x > key;
+                    rank += k.y > key;
+                }
+        } else {                                             // by bisection
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) {
+                const uint64_t *l = lists[(wave + w) % kWaves];
+                int n = 0;
+#pragma unroll
+                for (int step = kMaxTop / 2; step > 0; step /= 2) n += l[n + step - 1] > key ? step : 0;
+                rank += n + (l[n] > key);
+            }
         }
         if (rank < top) out[rank] = key;
     }
@@ -294,7 +339,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     Sums sums;
     sums.init();
     TopList list;
-    list.init(a.top > 0 ? a.top : 1);
+    __shared__ __attribute__((aligned(16))) uint64_t scratch[kWaves][64];
+    list.init(a.top > 0 ? a.top : 1, scratch[wave]);
     bool fresh = a.top > 0;
 
     // element e of this lane in chunk ch
@@ -490,8 +536,9 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
     auto read = [&](int i) -> uint64_t { return i + lane < n ? keys[i + lane] : 0; };
     uint64_t k = read(0), next = read(64);
     const Part p = join_parts(lane < a.pieces ? in[lane] : Part{0.0, 0.0, 0.f, 0}, a.c);
+    __shared__ __attribute__((aligned(16))) uint64_t scratch[64];
     TopList list;
-    list.init(a.top > 0 ? a.top : 1);
+    list.init(a.top > 0 ? a.top : 1, scratch);
     if (a.top > 0) {
         list.fill(k);
         for (int i = 64; i < n; i += 64) {
