@@ -147,12 +147,12 @@ __device__ __forceinline__ void gemv_tile(
 // Two to eight rows per unit on the matrix cores: v_mfma_f32_4x4x4_16b_bf16 holds
 // 16 products of 4 rows of X by 4 columns of W over 4 retained indices, a column
 // per lane, so each lane multiplies the columns it has loaded and W passes through
-// no LDS.  A wave takes every fourth group of four retained rows; two groups (8
+// no LDS.  A wave takes every fourth group of four retained rows; four groups (16
 // KiB) are on their way while two are multiplied: 16 byte permutations bring a
 // group's four values of each column together, and 8 (up to 4 rows) or 16
 // products follow, against 4 * (8 + 8 M) operations in the form above.
-// Three units of 5 x 4096 -> 6144, a set of 2048 each: 39 us in that form, 21 so;
-// 8 x 14336 -> 4096, k = 7168: 30 and 19 (4 rows: 18 and 16).
+// Three units of 5 x 4096 -> 6144, a set of 2048 each: 39 us in that form, 20 so (21
+// with two groups on their way); 8 x 14336 -> 4096, k = 7168: 30 and 19 (4 rows: 18 and 16).
 template <int MG, bool EP>
 __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
 #pragma unroll
         for (int m = 0; m < MR; ++m) xv[m] = row_in && m < M ? Xb[m * ldx + j] : uint16_t(0);
         const int groups = (nr + 3) / 4;
-        u32x4 w[2][2][4];
+        u32x4 w[3][2][4];
         auto fetch = [&](int g, u32x4 (&q)[2][4]) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -222,17 +222,22 @@ __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
                 }
             }
         };
-        // groups past the last one load nothing (out of range) and add zeros
-        fetch(wave, w[0]);                     // on its way while X's values arrive
+        // groups past the last one load nothing (out of range) and add zeros; the
+        // first two pairs are on their way while X's values arrive
+        fetch(wave, w[0]);
+        fetch(wave + 2 * NW, w[1]);
 #pragma unroll
         for (int m = 0; m < MR; ++m) xs[m * XS + tid] = xv[m];
         lds_barrier();
-        for (int g = wave; g < groups; g += 4 * NW) {
-            fetch(g + 2 * NW, w[1]);
+        for (int g = wave; g < groups; g += 6 * NW) {
+            fetch(g + 4 * NW, w[2]);
             multiply(g, w[0]);
             if (g + 2 * NW >= groups) break;
-            fetch(g + 4 * NW, w[0]);
+            fetch(g + 6 * NW, w[0]);
             multiply(g + 2 * NW, w[1]);
+            if (g + 4 * NW >= groups) break;
+            fetch(g + 8 * NW, w[1]);
+            multiply(g + 4 * NW, w[2]);
         }
         lds_barrier();                         // staged rows are reused by the next pass
     }

@@ -92,7 +92,7 @@ struct TopList {
         lim = last ? key_logit(last) : -__builtin_inff();
     }
     // every lane offers one key (0: none) to an empty list: each goes to the lane
-    // that as many keys are larger.  Two keys per LDS read that all lanes share (1000
+    // that as many keys are larger.  Two keys per LDS read that all lanes share (1900
     // cycles; one by one from the other lanes' registers 3300)
     __device__ void fill(uint64_t cand) {
         const int lane = threadIdx.x & 63;
