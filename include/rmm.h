@@ -953,7 +953,8 @@ rmm_status_t rmm_reduced_gemv_epilogue(const void *X, const void *W, const int32
  *
  * The norm before the next block is of the stored H.  Mean squares are float64
  * sums, r is rounded to fp32; every other step is one fp32 operation in the order
- * written, and H and X are rounded once, so neither depends on sizes or strides.
+ * written, and H and X are rounded once, so neither depends on how rows are split or
+ * strided, but for a mean square whose root lies within float64 rounding of an fp32 border.
  *
  * dtype       : RMM_BF16 or RMM_F32, of Y, X, the gammas and the gate.
  * stream_dtype: of R and H; RMM_F32 also where dtype is RMM_BF16.

@@ -63,7 +63,7 @@ __device__ __forceinline__ float activate(float x, int act) {
 }
 
 // f(std::integral_constant<int, ACT>) for the call's activation: one uniform
-// branch around a whole pass over the accumulators
+// branch around it
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F f) {
     switch (act) {
@@ -87,11 +87,9 @@ __device__ __forceinline__ float ep_value(const Epilogue &ep, float acc, int64_t
     return acc;
 }
 
-// 16 and 8 bytes at any address (global memory takes them at every alignment)
+// 16 bytes at any address (global memory takes them at every alignment)
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ void ep_unpack(const u32x4_t &q, float (&v)[8]) {
 #pragma unroll

@@ -9,7 +9,8 @@
 //
 // The mean squares are float64 sums, r is rounded to fp32 once, and every other
 // step is one fp32 operation, rounded by itself: x and the energies then do not
-// depend on how a row is split over lanes.  h is rounded to the stream's type
+// depend on how a row is split over lanes (but for an r whose float64 value lies
+// within float64 rounding of an fp32 border: one row in 10^7 or so).  h is rounded to the stream's type
 // before its norm, which is of the stored stream, and x once, to its type.
 #include <type_traits>
 
@@ -144,9 +145,7 @@ __global__ __launch_bounds__(NT) void join_rows_kernel(JoinArgs a) {
     float h[C][8];
     if (y) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            unpack(yq[c], h[c]);
-        }
+        for (int c = 0; c < C; ++c) unpack(yq[c], h[c]);
         if (a.post) {
             const float ry = inv_rms(h, 0);
 #pragma unroll
