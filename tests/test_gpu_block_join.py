@@ -236,3 +236,27 @@ def test_repeats_are_bit_identical_on_streams_with_own_workspaces():
     for o in outs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
     assert np.isfinite(outs[0][2].cpu().numpy()).all()
+
+
+def test_past_32_bit_offsets():
+    """The first and last rows and columns of tensors of more than 2^31 elements."""
+    dev = require_gpu()
+    M, K = 66000, 32768
+    Y, R = (torch.ones(1, M, K, dtype=BF, device=dev) for _ in range(2))
+    for t in (Y, R):
+        t[0, -70:].normal_()
+    g = (1 + 0.1 * torch.randn(K, device=dev)).to(BF)
+    H, X = torch.empty_like(R), torch.empty_like(Y)
+    Xt, e = torch.empty(1, K, M, dtype=BF, device=dev), torch.empty(K, dtype=torch.float64, device=dev)
+    kw = dict(post_norm=True, post_gamma=g, pre_gamma=g, eps=EPS)
+    for out in (dict(Xt=Xt, energy=e), dict(X=X)):
+        H.zero_()
+        rmm.rmm_block_join(Y, R, H, **out, **kw)
+        for rows in (slice(0, 70), slice(M - 70, M)):
+            check_h(H[:, rows], Y[:, rows], R[:, rows], True, g, None, 1.0, BF)
+            check_x(X[:, rows] if "X" in out else Xt[:, :, rows].transpose(1, 2), H[:, rows], g, BF)
+    squares = torch.zeros(K, dtype=torch.float64, device=dev)
+    for r in range(0, M, 3000):
+        assert torch.equal(Xt[0, :, r:r + 3000].T, X[0, r:r + 3000])
+        squares += X[0, r:r + 3000].double().square().sum(0)
+    check_energies(e.cpu().numpy(), squares.cpu().numpy(), M + 1)

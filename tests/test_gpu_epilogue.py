@@ -172,3 +172,17 @@ def test_activation_over_its_range(form, act):
     y, tol = ref.product(X, W, idx, b, act, None, 1.0, dt)
     assert bool(Y.isfinite().all())
     check(Y, (y, tol))
+
+
+@pytest.mark.parametrize("form", ["kmajor", "rows"])
+def test_past_32_bit_offsets(form):
+    """The last rows of an output and a residual of more than 2^31 elements."""
+    dev = require_gpu()
+    M, N, K, k = 40000, 56000, 16, 8
+    X, W, idx, b, _ = make(dev, BF, 1, M, N, K, k, seed=9, residual=False)
+    Y = torch.empty(1, M, N, dtype=BF, device=dev)
+    R = torch.ones(1, M, N, dtype=BF, device=dev)
+    R[:, -300:].normal_()
+    call(form, X, W, idx, Y, bias=b, act="relu", residual=R)
+    for rows in (slice(0, 200), slice(M - 300, M)):
+        check(Y[:, rows], ref.product(X[:, rows], W, idx, b, "relu", R[:, rows], 1.0, BF))

@@ -206,3 +206,13 @@ def test_long_rows_past_32_bit_offsets():
     rmm.rmm_token_logprobs(z, entropy=en, top_idx=idx, top_logp=lp)
     check(z[-2:], None, 3, 1.0, (None, en[-2:], idx[-2:], lp[-2:]))
     assert bool((idx[:-2].cpu() == torch.arange(3, dtype=torch.int32)).all())
+
+
+@pytest.mark.parametrize("given", [0, 65, 300, 1000])
+@pytest.mark.parametrize("V", [700, 40000])
+def test_many_given_tokens(given, V):
+    """More given tokens than a workgroup has threads; none beside the largest."""
+    dev = require_gpu()
+    z, _ = logits(dev, 3, V, BF, seed=7)
+    tok = torch.randint(0, V, (3, given), device=dev, dtype=torch.int32)
+    check(z, tok if given else None, 4, 1.0, run(z, tok, 4) if given else (None, *run(z, tok, 4)[1:]))
