@@ -36,7 +36,7 @@ constexpr double kLn2 = 0.69314718055994530942;
 struct Part {                            // one piece of a row
     double S, D;
     float b;
-    int set;                             // whether b is (some logit above -infinity)
+    int set;                             // some logit is above -infinity, or NaN
 };
 
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -232,9 +232,10 @@ __device__ __forceinline__ double base_weight(float b, float to, float c) {
 __device__ __forceinline__ Part join_parts(Part mine, float c) {
     const float b = wave_max(mine.set ? mine.b : -__builtin_inff());
     Part r = {0.0, 0.0, b, __ballot(mine.set) != 0};
-    // a NaN base (of a part whose only logits are NaN) leaves S one
+    // A NaN among a part's logits is in its S, never in its base (the largest of the
+    // others, 0 without any): it reaches the row whatever that base weighs.
     const double f = mine.set ? base_weight(mine.b, b, c) : 0.0;
-    const bool some = mine.set && f != 0.0;
+    const bool some = mine.set && (f != 0.0 || mine.S != mine.S);
     r.S = wave_sum(some ? f * mine.S : 0.0);
     r.D = wave_sum(some ? f * (mine.D + mine.S * static_cast<double>((mine.b - b) * c)) : 0.0);
     return r;

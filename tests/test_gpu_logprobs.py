@@ -216,3 +216,43 @@ def test_many_given_tokens(given, V):
     z, _ = logits(dev, 3, V, BF, seed=7)
     tok = torch.randint(0, V, (3, given), device=dev, dtype=torch.int32)
     check(z, tok if given else None, 4, 1.0, run(z, tok, 4) if given else (None, *run(z, tok, 4)[1:]))
+
+
+def nan_rows(z, tok, top, entropy=True):
+    """Every result of z's rows, each of which holds a NaN, but the ranking is NaN."""
+    lp, en, ti, tl = run(z, tok, top, entropy=entropy)
+    assert bool(lp.isnan().all()), "logp"
+    assert en is None or bool(en.isnan().all()), "entropy"
+    if top:
+        assert torch.equal(ti.long(), ref.top_tokens(z, top)) and bool(tl.isnan().all()), "top"
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,V", [(1, 513), (1, 9000), (1, 150000), (5, 20000), (1300, 1500), (1300, 9000)])
+@pytest.mark.parametrize("rest", ["lowest", "-inf", "low"])
+def test_a_nan_among_masked_logits(dt, T, V, rest):
+    """One NaN where every other logit is masked or far below: its wave's base weighs
+    nothing beside the row's."""
+    dev = require_gpu()
+    low = {"lowest": torch.finfo(dt).min, "-inf": -math.inf, "low": -300.0}[rest]
+    for at in (V - 1, 512, V // 2):
+        z, tok = logits(dev, T, V, dt, seed=8)
+        z[:, 300:] = low
+        z[:, at] = math.nan
+        nan_rows(z, tok % 300, 6)
+        nan_rows(z, tok % 300, 0, entropy=False)
+        z[:, at] = low                       # without it the row is an ordinary one
+        check(z, tok % 300, 6, 1.0, run(z, tok % 300, 6))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,V", [(1, 513), (1, 9000), (1, 150000), (5, 20000), (1300, 1500), (1300, 9000)])
+@pytest.mark.parametrize("level", [100.0, 300.0, -300.0])
+def test_a_run_of_nan(dt, T, V, level):
+    """Waves and pieces of nothing but NaN beside logits far from 0."""
+    dev = require_gpu()
+    z, tok = logits(dev, T, V, dt, seed=9)
+    z += level
+    z[:, min(512, V - 1):] = math.nan
+    nan_rows(z, tok % 512, 6)
+    nan_rows(z, tok % 512, 0, entropy=False)
