@@ -16,6 +16,11 @@ struct Epilogue {
     int act;
 };
 
+// Y of a kernel that may have an epilogue (EP): it may then be the residual itself,
+// which the same threads read through ep.res
+template <bool EP, class T>
+using OutPtr = std::conditional_t<EP, T *, T *__restrict__>;
+
 constexpr int kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kActGeluTanh = 4;
 
 // T: the output's type.  Where it is bf16 the forms below err by at most 2^-16 |x|
@@ -133,7 +138,7 @@ __device__ __forceinline__ char *ep_at(char *row, int r, int n) {
 // Every wave's reads of the ring and loads into it have ended before the call.
 // left: rows from the tile's origin on; row0: the origin's row over all units.
 template <int BN, int NW, int PASSES, int TM, class Put, class Obj>
-__device__ __forceinline__ void ep_tile(const Epilogue &ep, Put put, Obj obj, int wave, int lane, uint16_t *__restrict__ Y,
+__device__ __forceinline__ void ep_tile(const Epilogue &ep, Put put, Obj obj, int wave, int lane, uint16_t *Y,
                                         int64_t ldy, bool aligned16, int n0, int N, int left, int64_t row0) {
     constexpr int LPR = BN / 8, RPI = 64 / LPR, Q = 64 / (NW * RPI);     // lanes per row, rows per step
     const int c = lane % LPR, nc = N - n0 - 8 * c;

@@ -27,7 +27,7 @@ namespace {
 template <int BM, int BN, int BK, int WM, int WN, bool VECW, bool EP = false>
 __global__ __launch_bounds__(WM *WN *kWave) void gemm_gather_bf16_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W,
-    const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
+    const int32_t *__restrict__ idx, OutPtr<EP, uint16_t> Y, int M, int N, int k,
     int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}, bool vec_y = false) {
     constexpr int NT = WM * WN * kWave;
     constexpr int TM = BM / WM, TN = BN / WN;        // per-wave tile
@@ -172,7 +172,7 @@ __device__ __forceinline__ int at(int row, int chunk) { return row * BK + ((chun
 template <int NW, bool EP = false>
 __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_gather_bf16_big_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W,
-    const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
+    const int32_t *__restrict__ idx, OutPtr<EP, uint16_t> Y, int M, int N, int k,
     int64_t ldx, int64_t ldw, int64_t ldy, int64_t w_bytes, int tiles_m, int tiles_n, Epilogue ep = {},
     bool vec_y = false) {
     using namespace big;
@@ -410,7 +410,7 @@ __device__ __forceinline__ uint32_t swiglu_bf16(uint32_t gb, uint32_t ub) {
 template <int NW, int BKS, int S, int EPI = 0, int BNT = 256, int OCC = NW / 4>
 __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
     const uint16_t *__restrict__ Xt, const uint16_t *__restrict__ W,
-    const int32_t *__restrict__ idx, uint16_t *__restrict__ Y, int M, int N, int k,
+    const int32_t *__restrict__ idx, OutPtr<EPI == 2, uint16_t> Y, int M, int N, int k,
     int64_t ldxt, int64_t ldw, int64_t ldy, int64_t xt_bytes, int64_t w_bytes, int tiles_m,
     int tiles_n, int vec_y, double *__restrict__ part, int64_t w_ustride = 0, int w_ugroup = 1,
     int trim = 0, int64_t trim_off = 0, Epilogue ep = {}) {
@@ -865,7 +865,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
 template <int BM, int BN, int BK, bool VECW, bool VECY, bool EP = false>
 __global__ __launch_bounds__(256) void gemm_gather_f32_kernel(
     const float *__restrict__ X, const float *__restrict__ W, const int32_t *__restrict__ idx,
-    float *__restrict__ Y, int M, int N, int k, int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}) {
+    OutPtr<EP, float> Y, int M, int N, int k, int64_t ldx, int64_t ldw, int64_t ldy, Epilogue ep = {}) {
     constexpr int LS = BK + 4;                       // floats per LDS row
     constexpr int FM = BM / 32, FN = BN / 32;        // 16 x 16 fragments per wave
     constexpr int RPP = 256 / BK, XR = BM / RPP;     // X rows per pass and per thread

@@ -66,7 +66,7 @@ __device__ __forceinline__ int mid_swz(int r) {
 template <int BM, int BN, int WM, int WN, int BKS, int S, bool EP = false>
 __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kernel(
     const uint16_t *__restrict__ Xt, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
-    uint16_t *__restrict__ Y, int B, int M, int N, int k, int64_t ldxt, int64_t ldw, int64_t ldy,
+    OutPtr<EP, uint16_t> Y, int B, int M, int N, int k, int64_t ldxt, int64_t ldw, int64_t ldy,
     int64_t xt_bytes, int64_t w_bytes, int tiles_m, int tiles_n, int vec_y, int64_t w_ustride,
     int w_ugroup, int trim, int64_t trim_off, Epilogue ep = {}) {
     constexpr int NW = WM * WN, NT = NW * 64;

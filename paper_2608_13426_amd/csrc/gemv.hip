@@ -34,7 +34,7 @@ constexpr int MIN_SLICE = 64;      // retained rows per slice at least
 template <int MR, bool VEC, bool EP = false>
 __device__ __forceinline__ void gemv_tile(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
-    float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
+    float *__restrict__ P, OutPtr<EP, uint16_t> Y, int M, int N, int K, int k, int64_t ldx,
     int64_t ldw, int64_t ldy, int SR, int S, int chunk, int s, int b, bool DIRECT,
     const Epilogue &ep = Epilogue{}) {
     using namespace gv;
@@ -156,7 +156,7 @@ __device__ __forceinline__ void gemv_tile(
 template <int MG, bool EP>
 __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
-    float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
+    float *__restrict__ P, OutPtr<EP, uint16_t> Y, int M, int N, int K, int k, int64_t ldx,
     int64_t ldw, int64_t ldy, int SR, int S, Epilogue ep) {
     using namespace gv;
     constexpr int MR = 4 * MG, XS = RB + 4;    // xs rows apart in LDS (elements)
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
 template <int MR, bool VEC, bool DIRECT, bool EP = false>
 __global__ __launch_bounds__(gv::NT) void gemv_partial_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
-    float *__restrict__ P, uint16_t *__restrict__ Y, int M, int N, int K, int k, int64_t ldx,
+    float *__restrict__ P, OutPtr<EP, uint16_t> Y, int M, int N, int K, int k, int64_t ldx,
     int64_t ldw, int64_t ldy, int SR, int S, Epilogue ep = {}) {
     gemv_tile<MR, VEC, EP>(X, W, idx, P, Y, M, N, K, k, ldx, ldw, ldy, SR, S, blockIdx.x, blockIdx.y,
                            blockIdx.z, DIRECT, ep);
@@ -362,7 +362,7 @@ __device__ __forceinline__ float reduce_slices(const float *__restrict__ p, int6
 // reduce_slices; workgroup (x, m, b) covers columns 64x .. 64x+63
 template <bool EP = false>
 __global__ __launch_bounds__(256) void gemv_reduce_kernel(const float *__restrict__ P,
-                                                          uint16_t *__restrict__ Y, int M, int N,
+                                                          OutPtr<EP, uint16_t> Y, int M, int N,
                                                           int S, int64_t ldy, Epilogue ep = {}) {
     const int n = blockIdx.x * 64 + (threadIdx.x & 63);
     const int m = blockIdx.y, b = blockIdx.z;

@@ -186,3 +186,21 @@ def test_past_32_bit_offsets(form):
     call(form, X, W, idx, Y, bias=b, act="relu", residual=R)
     for rows in (slice(0, 200), slice(M - 300, M)):
         check(Y[:, rows], ref.product(X[:, rows], W, idx, b, "relu", R[:, rows], 1.0, BF))
+
+
+@pytest.mark.parametrize("form,dt,B,M,N,k", [("kmajor", BF, 1, 700, 1000, 50), ("kmajor", BF, 2, 90, 61, 30), ("kmajor", BF, 40, 4200, 120, 40),
+                                             ("kmajor", BF, 1, 2100, 4096, 50), ("rows", BF, 1, 2048, 4096, 50), ("rows", BF, 2, 130, 77, 50),
+                                             ("rows", F32, 2, 130, 256, 50), ("rows", F32, 1, 130, 77, 50), ("rows", F32, 1, 1100, 1028, 50),
+                                             ("few", BF, 2, 1, 1024, 50), ("few", BF, 2, 1, 1001, 900), ("few", BF, 2, 5, 1024, 50),
+                                             ("few", BF, 1, 8, 1001, 900), ("few", BF, 1, 3, 1024, 900)])
+@pytest.mark.parametrize("act", [None, "silu"])
+def test_in_place_is_the_same_bits(form, dt, B, M, N, k, act):
+    """A residual that is Y gives what it gives elsewhere, in every kernel."""
+    dev = require_gpu()
+    X, W, idx, b, R = make(dev, dt, B, M, N, 1000, k, seed=10)
+    Y = torch.empty(B, M, N, dtype=dt, device=dev)
+    kw = dict(bias=b, act=act, residual_scale=0.75)
+    call(form, X, W, idx, Y, residual=R, **kw)
+    Z = R.clone()
+    call(form, X, W, idx, Z, residual=Z, **kw)
+    assert torch.equal(Y, Z)
