@@ -1033,7 +1033,7 @@ rmm_status_t rmm_block_join(const rmm_join_t *join, void *workspace, size_t work
  * Errors    : INVALID_ARGUMENT for null pointers, sizes < 1, ldl < V, a scale that is
  *             not positive or infinite, negative given or top, top > V, nothing asked
  *             for, pointers off their type's alignment; UNSUPPORTED for top > 64, T >=
- *             2^22 or V >= 2^30; WORKSPACE_TOO_SMALL.
+ *             2^22, V >= 2^30 or given >= 2^30; WORKSPACE_TOO_SMALL.
  */
 size_t rmm_token_logprobs_workspace_size(int64_t T, int64_t V, int64_t top);
 rmm_status_t rmm_token_logprobs(const void *logits, rmm_dtype_t dtype, int64_t T, int64_t V, int64_t ldl,

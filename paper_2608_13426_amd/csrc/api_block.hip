@@ -16,6 +16,7 @@ constexpr int64_t kGridYZMax = 65535;
 constexpr int64_t kMaxRows = int64_t(1) << 22;     // a launch holds fewer than 2^32 threads
 
 constexpr int64_t kMaxVocab = int64_t(1) << 30;    // a row's indices and its last chunk's end in 32 bits
+constexpr int64_t kMaxGiven = int64_t(1) << 30;    // so are a row's given tokens and a thread's step past them
 
 inline size_t align256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 inline bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -195,7 +196,7 @@ rmm_status_t rmm_token_logprobs(const void *logits, rmm_dtype_t dtype, int64_t T
     if (!aligned(logits, size) || !aligned(tokens, 4) || !aligned(logp, 4) || !aligned(entropy, 4) ||
         !aligned(top_idx, 4) || !aligned(top_logp, 4))
         return RMM_ERR_INVALID_ARGUMENT;
-    if (top > rmm::kMaxTop || T >= kMaxRows || V >= kMaxVocab || given > kInt32Max) return RMM_ERR_UNSUPPORTED;
+    if (top > rmm::kMaxTop || T >= kMaxRows || V >= kMaxVocab || given >= kMaxGiven) return RMM_ERR_UNSUPPORTED;
     const size_t need = rmm_token_logprobs_workspace_size(T, V, top);
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return RMM_ERR_WORKSPACE_TOO_SMALL;

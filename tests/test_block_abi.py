@@ -178,3 +178,12 @@ def test_binding_refusals():
         p(z.t().contiguous().t(), entropy=torch.zeros(4))
     with pytest.raises(ValueError, match="GPU"):
         p(z, entropy=torch.zeros(4))
+
+
+def test_given_tokens_end_below_the_index_range():
+    """A row's loop over its given tokens goes by threads: near 2^31 its index would wrap to negative ones."""
+    def call(given):
+        return rmm.lib.rmm_token_logprobs(P, 1, 1, 1000, 1000, 1.0, P, given, P, None, 0, None, None, P, 1 << 40, None)
+
+    for given in (2 ** 30, 2 ** 31 - 256, 2 ** 31 - 1):
+        assert call(given) == UNSUPPORTED, given
