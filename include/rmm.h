@@ -231,7 +231,8 @@ rmm_status_t rmm_check_indices(const int32_t *idx, int64_t B, int64_t k, int64_t
  * The operands are gathered on the fly inside the GEMM; no compacted copy
  * of X[:, I] or W[I, :] is written to memory.
  * Errors: INVALID_ARGUMENT for null pointers, sizes < 1, k outside [1, K],
- *         ld too small, sizes above INT32_MAX.
+ *         ld too small, sizes above INT32_MAX; UNSUPPORTED for B > 65535,
+ *         M > 65535*64, N or k above 2^31 - 1024.
  */
 rmm_status_t rmm_reduced_gemm(const void *X, const void *W, const int32_t *idx,
                               rmm_dtype_t dtype, int64_t B, int64_t M, int64_t N,
@@ -907,7 +908,7 @@ rmm_status_t rmm_paged_attention(int64_t T, const rmm_heads_t *q, const rmm_kv_c
  *           product's type, or NULL.  residual: of the product's type, [B][M][ldr]
  *           (units M*ldr apart), or NULL (residual_scale is then not read); it may
  *           be Y itself (ldr == ldy) and must not overlap it otherwise.
- * Everything else as rmm_reduced_gemm (B <= 65535, M <= 65535*32),
+ * Everything else as rmm_reduced_gemm (but M <= 65535*32),
  * rmm_reduced_gemm_kmajor and rmm_reduced_gemv (bf16, M <= 8; workspace
  * rmm_gemv_workspace_size).
  * Errors  : as those, and INVALID_ARGUMENT for an unknown act, ldr < N, a

@@ -40,7 +40,7 @@ rmm_status_t check_gemm_shapes(const void *X, const void *W, rmm_dtype_t dt, int
     if (k < 1 || k > K) return RMM_ERR_INVALID_ARGUMENT;
     if (ldx < K || ldw < N || ldy < N) return RMM_ERR_INVALID_ARGUMENT;
     if (K > kInt32Max || M > kInt32Max || N > kInt32Max) return RMM_ERR_INVALID_ARGUMENT;
-    if (B > kGridYZMax || M > kGridYZMax * 64) return RMM_ERR_UNSUPPORTED;
+    if (B > kGridYZMax || M > kGridYZMax * 64 || N > rmm::kMaxStepped || k > rmm::kMaxStepped) return RMM_ERR_UNSUPPORTED;
     return RMM_OK;
 }
 

@@ -47,7 +47,7 @@ rmm_status_t check_product(const void *X, const void *W, const int32_t *idx, int
     if (B < 1 || M < 1 || N < 1 || K < 1 || k < 1 || k > K) return RMM_ERR_INVALID_ARGUMENT;
     if (ldw < N || ldy < N) return RMM_ERR_INVALID_ARGUMENT;
     if (K > kInt32Max || M > kInt32Max || N > kInt32Max) return RMM_ERR_INVALID_ARGUMENT;
-    if (B > kGridYZMax) return RMM_ERR_UNSUPPORTED;
+    if (B > kGridYZMax || N > rmm::kMaxStepped || k > rmm::kMaxStepped) return RMM_ERR_UNSUPPORTED;
     return RMM_OK;
 }
 

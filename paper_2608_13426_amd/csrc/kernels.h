@@ -64,6 +64,9 @@ hipError_t launch_check_indices(const int32_t *idx, int64_t B, int64_t k, int64_
 // ------------------------------------------------------- gathered GEMM
 // ep: null, or the product's epilogue (epilogue.h)
 struct Epilogue;
+// N and k at most: the kernels step both by whole tiles in 32 bits, up to 320 past
+// their ends
+constexpr int64_t kMaxStepped = (int64_t(1) << 31) - 1024;
 hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t *idx,
                             int64_t B, int64_t M, int64_t N, int64_t K, int64_t k,
                             int64_t ldx, int64_t ldw, uint16_t *Y, int64_t ldy,

@@ -187,3 +187,14 @@ def test_given_tokens_end_below_the_index_range():
 
     for given in (2 ** 30, 2 ** 31 - 256, 2 ** 31 - 1):
         assert call(given) == UNSUPPORTED, given
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_products_end_below_the_index_range(dtype):
+    """The row-major products step k and N by whole tiles in 32 bits, past the last column and index."""
+    gemm = forms()[0]
+    for n in (2 ** 31 - 1023, 2 ** 31 - 1):
+        assert gemm(ep(ldr=n), dtype=dtype, N=n, ldw=n, ldy=n) == UNSUPPORTED
+        assert gemm(ep(), dtype=dtype, M=1, K=n, k=n, ldx=n) == UNSUPPORTED
+        assert rmm.lib.rmm_reduced_gemm(P, P, P, dtype, 1, 4, n, 128, 32, 128, n, P, n, None) == UNSUPPORTED
+        assert rmm.lib.rmm_reduced_gemm(P, P, P, dtype, 1, 1, 64, n, n, n, 64, P, 64, None) == UNSUPPORTED
