@@ -23,10 +23,12 @@ using OutPtr = std::conditional_t<EP, T *, T *__restrict__>;
 
 constexpr int kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3, kActGeluTanh = 4;
 
-// T: the output's type.  Where it is bf16 the forms below err by at most 2^-16 |x|
-// (a 128th of what the rounding may), in as few operations as that takes: they run
-// on every output of a tile while its matrix cores wait (8192 x 14336 outputs of
-// 2048 retained indices: 406 us as a plain product, 428 with bias and silu).
+// T: the output's type.  Where it is bf16 gelu's negative side a Phi(-a) is off by 3e-5
+// of itself and the forms below by at most 3e-5 of their value (the rounding: 2^-8 of it),
+// in as few operations as that takes: they run on every output of a tile while its matrix
+// cores wait (8192 x 14336 outputs of 2048 retained indices: 406 us as a plain product,
+// 428 with bias and silu).  fp32 gelu is 1 + erf: exact to the argument's size, not to its
+// own where that is far smaller.
 template <int ACT, class T>
 __device__ __forceinline__ float activate(float x) {
     constexpr bool kFast = sizeof(T) == 2;
@@ -35,7 +37,8 @@ __device__ __forceinline__ float activate(float x) {
     if constexpr (ACT == kActGelu && !kFast) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
     if constexpr (ACT == kActGelu && kFast) {
         // x Phi(x) = max(x, 0) - a Phi(-a), a = |x|; log2 Phi(-a) as a polynomial of
-        // degree 8, least largest error on [0, 10] (3e-5 of Phi); past 10, a Phi(-a) < 1e-22
+        // degree 8, least largest error on [0, 10] (of Phi: 1.9e-5, with the fp32 steps'
+        // rounding 2.8e-5); past 10, a Phi(-a) < 1e-22
         const float a = fminf(fabsf(x), 10.f);
         float p = 6.003541844e-08f;
         p = fmaf(p, a, -3.129991683e-06f);

@@ -204,3 +204,47 @@ def test_in_place_is_the_same_bits(form, dt, B, M, N, k, act):
     Z = R.clone()
     call(form, X, W, idx, Z, residual=Z, **kw)
     assert torch.equal(Y, Z)
+
+
+def tail_bound(x, act, out):
+    """(y, bound) of an activation alone, relative to its value: on the far negative side
+    that is what keeps a wrong or missing tail from passing.
+
+    silu: rounding the exponent's argument moves e^-x by 2 u32 |x| (argument and
+    constant), exponential, sum, reciprocal and product add 8 u32.  gelu_tanh: its
+    argument w of 2^w is off by up to 4 roundings, 3 u32 |w| of the value.  bf16 gelu:
+    a Phi(-a) from the polynomial, off by 1.9e-5 as given and by up to 1e-5 through its
+    rounding to fp32 (largest last steps: 2^-18 + 10 * 2^-22 + 100 * 2^-25 of a log2), 5e-5
+    in all; past |x| = 10 it stays below 1e-22.  Where 2^126 is passed a reciprocal is 0: |y| < 2e-36."""
+    x = x.double()
+    if act == "silu":
+        y = x * torch.sigmoid(x)
+        e = (2 * x.abs() + 8) * ref.U32 * y.abs()
+    elif act == "gelu_tanh":
+        u = math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)
+        y = x * torch.sigmoid(2 * u)
+        e = (3 * 2 * u.abs() / math.log(2) + 8) * ref.U32 * y.abs()
+    else:
+        y = 0.5 * x * torch.erfc(-x * math.sqrt(0.5))
+        e = 5e-5 * 0.5 * x.abs() * torch.erfc(x.abs() * math.sqrt(0.5)) + 2 * ref.U32 * y.clamp_min(0) + 1e-22 * (x.abs() > 10)
+    return y, e + ref.U[out] * (y.abs() + e) + 2e-36
+
+
+# fp32 gelu, 1 + erf, is exact to the argument's size only (test_activation_over_its_range)
+TAILS = [(*f, act) for f in (("kmajor", BF, 8, 8), ("rows", BF, 8, 8), ("few", BF, 1, 8), ("few", BF, 1, 2048), ("few", BF, 5, 8),
+                             ("few", BF, 5, 2048), ("rows", F32, 8, 8)) for act in ("silu", "gelu", "gelu_tanh") if (f[1], act) != (F32, "gelu")]
+
+
+@pytest.mark.parametrize("form,dt,M,K,act", TAILS)
+def test_activation_tails(form, dt, M, K, act):
+    """Far negative arguments, as biases of an empty product: each output is as exact as its own size."""
+    dev = require_gpu()
+    b = torch.cat([torch.linspace(-20, 20, 4000), torch.linspace(-7, 0, 3000), torch.tensor([-30.0, -50.0, -80.0, -1e3, 1e3])]).to(dev).to(dt)
+    N = b.numel()
+    X, W = torch.zeros(1, M, K, dtype=dt, device=dev), torch.zeros(K, (N + 7) // 8 * 8, dtype=dt, device=dev)[:, :N]
+    idx = torch.arange(K, dtype=torch.int32, device=dev)
+    Y = torch.empty(1, M, N, dtype=dt, device=dev)
+    call(form, X, W, idx, Y, bias=b, act=act)
+    y, tol = tail_bound(b, act, dt)
+    err = (Y.double() - y).abs() / tol
+    assert float(err.max()) <= 1, (float(err.max()), float(b[int(err.amax((0, 1)).argmax())]))
