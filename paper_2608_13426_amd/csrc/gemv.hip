@@ -13,6 +13,8 @@
 // in flight), and the waves' sums are added in a fixed order in LDS.  Slices write fp32 partials that a second kernel adds in slice
 // order (or, with one slice, the workgroup writes Y directly), so results
 // are bit-reproducible.
+#include <type_traits>
+
 #include "device_common.h"
 #include "epilogue.h"
 #include "kernels.h"
@@ -417,29 +419,28 @@ template <bool VEC, bool EP>
 hipError_t launch_vec(const uint16_t *X, const uint16_t *W, const int32_t *idx, int64_t B, int64_t M,
                       int64_t N, int64_t K, int64_t k, int64_t ldx, int64_t ldw, uint16_t *Y,
                       int64_t ldy, float *P, int SR, int S, const Epilogue &ep, hipStream_t stream) {
-    if constexpr (VEC && EP) {
-        if (M > 1) {
-            const dim3 grid(static_cast<unsigned>((N + gv::CW - 1) / gv::CW), static_cast<unsigned>(S), static_cast<unsigned>(B));
-            auto quads = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, grid, dim3(gv::NT), 0, stream, X, W, idx, P, Y, static_cast<int>(M),
-                                   static_cast<int>(N), static_cast<int>(K), static_cast<int>(k), ldx, ldw, ldy, SR, S, ep);
-                return hipGetLastError();
-            };
-            const hipError_t e = M <= 4 ? quads(gemv_quad_kernel<1, EP>) : quads(gemv_quad_kernel<2, EP>);
-            if (e != hipSuccess || S == 1) return e;
-            hipLaunchKernelGGL(gemv_reduce_kernel<EP>, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>(M),
-                                                           static_cast<unsigned>(B)), dim3(256), 0, stream, P, Y,
-                               static_cast<int>(M), static_cast<int>(N), S, ldy, ep);
-            return hipGetLastError();
-        }
-    }
     auto go = [&](auto mr) {
         return launch_mr<decltype(mr)::value, VEC, EP>(X, W, idx, B, M, N, K, k, ldx, ldw, Y, ldy, P, SR, S, ep, stream);
     };
     if (M == 1) return go(std::integral_constant<int, 1>{});
-    if (M == 2) return go(std::integral_constant<int, 2>{});
-    if (M <= 4) return go(std::integral_constant<int, 4>{});
-    return go(std::integral_constant<int, 8>{});
+    if constexpr (VEC && EP) {
+        const dim3 grid(static_cast<unsigned>((N + gv::CW - 1) / gv::CW), static_cast<unsigned>(S), static_cast<unsigned>(B));
+        auto quads = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(gv::NT), 0, stream, X, W, idx, P, Y, static_cast<int>(M),
+                               static_cast<int>(N), static_cast<int>(K), static_cast<int>(k), ldx, ldw, ldy, SR, S, ep);
+            return hipGetLastError();
+        };
+        const hipError_t e = M <= 4 ? quads(gemv_quad_kernel<1, EP>) : quads(gemv_quad_kernel<2, EP>);
+        if (e != hipSuccess || S == 1) return e;
+        hipLaunchKernelGGL(gemv_reduce_kernel<EP>, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>(M),
+                                                       static_cast<unsigned>(B)), dim3(256), 0, stream, P, Y,
+                           static_cast<int>(M), static_cast<int>(N), S, ldy, ep);
+        return hipGetLastError();
+    } else {
+        if (M == 2) return go(std::integral_constant<int, 2>{});
+        if (M <= 4) return go(std::integral_constant<int, 4>{});
+        return go(std::integral_constant<int, 8>{});
+    }
 }
 
 }  // namespace
