@@ -154,8 +154,9 @@ def rmm_block_join(Y: torch.Tensor | None, R: torch.Tensor | None, H: torch.Tens
     y = norm(Y) * post_gamma with post_norm, else Y; H = residual_scale * R + gate * y,
     stored in the stream's type (bf16 or fp32); X = norm(H) * pre_gamma, or with Xt
     [B, K, M] and energy (float64 [B*K]) its K-major copy and column energies (bf16;
-    needs H).  gate: [K], or broadcastable to [B, M, K] with contiguous rows of K;
-    gammas [K] or None (ones).  Y or R may be None, and outputs that are not wanted.
+    needs H; fastest where Xt's rows lie a multiple of 64 elements apart).  gate: [K], or
+    three-dimensional and broadcastable to [B, M, K], with contiguous rows of K; gammas [K]
+    or None (ones).  Y or R may be None, and outputs that are not wanted.
     H may be R, X may be Y.  `workspace` (uint8, rmm_block_join_workspace_size(B, M, K)
     bytes, 256-byte aligned) is allocated here when Xt is wanted and it is not given.
     Returns H, X and Xt, those that were given."""
@@ -185,7 +186,7 @@ def rmm_block_join(Y: torch.Tensor | None, R: torch.Tensor | None, H: torch.Tens
             raise TypeError(f"gate must be {dt}")
         if gate.dim() not in (1, 3) or gate.shape[-1] != K or (K > 1 and gate.stride(-1) != 1) or \
                 (gate.dim() == 3 and (gate.shape[0] not in (1, B) or gate.shape[1] not in (1, M))):
-            raise ValueError("gate must be [K] or broadcastable to [B, M, K], with contiguous rows")
+            raise ValueError("gate must be [K], or three-dimensional and broadcastable to [B, M, K], with contiguous rows")
         if gate.dim() == 3:
             gu = gate.stride(0) if gate.shape[0] > 1 else 0
             gr = gate.stride(1) if gate.shape[1] > 1 else 0
@@ -193,8 +194,6 @@ def rmm_block_join(Y: torch.Tensor | None, R: torch.Tensor | None, H: torch.Tens
     d = _device_index(Y, R, H, X, Xt, energy, post_gamma, gate, pre_gamma, workspace)
     if Xt is not None:
         ldxt = _unit_rows(Xt, (B, K, M), torch.bfloat16, "Xt")
-        if B * K == 1:                       # one row: any padded length serves
-            ldxt = (M + 7) // 8 * 8
         if workspace is None:
             workspace = _scratch(rmm_block_join_workspace_size(B, M, K), some.device, stream)
         ws_bytes = workspace.nbytes
