@@ -154,7 +154,8 @@ __device__ __forceinline__ void gemv_tile(
 // group's four values of each column together, and 8 (up to 4 rows) or 16
 // products follow, against 4 * (8 + 8 M) operations in the form above.
 // Three units of 5 x 4096 -> 6144, a set of 2048 each: 39 us in that form, 20 so (21
-// with two groups on their way); 8 x 14336 -> 4096, k = 7168: 30 and 19 (4 rows: 18 and 16).
+// with two groups on their way); 8 x 14336 -> 4096, k = 7168: 29 and 17 (4 rows: 18 and
+// 16; 2 rows: 15 both).
 template <int MG, bool EP>
 __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
     const uint16_t *__restrict__ X, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,

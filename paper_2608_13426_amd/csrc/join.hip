@@ -297,7 +297,10 @@ hipError_t launch_rows(const JoinArgs &a, hipStream_t stream) {
     // 256 x 2 / 128 x 4: 4.6 / 5.0 / 6.3 us).  From 4096 waves on: two to four chunks per
     // thread (8192 x 4096 bf16, 512 x 1 / 256 x 2 / 128 x 4 / 64 x 8: 63 / 56 / 58 / 66 us;
     // 8192 x 2048, 512 x 1 / 256 x 2 / 64 x 4: 46 / 36 / 32; 2002 x 8192 with an fp32
-    // stream, 1024 x 1 / 512 x 2 / 256 x 4: 45.6 / 44.8 / 48.8)
+    // stream, 1024 x 1 / 512 x 2 / 256 x 4: 45.6 / 44.8 / 48.8).  Past 16384 a row is still
+    // held whole, eight chunks a thread, most of them absent just past it: 45 to 112 of its 128
+    // registers go to scratch, and its time is far from the copy's (2^25 bf16 in all, K =
+    // 16384 53 us; 16392 217, 20480 188, 32768 133, 65536 98).
     const auto many = [&](int waves) { return a.rows * waves >= 4096; };
     if (a.K <= 64 * 8) return go(join_rows_kernel<TY, TS, TAIL, 64, 1>, 64);
     if (a.K <= 128 * 8) return many(1) ? go(join_rows_kernel<TY, TS, TAIL, 64, 2>, 64) : go(join_rows_kernel<TY, TS, TAIL, 128, 1>, 128);

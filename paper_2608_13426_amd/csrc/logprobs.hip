@@ -427,7 +427,9 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             add(std::true_type{});
         }
         if (a.top == 0) return;
-        const bool nan = __ballot(sums.s != sums.s) != 0;    // a NaN has made s one
+        // A NaN has made s one: from its first on every logit of the wave is offered (2048 x
+        // 128000, the 5 largest: 108 us, with one NaN at the start of one row 136, of every row 305)
+        const bool nan = __ballot(sums.s != sums.s) != 0;
         // nothing compares with a limit of NaN: all pass
         float lim = __builtin_nanf("");
         if (!nan && !fresh) {
@@ -552,8 +554,8 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
     write_row<T>(a, row, p, list.key);
 }
 
-// Up to 2048 workgroups of one chunk per wave: one step each.  Beyond, steps of 64
-// bytes per lane.
+// Up to 512 workgroups (2048 waves): one chunk per wave and step, so one step each up to
+// 64 pieces' 131072 logits.  Beyond, steps of 64 bytes per lane.
 bool one_step(int64_t T, int64_t V) { return T * std::min<int64_t>(kMaxPieces, (V + kWaves * kChunk - 1) / (kWaves * kChunk)) <= 512; }
 
 template <typename T>

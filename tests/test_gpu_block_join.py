@@ -260,3 +260,16 @@ def test_past_32_bit_offsets():
         assert torch.equal(Xt[0, :, r:r + 3000].T, X[0, r:r + 3000])
         squares += X[0, r:r + 3000].double().square().sum(0)
     check_energies(e.cpu().numpy(), squares.cpu().numpy(), M + 1)
+
+
+@pytest.mark.parametrize("sd", [BF, F32])
+@pytest.mark.parametrize("M,K", [(1, 64), (77, 1024), (300, 4096)])
+def test_the_stream_itself_as_h(M, K, sd):
+    """A norm of the stream alone, K-major, with the stream as H: it keeps its bits, and Xt and the energies are as with a copy."""
+    dev = require_gpu()
+    _, R, _, gq, _ = make(dev, BF, sd, 2, M, K, seed=11)
+    R0, H = R.clone(), torch.empty_like(R)
+    (_, xa, ea), (_, xb, eb) = (kmajor(dev, 2, M, K) for _ in range(2))
+    rmm.rmm_block_join(None, R, H, Xt=xa, energy=ea, pre_gamma=gq, eps=EPS)
+    rmm.rmm_block_join(None, R, R, Xt=xb, energy=eb, pre_gamma=gq, eps=EPS)
+    assert torch.equal(R, R0) and torch.equal(H, R0) and torch.equal(xa, xb) and torch.equal(ea, eb)
