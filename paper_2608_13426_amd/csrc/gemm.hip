@@ -18,6 +18,7 @@
 #include "device_common.h"
 #include "epilogue.h"
 #include "kernels.h"
+#include "span.h"
 
 namespace rmm {
 
@@ -411,7 +412,7 @@ template <int NW, int BKS, int S, int EPI = 0, int BNT = 256, int OCC = NW / 4>
 __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
     const uint16_t *__restrict__ Xt, const uint16_t *__restrict__ W,
     const int32_t *__restrict__ idx, OutPtr<EPI == 2, uint16_t> Y, int M, int N, int k,
-    int64_t ldxt, int64_t ldw, int64_t ldy, int64_t xt_bytes, int64_t w_bytes, int tiles_m,
+    int64_t ldxt, int64_t ldw, int64_t ldy, int64_t xt_unit, int64_t xt_bytes, int64_t w_bytes, int tiles_m,
     int tiles_n, int vec_y, double *__restrict__ part, int64_t w_ustride = 0, int w_ugroup = 1,
     int trim = 0, int64_t trim_off = 0, Epilogue ep = {}) {
     using namespace trk;
@@ -479,8 +480,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void gemm_kmajor_tr_kernel(
 
     constexpr uint32_t kOut = 0x80000000u;
     const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t *>(Xt + unit * (xt_bytes / 2)), 0, static_cast<uint32_t>(xt_bytes),
-        0x00020000);
+        const_cast<uint16_t *>(Xt + unit * xt_unit), 0, static_cast<uint32_t>(xt_bytes), 0x00020000);
     // units u read weights W + (u / w_ugroup) * w_ustride (one matrix for all
     // units unless the caller groups them, e.g. query heads sharing a value head)
     const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc(
@@ -1046,9 +1046,9 @@ hipError_t launch_gemm_bf16(const uint16_t *X, const uint16_t *W, const int32_t 
     (void)K;
     const bool vec = (reinterpret_cast<uintptr_t>(W) % 16 == 0) && (ldw % 8 == 0);
     const int64_t big_tiles = ((M + big::BM - 1) / big::BM) * ((N + big::BN - 1) / big::BN);
-    const int64_t w_bytes = K * ldw * 2;
+    const int64_t w_bytes = span_bytes(K, ldw, N);
     const bool offsets_fit = static_cast<int64_t>(big::BM + 1) * ldx * 2 < (int64_t(1) << 31) &&
-                             w_bytes + ldw * 2 < (int64_t(1) << 31);
+                             K * ldw * 2 + ldw * 2 < (int64_t(1) << 31);
     const bool vec_y = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0;
     if (vec && offsets_fit && big_tiles * B >= 128) {
         const int tm = static_cast<int>((M + big::BM - 1) / big::BM);
@@ -1131,7 +1131,7 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
                            int64_t M, int64_t N, int64_t K, int64_t k, int64_t ldxt, int64_t ldw,
                            uint16_t *Y, int64_t ldy, int64_t w_ustride, int w_ugroup,
                            int trim, int64_t trim_off, const Epilogue *ep, hipStream_t stream) {
-    const int64_t xt_bytes = K * ldxt * 2, w_bytes = K * ldw * 2;
+    const int64_t xt_bytes = span_bytes(K, ldxt, M), w_bytes = span_bytes(K, ldw, N);
     const bool grouped = (w_ustride != 0 && w_ugroup < B) || trim;
     // the 256 x 256 kernel addresses one tile's Y rows with 32-bit byte offsets
     const bool big_ok = ldy < (int64_t(1) << 23);
@@ -1153,7 +1153,7 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
         auto launch = [&](auto kernel, int waves, int tn_) {
             hipLaunchKernelGGL(kernel, dim3(tm * tn_, static_cast<unsigned>(B)), dim3(waves * 64), 0, stream, Xt, W,
                                idx, Y, static_cast<int>(M), static_cast<int>(N), static_cast<int>(k), ldxt, ldw, ldy,
-                               xt_bytes, w_bytes, tm, tn_, vec_y, nullptr, w_ustride, w_ugroup, trim, trim_off, *ep);
+                               K * ldxt, xt_bytes, w_bytes, tm, tn_, vec_y, nullptr, w_ustride, w_ugroup, trim, trim_off, *ep);
             return hipGetLastError();
         };
         return tall ? launch(gemm_kmajor_tr_kernel<4, kTrRows, kTrStages, 2, 128, 2>, 4, 1)
@@ -1163,14 +1163,14 @@ hipError_t kmajor_dispatch(const uint16_t *Xt, const uint16_t *W, const int32_t 
         hipLaunchKernelGGL((gemm_kmajor_tr_kernel<4, kTrRows, kTrStages, 0, 128, 2>),
                            dim3(tm, static_cast<unsigned>(B)), dim3(4 * 64), 0, stream,
                            Xt, W, idx, Y, static_cast<int>(M), static_cast<int>(N),
-                           static_cast<int>(k), ldxt, ldw, ldy, xt_bytes, w_bytes, tm, 1, vec_y,
+                           static_cast<int>(k), ldxt, ldw, ldy, K * ldxt, xt_bytes, w_bytes, tm, 1, vec_y,
                            nullptr, w_ustride, w_ugroup, trim, trim_off);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((gemm_kmajor_tr_kernel<kTrWaves, kTrRows, kTrStages>),
                        dim3(tm * tn, static_cast<unsigned>(B)), dim3(kTrWaves * 64), 0, stream,
                        Xt, W, idx, Y, static_cast<int>(M), static_cast<int>(N),
-                       static_cast<int>(k), ldxt, ldw, ldy, xt_bytes, w_bytes, tm, tn, vec_y,
+                       static_cast<int>(k), ldxt, ldw, ldy, K * ldxt, xt_bytes, w_bytes, tm, tn, vec_y,
                        nullptr, w_ustride, w_ugroup, trim, trim_off);
     return hipGetLastError();
 }
@@ -1198,12 +1198,12 @@ hipError_t launch_gemm_swiglu_kmajor_bf16(const uint16_t *Xt, const uint16_t *W,
                                          int64_t K, int64_t k, int64_t ldxt, int64_t ldw,
                                          uint16_t *Ht, int64_t ldht, double *energy,
                                          double *partials, hipStream_t stream) {
-    const int64_t xt_bytes = K * ldxt * 2, w_bytes = K * ldw * 2;
+    const int64_t xt_bytes = span_bytes(K, ldxt, M), w_bytes = span_bytes(K, ldw, 2 * F);
     const int tm = static_cast<int>((M + 255) / 256), tn = static_cast<int>(F / 128);
     hipLaunchKernelGGL((gemm_kmajor_tr_kernel<kTrWaves, kTrRows, kTrStages, 1>),
                        dim3(tm * tn, static_cast<unsigned>(B)), dim3(kTrWaves * 64), 0, stream,
                        Xt, W, idx, Ht, static_cast<int>(M), static_cast<int>(2 * F),
-                       static_cast<int>(k), ldxt, ldw, ldht, xt_bytes, w_bytes, tm, tn, 2, partials);
+                       static_cast<int>(k), ldxt, ldw, ldht, K * ldxt, xt_bytes, w_bytes, tm, tn, 2, partials);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // energies: the row tiles' partial sums, added in tile order

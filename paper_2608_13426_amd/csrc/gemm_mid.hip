@@ -36,6 +36,7 @@
 #include "device_common.h"
 #include "epilogue.h"
 #include "kernels.h"
+#include "span.h"
 
 namespace rmm {
 
@@ -67,7 +68,7 @@ template <int BM, int BN, int WM, int WN, int BKS, int S, bool EP = false>
 __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kernel(
     const uint16_t *__restrict__ Xt, const uint16_t *__restrict__ W, const int32_t *__restrict__ idx,
     OutPtr<EP, uint16_t> Y, int B, int M, int N, int k, int64_t ldxt, int64_t ldw, int64_t ldy,
-    int64_t xt_bytes, int64_t w_bytes, int tiles_m, int tiles_n, int vec_y, int64_t w_ustride,
+    int64_t xt_unit, int64_t xt_bytes, int64_t w_bytes, int tiles_m, int tiles_n, int vec_y, int64_t w_ustride,
     int w_ugroup, int trim, int64_t trim_off, Epilogue ep = {}) {
     constexpr int NW = WM * WN, NT = NW * 64;
     constexpr int RA = BM * 2, RB = BN * 2;             // bytes per staged row
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN / 4) void gemm_kmajor_mid_kerne
 
     constexpr uint32_t kOut = 0x80000000u;
     const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t *>(Xt + unit * (xt_bytes / 2)), 0, static_cast<uint32_t>(xt_bytes), 0x00020000);
+        const_cast<uint16_t *>(Xt + unit * xt_unit), 0, static_cast<uint32_t>(xt_bytes), 0x00020000);
     const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(W + (unit / w_ugroup) * w_ustride), 0, static_cast<uint32_t>(w_bytes), 0x00020000);
     const uint32_t arow = static_cast<uint32_t>(ldxt) * 2u, brow = static_cast<uint32_t>(ldw) * 2u;
@@ -372,7 +373,8 @@ hipError_t launch_mid(const uint16_t *Xt, const uint16_t *W, const int32_t *idx,
     auto launch = [&](auto kernel, const Epilogue &e) {
         hipLaunchKernelGGL(kernel, grid, dim3(WM * WN * 64), 0,
                            stream, Xt, W, idx, Y, static_cast<int>(B), static_cast<int>(M), static_cast<int>(N),
-                           static_cast<int>(k), ldxt, ldw, ldy, K * ldxt * 2, K * ldw * 2, static_cast<int>(tm),
+                           static_cast<int>(k), ldxt, ldw, ldy, K * ldxt, span_bytes(K, ldxt, M),
+                           span_bytes(K, ldw, N), static_cast<int>(tm),
                            static_cast<int>(tn), vec_y, w_ustride, w_ugroup, trim, trim_off, e);
         return hipGetLastError();
     };

@@ -18,6 +18,7 @@
 #include "device_common.h"
 #include "epilogue.h"
 #include "kernels.h"
+#include "span.h"
 
 namespace rmm {
 
@@ -50,11 +51,11 @@ __device__ __forceinline__ void gemv_tile(
     const int t0 = s * SR, t1 = min(k, t0 + SR);
     const int32_t *I = idx + static_cast<int64_t>(b) * k;
     const uint16_t *Xb = X + static_cast<int64_t>(b) * M * ldx;
-    // the whole of W from this chunk's first column on: a row's columns past
-    // N read padding or the next row, and past the matrix's end read zeros
+    // the whole of W from this chunk's first column on: a row's columns past N read
+    // padding or the next row, and past the last row's end zeros
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(W + n0), 0,
-        static_cast<uint32_t>((static_cast<int64_t>(K) * ldw - n0) * 2), 0x00020000);
+        static_cast<uint32_t>(span_bytes(K, ldw, N, VEC) - n0 * 2), 0x00020000);
 
     float acc[MR][8];
 #pragma unroll
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(gv::NT) void gemv_quad_kernel(
     const uint16_t *Xb = X + static_cast<int64_t>(b) * M * ldx;
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(W + n0), 0,
-        static_cast<uint32_t>((static_cast<int64_t>(K) * ldw - n0) * 2), 0x00020000);
+        static_cast<uint32_t>(span_bytes(K, ldw, N) - n0 * 2), 0x00020000);
 
     f32x4_t acc[MG][8];                        // [rows 4g ..][the lane's column]
 #pragma unroll

@@ -40,6 +40,7 @@
 
 #include "device_common.h"
 #include "kernels.h"
+#include "span.h"
 #include "gemv_shared.h"
 
 namespace rmm {
@@ -314,10 +315,10 @@ void share_product_kernel(ShareGroups G, int B) {
     __syncthreads();
 
     // W rows from column n0 on; columns past N read padding or the next row
-    // (never stored), rows past the matrix's end read zeros
+    // (never stored), past the last row's end zeros
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(q.W + n0), 0,
-        static_cast<uint32_t>((static_cast<int64_t>(q.K) * q.ldw - n0) * 2), 0x00020000);
+        static_cast<uint32_t>(span_bytes(q.K, q.ldw, q.N) - n0 * 2), 0x00020000);
     // the run's xs rows (sequences past B are never read)
     const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(q.xs + static_cast<int64_t>(r0) * 32 * RG), 0,
