@@ -248,3 +248,20 @@ def test_activation_tails(form, dt, M, K, act):
     y, tol = tail_bound(b, act, dt)
     err = (Y.double() - y).abs() / tol
     assert float(err.max()) <= 1, (float(err.max()), float(b[int(err.amax((0, 1)).argmax())]))
+
+
+@pytest.mark.parametrize("B,M,N,K,k", [(2, 1001, 4097, 1000, 610), (1, 3000, 3000, 600, 300), (40, 4200, 120, 200, 100), (1, 100, 100, 4096, 2048),
+                                       (1, 2048, 4096, 600, 50)])
+@pytest.mark.parametrize("form,dt", [("kmajor", BF), ("rows", BF), ("rows", F32)])
+def test_without_an_epilogue_the_plain_bits_whatever_the_tiles(form, dt, B, M, N, K, k):
+    """The tile rules differ (prompts of an odd width); the order of a sum does not."""
+    dev = require_gpu()
+    X, W, idx, _, _ = make(dev, dt, B, M, N, K, k, seed=12, bias=False, residual=False)
+    Y, Z = (torch.empty(B, M, N, dtype=dt, device=dev) for _ in range(2))
+    call(form, X, W, idx, Y)
+    if form == "kmajor":
+        Xt = torch.zeros(B, K, (M + 7) // 8 * 8, dtype=dt, device=dev)[:, :, :M]
+        rmm.rmm_reduced_gemm_kmajor(Xt.copy_(X.transpose(1, 2)), W, idx, Z)
+    else:
+        rmm.rmm_reduced_gemm(X, W, idx, Z)
+    assert torch.equal(Y, Z)
